@@ -57,13 +57,19 @@ enum {
     TLI_ROW_FALLBACK = 8,         /* empty intersection or zero residual mass: sampled from p instead */
     TLI_ROW_TIMEOUT = 16,         /* a bounded wait inside a kernel ran out: results not to be trusted.  Sticky: every
                                    * later call on the context reports it too, until tli_reset() */
-    TLI_ROW_BAD_TEMPERATURE = 32  /* temperature negative or not finite: accepted = 0, next_token = 0 */
+    TLI_ROW_BAD_TEMPERATURE = 32, /* temperature negative or not finite: accepted = 0, next_token = 0 */
+    TLI_ROW_BAD_FILTER = 64       /* top_p or min_p is NaN (tli_sample(), tli_filter()) */
 };
+
+/* which of the context's two vocabularies ids, rows of logits or an embedding table belong to */
+enum { TLI_SIDE_TARGET = 0, TLI_SIDE_DRAFTER = 1 };
 
 #define TLI_MAX_B 65535    /* sequences per call */
 #define TLI_MAX_K 64       /* drafts per sequence */
 #define TLI_MAX_V 1048576  /* vocabulary size (either side) */
 #define TLI_MAX_SHARDS 64   /* vocabulary shards (tli_shard_create) */
+#define TLI_MAX_TOKENS 4194304 /* tokens per call of tli_embed() and tli_embed_grad() */
+#define TLI_MAX_H 65536     /* width of an embedding row */
 #define TLI_STATIC_SCRATCH_BYTES 4194304 /* 4 MiB: scratch built into the library for tli_verify_static() */
 
 /*
@@ -428,6 +434,147 @@ int tli_shard_stats(tli_ctx *ctx, const tli_verify_args *args, void *record_out,
 int tli_shard_decide(tli_ctx *ctx, const tli_verify_args *args, const void *records_all, void *rows_out, void *cuda_stream);
 int tli_shard_weights(tli_ctx *ctx, const tli_verify_args *args, const void *rows_all, void *mass_out, void *cuda_stream);
 int tli_shard_select(tli_ctx *ctx, const tli_verify_args *args, const void *rows_all, const void *masses_all, void *cuda_stream);
+
+/*
+ * Filtered sampling.  A server's requests carry top-k, top-p and min-p beside
+ * the temperature; these two calls apply them, tli_sample() by drawing an id
+ * from what is left of a row, tli_filter() by writing the row with -inf outside
+ * it.  (The paper samples at plain temperature; filters compose with it because
+ * Algorithm 5 is lossless for whatever p and q' it is given: run tli_filter()
+ * over the target rows and over the drafter rows the drafts were drawn from,
+ * then tli_verify() on the filtered rows, and the emitted tokens follow the
+ * *filtered* target distribution.)
+ *
+ * The kept set of a row z with tau = temperature[b] > 0.  The ids that take part
+ * are all of the row on the target side, those inside the intersection on the
+ * drafter side, without those whose logit is -inf.  They are ordered by logit,
+ * largest first, equal logits by id, lowest first; w = exp((z - max z) / tau).
+ *   top_k >= 1    keeps the first top_k (exactly that many, ties or not); <= 0: off
+ *   top_p < 1     of those, keeps the shortest run from the front whose mass is at
+ *                 least top_p times the mass of those; >= 1: off
+ *   min_p > 0     keeps ids with w >= min_p, i.e. at least min_p times as probable as
+ *                 the first; <= 0: off
+ * The first id is always kept.  tau == 0 keeps it alone, whatever the filters say.
+ *
+ * Weights and sums are fp64: the kept set and the id drawn equal those of the
+ * definition unless a mass lies within fp64 rounding of its border, and do not
+ * depend on timing.  Both calls are asynchronous on the stream, allocate
+ * nothing, only launch kernels (they can be captured) and use of the context
+ * only its maps: calls on one context may overlap if their workspaces and outputs
+ * are distinct.  Errors as for tli_verify(); a context of tli_shard_create() is
+ * refused.  The context's device must be current.
+ */
+typedef struct {
+    int32_t B;      /* sequences, >= 1 */
+    int32_t R;      /* rows per sequence, >= 1; B * R <= TLI_MAX_B */
+    int32_t dtype;  /* TLI_F32 or TLI_BF16 */
+    int32_t side;   /* TLI_SIDE_TARGET: rows of V_t logits; TLI_SIDE_DRAFTER: rows of V_d, the
+                     * ids inside the intersection take part (sampling from q') */
+
+    /* [device] logits [B, R, V]; strides in elements (0 repeats a row), vocabulary axis
+     * contiguous, base pointer aligned to the element size. */
+    const void *logits;
+    int64_t stride_b, stride_r;
+
+    const float *temperature;   /* [device] float[B] */
+    const int32_t *top_k;       /* [device] int32[B]; NULL = off */
+    const float *top_p;         /* [device] float[B]; NULL = off */
+    const float *min_p;         /* [device] float[B]; NULL = off */
+    const float *uniforms;      /* [device] float[B, R] in [0, 1) */
+
+    int32_t *tokens;            /* [device] out int32[B, R]: the drawn id (of `side`): the lowest kept id whose
+                                 * cumulative weight, in increasing id order, exceeds uniforms * total; -1
+                                 * when the row is flagged */
+    float *prob;                /* [device] out float[B, R]: its probability among the kept ids (0 when
+                                 * flagged); may be NULL */
+    int32_t *status;            /* [device] out int32[B, R] of TLI_ROW_* bits: NONFINITE (NaN or +inf among the
+                                 * ids that take part), FALLBACK (no id takes part), BAD_TEMPERATURE, BAD_FILTER;
+                                 * may be NULL */
+
+    void *workspace;            /* [device] scratch, 256-byte aligned, >= tli_sample_workspace_bytes() */
+    size_t workspace_bytes;
+} tli_sample_args;
+
+/* Bytes of device scratch tli_sample() needs for (B, R, dtype, side); 0 on bad arguments. */
+size_t tli_sample_workspace_bytes(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, int32_t side);
+int tli_sample(tli_ctx *ctx, const tli_sample_args *args, void *cuda_stream);
+
+typedef struct {
+    int32_t B, R, dtype, side;  /* as in tli_sample_args */
+    const void *logits;
+    int64_t stride_b, stride_r;
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+
+    /* [device] out [B, R, V] in the rows' type: the logit where it is kept, -inf elsewhere.  May be
+     * `logits` itself with the same strides (in place); any other overlap with it, or of
+     * its rows with one another, is an error.  A flagged row is copied unchanged (so that a later
+     * call flags it too), except that a row without ids (FALLBACK) becomes -inf. */
+    void *out;
+    int64_t out_stride_b, out_stride_r;
+
+    int32_t *status;            /* [device] out int32[B, R]; may be NULL */
+    void *workspace;            /* [device] scratch, 256-byte aligned, >= tli_filter_workspace_bytes() */
+    size_t workspace_bytes;
+} tli_filter_args;
+
+size_t tli_filter_workspace_bytes(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, int32_t side);
+int tli_filter(tli_ctx *ctx, const tli_filter_args *args, void *cuda_stream);
+
+/*
+ * Embedding rows for ids of either vocabulary.  The drafts that tli_verify()
+ * checks are drafter ids and enter the target's forward pass as target
+ * embeddings; its next_token is a target id and enters the drafter's.  This call
+ * carries ids to the table's vocabulary (the id map, its inverse, or
+ * neither) and looks the rows up:
+ *     out[i] = scale * table[t(ids[i])]        one rounding to the type of the rows
+ * An id outside its vocabulary or without a counterpart in the table's
+ * gives a row of zeros and table_ids[i] = -1.  Asynchronous on the stream,
+ * allocates nothing, launches one kernel, uses of the context only its maps.
+ */
+typedef struct {
+    int32_t N;                  /* tokens, 0 .. TLI_MAX_TOKENS */
+    int32_t H;                  /* width of a row, 1 .. TLI_MAX_H */
+    int32_t dtype;              /* TLI_F32 or TLI_BF16, of table and out */
+    int32_t ids_side, table_side; /* TLI_SIDE_*: vocabulary of the ids, of the table */
+    const int32_t *ids;         /* [device] int32[N] */
+    const void *table;          /* [device] [V, H], V the table side's size; rows contiguous */
+    int64_t table_stride;       /* elements from row to row */
+    float scale;
+    void *out;                  /* [device] out [N, H] */
+    int64_t out_stride;         /* elements from row to row, >= H */
+    int32_t *table_ids;         /* [device] out int32[N]: the ids in the table's vocabulary; may be NULL */
+} tli_embed_args;
+
+int tli_embed(tli_ctx *ctx, const tli_embed_args *args, void *cuda_stream);
+
+/*
+ * The gradient of tli_embed() with respect to the table, for fine-tuning a
+ * drafter (or a target) on tokens of either vocabulary:
+ *     out[v] = scale * sum over i with t(ids[i]) == v of grad[i]
+ * Every row of out is written (zeros where no token refers to it).  Sums are
+ * fp32 over the tokens sorted by (row, position): the result does not depend on
+ * timing, and is rounded once.  Asynchronous, allocates nothing, only launches
+ * kernels, uses of the context only its maps.
+ */
+typedef struct {
+    int32_t N, H;               /* as in tli_embed_args */
+    int32_t grad_dtype;         /* TLI_F32 or TLI_BF16 */
+    int32_t out_dtype;          /* TLI_F32 or TLI_BF16 */
+    int32_t ids_side, table_side;
+    const int32_t *ids;         /* [device] int32[N] */
+    const void *grad;           /* [device] [N, H]; rows contiguous */
+    int64_t grad_stride;        /* elements from row to row (0: one row for all tokens) */
+    float scale;
+    void *out;                  /* [device] out [V, H] */
+    int64_t out_stride;         /* elements from row to row, >= H; what lies between rows is left alone */
+    void *workspace;            /* [device] scratch, 256-byte aligned, >= tli_embed_grad_workspace_bytes() */
+    size_t workspace_bytes;
+} tli_embed_grad_args;
+
+size_t tli_embed_grad_workspace_bytes(const tli_ctx *ctx, int32_t N, int32_t H);
+int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *args, void *cuda_stream);
 
 /*
  * How tli_verify() will run a batch of this shape on this context: [host]

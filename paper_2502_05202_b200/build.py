@@ -1,4 +1,4 @@
-"""Build step: compiles csrc/tli.cu for sm_100a into libtli.so beside this file."""
+"""Build step: compiles csrc/tli_lib.cu (one translation unit of csrc/*.cu) for sm_100a into libtli.so beside this file."""
 from __future__ import annotations
 
 import os
@@ -7,7 +7,8 @@ import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SRC = os.path.join(_HERE, "csrc", "tli.cu")
+SRC = os.path.join(_HERE, "csrc", "tli_lib.cu")
+PARTS = [os.path.join(_HERE, "csrc", n) for n in ("tli.cu", "tli_rows.cu", "tli_embed.cu")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(_HERE, "libtli.so")
 
@@ -24,7 +25,7 @@ def _nvcc() -> str:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; returns its path."""
-    deps = [SRC, os.path.join(INCLUDE, "tli.h")]
+    deps = [SRC] + PARTS + [os.path.join(INCLUDE, "tli.h")]
     if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= os.path.getmtime(d) for d in deps):
         return LIB
     tmp = LIB + ".tmp.%d" % os.getpid()

@@ -1,0 +1,571 @@
+// Embedding rows for ids of either vocabulary, and the gradient of that lookup.
+// (Part of tli_lib.cu: uses tli_ctx and the error helpers of tli.cu.)
+//
+//   tli_embed_kernel       out[i] = scale * table[t(ids[i])], t the id map, its inverse or the identity; one warp per
+//                          token and run of 128 vectors.  A copy: bound by DRAM, or for a decoding step by the
+//                          chain id -> map -> row.
+//   gradient               dW[v] = scale * sum over the tokens i with t(ids[i]) = v of g[i], every row written.
+//       tli_grad_sort_kernel     tokens by (table id, position), least significant digit first, two digits of ten bits,
+//                                stable, so that every sum below has one order whatever the timing; the other CTAs of
+//                                the same grid fill dW with zeros meanwhile (the dense write is the floor).
+//       tli_grad_count_kernel, tli_grad_scatter_kernel   the same sort over several CTAs for many tokens.
+//       tli_grad_sum_kernel      a window of sorted tokens per group of threads: rows whose tokens all lie in the
+//                                window are written, the pieces of a row that crosses a window go to the workspace.
+//       tli_grad_join_kernel     adds the pieces of such a row in window order.
+// Sums are fp32 (a row is rounded once, after the scale).
+
+namespace {
+
+constexpr int kEmbThreads = 256;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kDigits = 1024;
+constexpr int kSumThreads = 128;
+
+// table id of a token, -1 if it has none
+__device__ __forceinline__ int table_id(const int *map, int n_ids, int id) {
+    if (id < 0 || id >= n_ids) return -1;
+    return map ? __ldg(map + id) : id;
+}
+
+struct EmbedParams {
+    int N, H, n_ids, chunks;
+    const int *map, *ids;
+    const void *table; long long ts;
+    void *out; long long os;
+    float scale;
+    int *table_ids;
+};
+
+template <int DT> __device__ __forceinline__ uint4 scale_vector(const uint4 &r, float c) {
+    float z[Elt<DT>::kPerVec];
+    unpack<DT>(r, z);
+    if constexpr (DT == TLI_F32) {
+        return make_uint4(__float_as_uint(z[0] * c), __float_as_uint(z[1] * c), __float_as_uint(z[2] * c), __float_as_uint(z[3] * c));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)                                // one rounding, to nearest even
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(z[2 * i + 1] * c), "f"(z[2 * i] * c));
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <int DT> __device__ __forceinline__ float element(const void *p, long long i) {
+    if constexpr (DT == TLI_F32) return __ldg(reinterpret_cast<const float *>(p) + i);
+    else return __uint_as_float(static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short *>(p) + i)) << 16);
+}
+template <int DT> __device__ __forceinline__ void set_element(void *p, long long i, float x) {
+    if constexpr (DT == TLI_F32) {
+        reinterpret_cast<float *>(p)[i] = x;
+    } else {
+        unsigned short h;
+        asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(x));
+        reinterpret_cast<unsigned short *>(p)[i] = h;
+    }
+}
+
+constexpr int kEmbUnroll = 4;
+
+// VEC: rows of both sides lie on 16-byte boundaries and H is a whole number of vectors; otherwise element by element
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kEmbThreads) tli_embed_kernel(const EmbedParams P) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const long long task = static_cast<long long>(blockIdx.x) * (kEmbThreads / 32) + (threadIdx.x >> 5);
+    const int i = static_cast<int>(task / P.chunks), chunk = static_cast<int>(task % P.chunks), lane = threadIdx.x & 31;
+    if (i >= P.N) return;
+    const int t = table_id(P.map, P.n_ids, __ldg(P.ids + i));
+    if (chunk == 0 && lane == 0 && P.table_ids) P.table_ids[i] = t;
+    const int first = chunk * (32 * kEmbUnroll) + lane;
+    if constexpr (VEC) {
+        const int nv = P.H / Elt<DT>::kPerVec;
+        const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(P.table) + t * P.ts * Elt<DT>::kBytes);
+        uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<char *>(P.out) + i * P.os * Elt<DT>::kBytes);
+        uint4 r[kEmbUnroll];
+#pragma unroll
+        for (int q = 0; q < kEmbUnroll; ++q)
+            r[q] = t >= 0 && first + q * 32 < nv ? __ldg(src + first + q * 32) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < kEmbUnroll; ++q)
+            if (first + q * 32 < nv) dst[first + q * 32] = t >= 0 ? scale_vector<DT>(r[q], P.scale) : r[q];
+    } else {
+        float x[kEmbUnroll];
+#pragma unroll
+        for (int q = 0; q < kEmbUnroll; ++q)
+            x[q] = t >= 0 && first + q * 32 < P.H ? element<DT>(P.table, t * P.ts + first + q * 32) * P.scale : 0.f;
+#pragma unroll
+        for (int q = 0; q < kEmbUnroll; ++q)
+            if (first + q * 32 < P.H) set_element<DT>(P.out, i * P.os + first + q * 32, x[q]);
+    }
+}
+
+struct GradParams {
+    int N, H, n_ids, V, groups, tile;      // groups: CTAs of the sort; tile: tokens of one of them
+    int window, nwin, tx;                  // sorted tokens per window; threads across a row
+    const int *map, *ids;
+    const void *g; long long gs;
+    void *out; long long os;
+    float scale;
+    int *key[2], *pos[2];                  // [N]: sorted by the low digit, by both
+    int *n_valid;                          // tokens that have a table id
+    int *count;                            // [groups][kDigits]
+    float *piece;                          // [nwin][2][H]: of the row that came in from the window before, of the one that goes on
+};
+
+// One digit of the sort for tokens [first, last) of the source, by one CTA.  pass 0 takes the ids, pass 1 what
+// pass 0 left.  `before` [kDigits] in shared memory: where the digit's tokens of this CTA begin.
+struct SortShared { int wsum[kSortWarps]; };
+
+__device__ __forceinline__ int sort_key(const GradParams &P, int pass, int i, int &pos) {
+    if (pass == 0) { pos = i; return table_id(P.map, P.n_ids, __ldg(P.ids + i)); }
+    pos = __ldcg(P.pos[0] + i);
+    return __ldcg(P.key[0] + i);
+}
+__device__ __forceinline__ int digit_of(int pass, int key) { return pass == 0 ? key & (kDigits - 1) : key >> 10; }
+
+__device__ __forceinline__ int sort_scan(int x, SortShared &sh, int &total) {       // inclusive, over 1024 threads
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) sh.wsum[warp] = x;
+    __syncthreads();
+    int s = sh.wsum[lane], incl = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    const int before = __shfl_sync(0xffffffffu, incl - s, warp);
+    total = __shfl_sync(0xffffffffu, incl, 31);
+    __syncthreads();
+    return x + before;
+}
+
+__device__ void sort_digit(const GradParams &P, int pass, int cta, int n, int *cnt, SortShared &sh) {
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int first = min(n, cta * P.tile), last = min(n, first + P.tile);
+    const int chunk = ((last - first + kSortWarps - 1) / kSortWarps + 31) & ~31;     // a warp's tokens, in order
+    const int w0 = min(last, first + warp * chunk), w1 = min(last, w0 + chunk);
+    for (int i = tid; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
+    __syncthreads();
+    int *mine = cnt + warp * kDigits;
+    for (int i = w0 + lane; i < w1; i += 32) {
+        int pos;
+        const int key = sort_key(P, pass, i, pos);
+        if (key >= 0) atomicAdd(mine + digit_of(pass, key), 1);
+    }
+    __syncthreads();
+    // thread d: digit d
+    int sum = 0, others = 0, all = 0;
+    for (int w = 0; w < kSortWarps; ++w) {
+        const int c = cnt[w * kDigits + tid];
+        cnt[w * kDigits + tid] = sum;
+        sum += c;
+    }
+    if (P.groups > 1) {
+        for (int c = 0; c < P.groups; ++c) {
+            const int x = __ldcg(P.count + c * kDigits + tid);
+            if (c < cta) others += x;
+            all += x;
+        }
+    } else {
+        all = sum;
+    }
+    int total;
+    const int base = sort_scan(all, sh, total) - all + others;
+    if (pass == 0 && cta == 0 && tid == 0) *P.n_valid = total;
+    for (int w = 0; w < kSortWarps; ++w) cnt[w * kDigits + tid] += base;
+    __syncthreads();
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane;
+        int pos = 0;
+        const int key = i < w1 ? sort_key(P, pass, i, pos) : -1;
+        const int d = key >= 0 ? digit_of(pass, key) : -1;
+        const unsigned peers = __match_any_sync(0xffffffffu, d);
+        const int rank = __popc(peers & ((1u << lane) - 1u));
+        int at = 0;
+        if (d >= 0) at = mine[d] + rank;
+        __syncwarp();
+        if (d >= 0 && rank == 0) mine[d] += __popc(peers);
+        __syncwarp();
+        if (d >= 0) {
+            __stcg(P.key[pass] + at, key);
+            __stcg(P.pos[pass] + at, pos);
+        }
+    }
+    __syncthreads();
+}
+
+// dW = 0, by CTAs [0, n) of a grid
+template <int OT>
+__device__ void fill_zero(const GradParams &P, unsigned cta, unsigned n) {
+    const size_t step = static_cast<size_t>(n) * kSortThreads, me = static_cast<size_t>(cta) * kSortThreads + threadIdx.x;
+    if (P.os == P.H) {
+        char *p = reinterpret_cast<char *>(P.out);
+        const size_t bytes = static_cast<size_t>(P.V) * P.H * Elt<OT>::kBytes;
+        const size_t head = min(bytes, static_cast<size_t>((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15));
+        const size_t nv = (bytes - head) / 16;
+        uint4 *v = reinterpret_cast<uint4 *>(p + head);
+        for (size_t i = me; i < nv; i += step) v[i] = make_uint4(0, 0, 0, 0);
+        const size_t edge = bytes - nv * 16;                       // the bytes in front of and behind the vectors
+        for (size_t i = me; i < edge; i += step) p[i < head ? i : nv * 16 + i] = 0;
+    } else {
+        const size_t total = static_cast<size_t>(P.V) * P.H;
+        for (size_t i = me; i < total; i += step) set_element<OT>(P.out, static_cast<long long>(i / P.H) * P.os + i % P.H, 0.f);
+    }
+}
+
+template <int OT>
+__global__ void __launch_bounds__(kSortThreads) tli_grad_sort_kernel(const GradParams P) {
+    extern __shared__ __align__(16) int sort_smem[];
+    __shared__ SortShared sh;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const unsigned sorters = P.groups == 1 ? 1u : 0u;
+    if (blockIdx.x < sorters) {
+        sort_digit(P, 0, 0, P.N, sort_smem, sh);
+        sort_digit(P, 1, 0, __ldcg(P.n_valid), sort_smem, sh);
+        return;
+    }
+    fill_zero<OT>(P, blockIdx.x - sorters, gridDim.x - sorters);
+}
+
+__global__ void __launch_bounds__(kSortThreads) tli_grad_count_kernel(const GradParams P, int pass) {
+    __shared__ int cnt[kDigits];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    cnt[threadIdx.x] = 0;
+    __syncthreads();
+    const int n = pass == 0 ? P.N : __ldcg(P.n_valid);
+    const int first = min(n, static_cast<int>(blockIdx.x) * P.tile), last = min(n, first + P.tile);
+    for (int i = first + threadIdx.x; i < last; i += kSortThreads) {
+        int pos;
+        const int key = sort_key(P, pass, i, pos);
+        if (key >= 0) atomicAdd(cnt + digit_of(pass, key), 1);
+    }
+    __syncthreads();
+    P.count[blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kSortThreads) tli_grad_scatter_kernel(const GradParams P, int pass) {
+    extern __shared__ __align__(16) int sort_smem[];
+    __shared__ SortShared sh;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    sort_digit(P, pass, blockIdx.x, pass == 0 ? P.N : __ldcg(P.n_valid), sort_smem, sh);
+}
+
+// ---- sums over the sorted tokens ----
+//
+// Columns of a thread.  VEC: one 16-byte vector of the gradient; otherwise four columns, kSumThreads-like strides apart
+// so that a warp's loads stay together.
+template <int GT, bool VEC> struct Columns {
+    static constexpr int kN = VEC ? Elt<GT>::kPerVec : 4;
+    int col[VEC ? 1 : 4];
+    __device__ __forceinline__ Columns(const GradParams &P, int block) {
+        const int x = threadIdx.x % P.tx;
+        if constexpr (VEC) {
+            col[0] = (block * P.tx + x) * kN;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) col[k] = (block * 4 + k) * P.tx + x;
+        }
+    }
+    __device__ __forceinline__ bool any(const GradParams &P) const { return col[0] < P.H; }
+    __device__ __forceinline__ void load(const GradParams &P, long long i, float (&x)[kN]) const {
+        if constexpr (VEC) {
+            const uint4 r = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(P.g) + (i * P.gs + col[0]) * Elt<GT>::kBytes));
+            unpack<GT>(r, x);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = col[k] < P.H ? element<GT>(P.g, i * P.gs + col[k]) : 0.f;
+        }
+    }
+    template <int OT> __device__ __forceinline__ void store(const GradParams &P, int v, const float (&acc)[kN]) const {
+        if constexpr (VEC) {
+            char *p = reinterpret_cast<char *>(P.out) + (v * P.os + col[0]) * Elt<OT>::kBytes;
+            float z[kN];
+#pragma unroll
+            for (int k = 0; k < kN; ++k) z[k] = acc[k] * P.scale;
+            if constexpr (OT == TLI_F32) {
+#pragma unroll
+                for (int k = 0; k < kN; k += 4) reinterpret_cast<float4 *>(p)[k / 4] = make_float4(z[k], z[k + 1], z[k + 2], z[k + 3]);
+            } else {
+                uint32_t w[kN / 2];
+#pragma unroll
+                for (int k = 0; k < kN / 2; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(z[2 * k + 1]), "f"(z[2 * k]));
+                if constexpr (kN == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col[k] < P.H) set_element<OT>(P.out, v * P.os + col[k], acc[k] * P.scale);
+        }
+    }
+    // fp32 pieces in the workspace
+    __device__ __forceinline__ void put(const GradParams &P, float *p, const float (&acc)[kN]) const {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < kN; k += 4) __stcg(reinterpret_cast<float4 *>(p + col[0]) + k / 4, make_float4(acc[k], acc[k + 1], acc[k + 2], acc[k + 3]));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col[k] < P.H) __stcg(p + col[k], acc[k]);
+        }
+    }
+    __device__ __forceinline__ void add(const GradParams &P, const float *p, float (&acc)[kN]) const {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int k = 0; k < kN; k += 4) {
+                const float4 y = __ldcg(reinterpret_cast<const float4 *>(p + col[0]) + k / 4);
+                acc[k] += y.x; acc[k + 1] += y.y; acc[k + 2] += y.z; acc[k + 3] += y.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col[k] < P.H) acc[k] += __ldcg(p + col[k]);
+        }
+    }
+};
+
+constexpr int kSumBatch = 8;               // rows of the gradient a thread has in flight
+
+template <int GT, int OT, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const GradParams P) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n = __ldcg(P.n_valid);
+    const int win = blockIdx.x * (kSumThreads / P.tx) + threadIdx.x / P.tx;
+    const Columns<GT, VEC> c(P, blockIdx.y);
+    const int a = win * P.window, e = min(n, a + P.window);
+    if (win >= P.nwin || a >= e || !c.any(P)) return;
+    const int *key = P.key[1], *pos = P.pos[1];
+    constexpr int kN = Columns<GT, VEC>::kN;
+    float acc[kN] = {};
+    bool from_before = a > 0 && __ldcg(key + a - 1) == __ldcg(key + a);
+    int cur = __ldcg(key + a);
+    auto flush = [&](bool goes_on) {
+        if (from_before) c.put(P, P.piece + (static_cast<size_t>(win) * 2) * P.H, acc);          // (it may go on as well)
+        else if (goes_on) c.put(P, P.piece + (static_cast<size_t>(win) * 2 + 1) * P.H, acc);
+        else c.template store<OT>(P, cur, acc);
+    };
+    for (int i = a; i < e; i += kSumBatch) {
+        float x[kSumBatch][kN];
+        int k[kSumBatch];
+#pragma unroll
+        for (int j = 0; j < kSumBatch; ++j) {
+            k[j] = -1;
+            if (i + j < e) {
+                k[j] = __ldcg(key + i + j);
+                c.load(P, __ldcg(pos + i + j), x[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kSumBatch; ++j) {
+            if (k[j] < 0) break;
+            if (k[j] != cur) {
+                flush(false);
+                from_before = false;
+                cur = k[j];
+#pragma unroll
+                for (int q = 0; q < kN; ++q) acc[q] = x[j][q];
+            } else {
+#pragma unroll
+                for (int q = 0; q < kN; ++q) acc[q] += x[j][q];
+            }
+        }
+    }
+    flush(e < n && __ldcg(key + e) == cur);
+}
+
+// The row that begins in a window and goes on in the next ones.
+template <int GT, int OT, bool VEC>
+__global__ void __launch_bounds__(kSumThreads) tli_grad_join_kernel(const GradParams P) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int n = __ldcg(P.n_valid);
+    int win = blockIdx.x * (kSumThreads / P.tx) + threadIdx.x / P.tx;
+    const Columns<GT, VEC> c(P, blockIdx.y);
+    const int a = win * P.window, e = min(n, a + P.window);
+    if (win >= P.nwin || a >= e || e >= n || !c.any(P)) return;
+    const int *key = P.key[1];
+    const int cur = __ldcg(key + e - 1);
+    if (__ldcg(key + e) != cur) return;                            // ends in this window
+    if (a > 0 && __ldcg(key + a - 1) == cur) return;               // began before it
+    constexpr int kN = Columns<GT, VEC>::kN;
+    float acc[kN] = {};
+    c.add(P, P.piece + (static_cast<size_t>(win) * 2 + 1) * P.H, acc);
+    int at = e;
+    do {
+        ++win;
+        c.add(P, P.piece + (static_cast<size_t>(win) * 2) * P.H, acc);
+        at = min(n, at + P.window);
+    } while (at < n && __ldcg(key + at) == cur && __ldcg(key + at - 1) == cur);
+    c.template store<OT>(P, cur, acc);
+}
+
+// ---- host ----
+
+constexpr int kSortOneCta = 65536;         // tokens one CTA sorts (it runs beside the zero fill)
+constexpr int kSortTile = 16384;           // tokens per CTA beyond that
+
+struct GradLayout { int groups, tile, window, nwin; size_t key0, pos0, key1, pos1, n_valid, count, piece, total; };
+
+GradLayout grad_layout(int N, int H) {
+    GradLayout L;
+    L.groups = N <= kSortOneCta ? (N > 0) : (N + kSortTile - 1) / kSortTile;
+    L.tile = L.groups <= 1 ? N : kSortTile;
+    // short windows spread a frequent row over more threads; long ones keep the pieces of many tokens small
+    L.window = 32;
+    while (L.window < 256 && N / L.window > 8192) L.window *= 2;
+    L.nwin = (N + L.window - 1) / L.window;
+    size_t off = 0;
+    L.key0 = off; off = align_up(off + sizeof(int) * N, 256);
+    L.pos0 = off; off = align_up(off + sizeof(int) * N, 256);
+    L.key1 = off; off = align_up(off + sizeof(int) * N, 256);
+    L.pos1 = off; off = align_up(off + sizeof(int) * N, 256);
+    L.n_valid = off; off += 256;
+    L.count = off; off = align_up(off + (L.groups > 1 ? sizeof(int) * kDigits * L.groups : 0), 256);
+    L.piece = off; off = align_up(off + sizeof(float) * 2 * L.nwin * static_cast<size_t>(H), 256);
+    L.total = off;
+    return L;
+}
+
+int embed_side(const tli_ctx *ctx, int32_t ids_side, int32_t table_side, int &n_ids, int &V, const int *&map) {
+    if (ids_side != TLI_SIDE_TARGET && ids_side != TLI_SIDE_DRAFTER) return TLI_ERR_ARG;
+    if (table_side != TLI_SIDE_TARGET && table_side != TLI_SIDE_DRAFTER) return TLI_ERR_ARG;
+    n_ids = ids_side == TLI_SIDE_TARGET ? ctx->V_t : ctx->V_d;
+    V = table_side == TLI_SIDE_TARGET ? ctx->V_t : ctx->V_d;
+    map = ids_side == table_side ? nullptr : (ids_side == TLI_SIDE_DRAFTER ? ctx->d_map : ctx->d_inv);
+    return TLI_OK;
+}
+bool on_vectors(const void *p, int64_t stride, size_t elt) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * static_cast<int64_t>(elt) % 16 == 0;
+}
+void pdl_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, cudaStream_t stream) {
+    memset(&cfg, 0, sizeof cfg);
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
+}
+
+template <int GT, int OT, bool VEC> int launch_grad_sums(const GradParams &P, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    pdl_config(cfg, attr, stream);
+    constexpr int kN = Columns<GT, VEC>::kN;
+    const int per_block = P.tx * kN;
+    cfg.gridDim = dim3((P.nwin + kSumThreads / P.tx - 1) / (kSumThreads / P.tx), (P.H + per_block - 1) / per_block);
+    cfg.blockDim = dim3(kSumThreads);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, tli_grad_sum_kernel<GT, OT, VEC>, P);
+    if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_sum_kernel");
+    e = cudaLaunchKernelEx(&cfg, tli_grad_join_kernel<GT, OT, VEC>, P);
+    if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_join_kernel");
+    return TLI_OK;
+}
+
+template <int OT> int launch_grad(GradParams &P, int gdtype, int num_sms, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    pdl_config(cfg, attr, stream);
+    const size_t smem = sizeof(int) * kSortWarps * kDigits;
+    cudaError_t e = cudaFuncSetAttribute(tli_grad_sort_kernel<OT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(tli_grad_scatter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.gridDim = dim3(num_sms); cfg.dynamicSmemBytes = smem;
+    e = cudaLaunchKernelEx(&cfg, tli_grad_sort_kernel<OT>, P);
+    if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_sort_kernel");
+    if (P.N == 0) return TLI_OK;
+    if (P.groups > 1) {
+        for (int pass = 0; pass < 2; ++pass) {
+            cfg.gridDim = dim3(P.groups); cfg.dynamicSmemBytes = 0;
+            e = cudaLaunchKernelEx(&cfg, tli_grad_count_kernel, P, pass);
+            if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_count_kernel");
+            cfg.dynamicSmemBytes = smem;
+            e = cudaLaunchKernelEx(&cfg, tli_grad_scatter_kernel, P, pass);
+            if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_scatter_kernel");
+        }
+    }
+    const size_t ge = gdtype == TLI_F32 ? 4 : 2;
+    const bool vec = on_vectors(P.g, P.gs, ge) && on_vectors(P.out, P.os, Elt<OT>::kBytes) && P.H % 8 == 0;
+    const int across = vec ? P.H / (gdtype == TLI_F32 ? 4 : 8) : (P.H + 3) / 4;
+    P.tx = 1;
+    while (P.tx < kSumThreads && P.tx < across) P.tx *= 2;
+    if (gdtype == TLI_F32) return vec ? launch_grad_sums<TLI_F32, OT, true>(P, stream) : launch_grad_sums<TLI_F32, OT, false>(P, stream);
+    return vec ? launch_grad_sums<TLI_BF16, OT, true>(P, stream) : launch_grad_sums<TLI_BF16, OT, false>(P, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tli_embed(tli_ctx *ctx, const tli_embed_args *a, void *cuda_stream) {
+    if (!ctx || !a || ctx->n_shards != 1) return TLI_ERR_ARG;
+    if (a->N < 0 || a->H < 1) return TLI_ERR_ARG;
+    if (a->N > TLI_MAX_TOKENS || a->H > TLI_MAX_H) return TLI_ERR_UNSUPPORTED;
+    if (a->dtype != TLI_F32 && a->dtype != TLI_BF16) return TLI_ERR_ARG;
+    EmbedParams P;
+    int V;
+    const int rc = embed_side(ctx, a->ids_side, a->table_side, P.n_ids, V, P.map);
+    if (rc != TLI_OK) return rc;
+    if (a->N == 0) return TLI_OK;
+    if (!a->ids || !a->table || !a->out) return TLI_ERR_ARG;
+    const size_t elt = a->dtype == TLI_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(a->table) % elt || reinterpret_cast<uintptr_t>(a->out) % elt) return TLI_ERR_ARG;
+    if (a->table_stride < 0 || (a->N > 1 && a->out_stride < a->H)) return TLI_ERR_ARG;
+    P.N = a->N; P.H = a->H; P.ids = a->ids;
+    P.table = a->table; P.ts = a->table_stride;
+    P.out = a->out; P.os = a->out_stride;
+    P.scale = a->scale; P.table_ids = a->table_ids;
+    const int epv = static_cast<int>(16 / elt);
+    const bool vec = on_vectors(P.table, P.ts, elt) && on_vectors(P.out, P.os, elt) && P.H % epv == 0;
+    const int units = vec ? P.H / epv : P.H;
+    P.chunks = (units + 32 * kEmbUnroll - 1) / (32 * kEmbUnroll);
+    const long long tasks = static_cast<long long>(P.N) * P.chunks, per = kEmbThreads / 32;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    pdl_config(cfg, attr, reinterpret_cast<cudaStream_t>(cuda_stream));
+    cfg.gridDim = dim3(static_cast<unsigned>((tasks + per - 1) / per)); cfg.blockDim = dim3(kEmbThreads);
+    cudaError_t e;
+    if (a->dtype == TLI_F32) e = vec ? cudaLaunchKernelEx(&cfg, tli_embed_kernel<TLI_F32, true>, P) : cudaLaunchKernelEx(&cfg, tli_embed_kernel<TLI_F32, false>, P);
+    else e = vec ? cudaLaunchKernelEx(&cfg, tli_embed_kernel<TLI_BF16, true>, P) : cudaLaunchKernelEx(&cfg, tli_embed_kernel<TLI_BF16, false>, P);
+    if (e != cudaSuccess) return cuda_fail(e, "launch tli_embed_kernel");
+    return TLI_OK;
+}
+
+size_t tli_embed_grad_workspace_bytes(const tli_ctx *ctx, int32_t N, int32_t H) {
+    if (!ctx || ctx->n_shards != 1 || N < 0 || H < 1 || N > TLI_MAX_TOKENS || H > TLI_MAX_H) return 0;
+    return grad_layout(N, H).total;
+}
+
+int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *a, void *cuda_stream) {
+    if (!ctx || !a || ctx->n_shards != 1) return TLI_ERR_ARG;
+    if (a->N < 0 || a->H < 1) return TLI_ERR_ARG;
+    if (a->N > TLI_MAX_TOKENS || a->H > TLI_MAX_H) return TLI_ERR_UNSUPPORTED;
+    if ((a->grad_dtype != TLI_F32 && a->grad_dtype != TLI_BF16) || (a->out_dtype != TLI_F32 && a->out_dtype != TLI_BF16)) return TLI_ERR_ARG;
+    GradParams P;
+    memset(&P, 0, sizeof P);
+    const int rc = embed_side(ctx, a->ids_side, a->table_side, P.n_ids, P.V, P.map);
+    if (rc != TLI_OK) return rc;
+    if (!a->out || (a->N > 0 && (!a->ids || !a->grad))) return TLI_ERR_ARG;
+    const size_t ge = a->grad_dtype == TLI_F32 ? 4 : 2, oe = a->out_dtype == TLI_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(a->grad) % ge || reinterpret_cast<uintptr_t>(a->out) % oe) return TLI_ERR_ARG;
+    if (a->grad_stride < 0 || (P.V > 1 && a->out_stride < a->H)) return TLI_ERR_ARG;
+    const GradLayout L = grad_layout(a->N, a->H);
+    if (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 256 || a->workspace_bytes < L.total) return TLI_ERR_WORKSPACE;
+    P.N = a->N; P.H = a->H; P.groups = L.groups; P.tile = L.tile; P.window = L.window; P.nwin = L.nwin;
+    P.ids = a->ids;
+    P.g = a->grad; P.gs = a->grad_stride;
+    P.out = a->out; P.os = a->out_stride;
+    P.scale = a->scale;
+    char *ws = reinterpret_cast<char *>(a->workspace);
+    P.key[0] = reinterpret_cast<int *>(ws + L.key0); P.pos[0] = reinterpret_cast<int *>(ws + L.pos0);
+    P.key[1] = reinterpret_cast<int *>(ws + L.key1); P.pos[1] = reinterpret_cast<int *>(ws + L.pos1);
+    P.n_valid = reinterpret_cast<int *>(ws + L.n_valid);
+    P.count = reinterpret_cast<int *>(ws + L.count);
+    P.piece = reinterpret_cast<float *>(ws + L.piece);
+    cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
+    return a->out_dtype == TLI_F32 ? launch_grad<TLI_F32>(P, a->grad_dtype, ctx->num_sms, stream)
+                                   : launch_grad<TLI_BF16>(P, a->grad_dtype, ctx->num_sms, stream);
+}
+
+}  // extern "C"

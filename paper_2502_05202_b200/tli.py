@@ -32,15 +32,22 @@ TLI_ROW_NONFINITE = 4
 TLI_ROW_FALLBACK = 8
 TLI_ROW_TIMEOUT = 16
 TLI_ROW_BAD_TEMPERATURE = 32
+TLI_ROW_BAD_FILTER = 64
+TLI_SIDE_TARGET = 0
+TLI_SIDE_DRAFTER = 1
 TLI_MAX_B = 65535
 TLI_MAX_K = 64
 TLI_MAX_V = 1048576
 TLI_MAX_SHARDS = 64
+TLI_MAX_TOKENS = 4194304
+TLI_MAX_H = 65536
 TLI_STATIC_SCRATCH_BYTES = 4194304
 
 EXPORTS = ("tli_create", "tli_destroy", "tli_workspace_bytes", "tli_verify", "tli_verify_static", "tli_verify_profile", "tli_set_tiled", "tli_set_max_cluster", "tli_reset", "tli_selftest_bounded_wait",
            "tli_draft_workspace_bytes", "tli_draft_sample", "tli_slem_workspace_bytes", "tli_slem_verify",
            "tli_verify_host_buffer_bytes", "tli_verify_host", "tli_rates_workspace_bytes", "tli_acceptance_rates",
+           "tli_sample_workspace_bytes", "tli_sample", "tli_filter_workspace_bytes", "tli_filter",
+           "tli_embed", "tli_embed_grad_workspace_bytes", "tli_embed_grad",
            "tli_ctx_info",
            "tli_shard_create", "tli_shard_info", "tli_shard_workspace_bytes", "tli_shard_record_bytes", "tli_shard_rows_bytes",
            "tli_shard_stats", "tli_shard_decide", "tli_shard_weights", "tli_shard_select",
@@ -105,6 +112,50 @@ class tli_slem_args(ctypes.Structure):
     ]
 
 
+class tli_sample_args(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("R", ctypes.c_int32), ("dtype", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_r", ctypes.c_int64),
+        ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+        ("min_p", ctypes.c_void_p), ("uniforms", ctypes.c_void_p),
+        ("tokens", ctypes.c_void_p), ("prob", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class tli_filter_args(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("R", ctypes.c_int32), ("dtype", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_r", ctypes.c_int64),
+        ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+        ("min_p", ctypes.c_void_p),
+        ("out", ctypes.c_void_p), ("out_stride_b", ctypes.c_int64), ("out_stride_r", ctypes.c_int64),
+        ("status", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class tli_embed_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("table_side", ctypes.c_int32),
+        ("ids", ctypes.c_void_p), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64), ("table_ids", ctypes.c_void_p),
+    ]
+
+
+class tli_embed_grad_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("table_side", ctypes.c_int32),
+        ("ids", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("grad_stride", ctypes.c_int64),
+        ("scale", ctypes.c_float),
+        ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 class TLIError(RuntimeError):
     def __init__(self, code: int, where: str):
         lib = load()
@@ -154,6 +205,15 @@ def load() -> ctypes.CDLL:
         lib.tli_rates_workspace_bytes.restype = ctypes.c_size_t
         lib.tli_acceptance_rates.argtypes = [ctypes.c_void_p, ctypes.POINTER(tli_rates_args), ctypes.c_void_p]
         lib.tli_acceptance_rates.restype = ctypes.c_int
+        for name, args in (("tli_sample", tli_sample_args), ("tli_filter", tli_filter_args), ("tli_embed", tli_embed_args),
+                           ("tli_embed_grad", tli_embed_grad_args)):
+            getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.POINTER(args), ctypes.c_void_p]
+            getattr(lib, name).restype = ctypes.c_int
+        for name in ("tli_sample_workspace_bytes", "tli_filter_workspace_bytes"):
+            getattr(lib, name).argtypes = [ctypes.c_void_p] + [ctypes.c_int32] * 4
+            getattr(lib, name).restype = ctypes.c_size_t
+        lib.tli_embed_grad_workspace_bytes.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32]
+        lib.tli_embed_grad_workspace_bytes.restype = ctypes.c_size_t
         lib.tli_shard_create.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_int, ctypes.c_int32, ctypes.c_int32,
                                          ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32]
         lib.tli_shard_create.restype = ctypes.c_int
@@ -411,6 +471,151 @@ def tli_slem_verify(ctx: int, args: tli_slem_args, stream: Optional[int] = None)
         raise TLIError(rc, "tli_slem_verify")
 
 
+def tli_sample_workspace_bytes(ctx: int, B: int, R: int, dtype: int, side: int) -> int:
+    return int(load().tli_sample_workspace_bytes(ctx, B, R, dtype, side))
+
+
+def tli_filter_workspace_bytes(ctx: int, B: int, R: int, dtype: int, side: int) -> int:
+    return int(load().tli_filter_workspace_bytes(ctx, B, R, dtype, side))
+
+
+def _check_rows(ctx: int, logits: torch.Tensor, side: int, tensors) -> None:
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, R, V]")
+    if side not in (TLI_SIDE_TARGET, TLI_SIDE_DRAFTER):
+        raise ValueError("side must be TLI_SIDE_TARGET or TLI_SIDE_DRAFTER")
+    V_t, V_d = ctypes.c_int32(), ctypes.c_int32()
+    rc = load().tli_ctx_info(ctx, ctypes.byref(V_t), ctypes.byref(V_d), None)
+    if rc != TLI_OK:
+        raise TLIError(rc, "tli_ctx_info")
+    V = V_t.value if side == TLI_SIDE_TARGET else V_d.value
+    if logits.shape[2] != V:
+        raise ValueError("rows of this side have %d logits, not %d" % (V, logits.shape[2]))
+    if V > 1 and logits.stride(2) != 1:
+        raise ValueError("the vocabulary axis must be contiguous")
+    for name, t, dtype, shape in tensors:
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, shape))
+        if t is not None and t.device != logits.device:
+            raise ValueError("%s must be on %s" % (name, logits.device))
+
+
+def make_sample_args(ctx: int, logits: torch.Tensor, temperature: torch.Tensor, uniforms: torch.Tensor, tokens: torch.Tensor,
+                     workspace: torch.Tensor, side: int = TLI_SIDE_TARGET, top_k: Optional[torch.Tensor] = None,
+                     top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                     prob: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> tli_sample_args:
+    """Fill a tli_sample_args from device tensors (no copies; the tensors must outlive the call)."""
+    dt = _logit_dtype(logits)
+    B, R = logits.shape[0], logits.shape[1] if logits.dim() == 3 else 0
+    _check_rows(ctx, logits, side, (("temperature", temperature, torch.float32, (B,)), ("top_k", top_k, torch.int32, (B,)),
+                                    ("top_p", top_p, torch.float32, (B,)), ("min_p", min_p, torch.float32, (B,)),
+                                    ("uniforms", uniforms, torch.float32, (B, R)), ("tokens", tokens, torch.int32, (B, R)),
+                                    ("prob", prob, torch.float32, (B, R)), ("status", status, torch.int32, (B, R))))
+    opt = lambda t: None if t is None else t.data_ptr()
+    return tli_sample_args(B, R, dt, side, logits.data_ptr(), logits.stride(0), logits.stride(1),
+                           temperature.data_ptr(), opt(top_k), opt(top_p), opt(min_p), uniforms.data_ptr(),
+                           tokens.data_ptr(), opt(prob), opt(status),
+                           workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def tli_sample(ctx: int, args: tli_sample_args, stream: Optional[int] = None) -> None:
+    """tli_sample() on ``stream`` (a cudaStream_t as int; default: torch's current stream)."""
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    rc = load().tli_sample(ctx, ctypes.byref(args), ctypes.c_void_p(stream))
+    if rc != TLI_OK:
+        raise TLIError(rc, "tli_sample")
+
+
+def make_filter_args(ctx: int, logits: torch.Tensor, temperature: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                     side: int = TLI_SIDE_TARGET, top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                     min_p: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> tli_filter_args:
+    """Fill a tli_filter_args from device tensors (no copies; the tensors must outlive the call)."""
+    dt = _logit_dtype(logits)
+    B, R = logits.shape[0], logits.shape[1] if logits.dim() == 3 else 0
+    _check_rows(ctx, logits, side, (("temperature", temperature, torch.float32, (B,)), ("top_k", top_k, torch.int32, (B,)),
+                                    ("top_p", top_p, torch.float32, (B,)), ("min_p", min_p, torch.float32, (B,)),
+                                    ("status", status, torch.int32, (B, R))))
+    if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device or (out.shape[2] > 1 and out.stride(2) != 1):
+        raise ValueError("out must have the logits' type, shape and device, and a contiguous vocabulary axis")
+    opt = lambda t: None if t is None else t.data_ptr()
+    return tli_filter_args(B, R, dt, side, logits.data_ptr(), logits.stride(0), logits.stride(1),
+                           temperature.data_ptr(), opt(top_k), opt(top_p), opt(min_p),
+                           out.data_ptr(), out.stride(0), out.stride(1), opt(status),
+                           workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def tli_filter(ctx: int, args: tli_filter_args, stream: Optional[int] = None) -> None:
+    """tli_filter() on ``stream`` (a cudaStream_t as int; default: torch's current stream)."""
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    rc = load().tli_filter(ctx, ctypes.byref(args), ctypes.c_void_p(stream))
+    if rc != TLI_OK:
+        raise TLIError(rc, "tli_filter")
+
+
+def _matrix(name: str, t: torch.Tensor) -> int:
+    """Row stride of a [rows, H] tensor with contiguous rows."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a matrix with contiguous rows" % name)
+    return t.stride(0)
+
+
+def _check_ids(ids: torch.Tensor, N: int) -> None:
+    if ids.dtype != torch.int32 or ids.numel() != N or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous %s tensor of %d entries" % (torch.int32, N))
+
+
+def make_embed_args(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                    ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET,
+                    table_ids: Optional[torch.Tensor] = None) -> tli_embed_args:
+    """Fill a tli_embed_args from device tensors (no copies; the tensors must outlive the call)."""
+    N = ids.numel()
+    _check_ids(ids, N)
+    H = table.shape[-1]
+    if tuple(out.shape) != (N, H) or out.dtype != table.dtype:
+        raise ValueError("out must be [%d, %d] in the table's type" % (N, H))
+    if table_ids is not None:
+        _check_ids(table_ids, N)
+    return tli_embed_args(N, H, _logit_dtype(table), ids_side, table_side, ids.data_ptr(), table.data_ptr(), _matrix("table", table),
+                          float(scale), out.data_ptr(), _matrix("out", out), None if table_ids is None else table_ids.data_ptr())
+
+
+def tli_embed(ctx: int, args: tli_embed_args, stream: Optional[int] = None) -> None:
+    """tli_embed() on ``stream`` (a cudaStream_t as int; default: torch's current stream)."""
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    rc = load().tli_embed(ctx, ctypes.byref(args), ctypes.c_void_p(stream))
+    if rc != TLI_OK:
+        raise TLIError(rc, "tli_embed")
+
+
+def tli_embed_grad_workspace_bytes(ctx: int, N: int, H: int) -> int:
+    return int(load().tli_embed_grad_workspace_bytes(ctx, N, H))
+
+
+def make_embed_grad_args(ids: torch.Tensor, grad: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                         ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET) -> tli_embed_grad_args:
+    """Fill a tli_embed_grad_args from device tensors (no copies; the tensors must outlive the call)."""
+    N = ids.numel()
+    _check_ids(ids, N)
+    H = grad.shape[-1]
+    if tuple(grad.shape) != (N, H) or out.dim() != 2 or out.shape[1] != H:
+        raise ValueError("grad must be [%d, H] and out [V, H]" % N)
+    return tli_embed_grad_args(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
+                               grad.data_ptr(), _matrix("grad", grad), float(scale), out.data_ptr(), _matrix("out", out),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def tli_embed_grad(ctx: int, args: tli_embed_grad_args, stream: Optional[int] = None) -> None:
+    """tli_embed_grad() on ``stream`` (a cudaStream_t as int; default: torch's current stream)."""
+    if stream is None:
+        stream = torch.cuda.current_stream().cuda_stream
+    rc = load().tli_embed_grad(ctx, ctypes.byref(args), ctypes.c_void_p(stream))
+    if rc != TLI_OK:
+        raise TLIError(rc, "tli_embed_grad")
+
+
 def tli_verify_profile(ctx: int, args: tli_verify_args, stream: Optional[int] = None):
     """tli_verify_profile(): blocks; returns ms of (statistics kernel, decision kernel or 0, sampling kernel)."""
     if stream is None:
@@ -573,6 +778,65 @@ class Verifier:
                                out["q_draft"], out["draft_status"])
         tli_draft_sample(self.ctx, args)
         return out
+
+    def _scratch(self, need: int, where: str) -> torch.Tensor:
+        """Scratch of one call that may overlap others on this context: its own, not the shared one."""
+        if need == 0:
+            raise TLIError(TLI_ERR_UNSUPPORTED, where)
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+    def sample(self, logits, temperature, uniforms, side: int = TLI_SIDE_TARGET, top_k=None, top_p=None,
+               min_p=None) -> Dict[str, torch.Tensor]:
+        """Draw one id per row of ``logits`` [B,R,V] under temperature, top-k, top-p and min-p (per sequence,
+        ``None`` = off); on the drafter side from the ids inside the intersection.  Returns device tensors."""
+        B, R = logits.shape[0], logits.shape[1]
+        dev = self.device
+        out = {"tokens": torch.empty(B, R, dtype=torch.int32, device=dev),
+               "prob": torch.empty(B, R, dtype=torch.float32, device=dev),
+               "status": torch.empty(B, R, dtype=torch.int32, device=dev)}
+        ws = self._scratch(tli_sample_workspace_bytes(self.ctx, B, R, _logit_dtype(logits), side), "tli_sample_workspace_bytes")
+        args = make_sample_args(self.ctx, logits, temperature, uniforms, out["tokens"], ws, side, top_k, top_p, min_p,
+                                out["prob"], out["status"])
+        tli_sample(self.ctx, args, torch.cuda.current_stream(dev).cuda_stream)
+        return out
+
+    def filter(self, logits, temperature, side: int = TLI_SIDE_TARGET, top_k=None, top_p=None, min_p=None,
+               out=None) -> Dict[str, torch.Tensor]:
+        """The rows of ``logits`` [B,R,V] with -inf outside the kept set (``out=logits``: in place)."""
+        B, R = logits.shape[0], logits.shape[1]
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
+        status = torch.empty(B, R, dtype=torch.int32, device=self.device)
+        ws = self._scratch(tli_filter_workspace_bytes(self.ctx, B, R, _logit_dtype(logits), side), "tli_filter_workspace_bytes")
+        args = make_filter_args(self.ctx, logits, temperature, out, ws, side, top_k, top_p, min_p, status)
+        tli_filter(self.ctx, args, torch.cuda.current_stream(self.device).cuda_stream)
+        return {"logits": out, "status": status}
+
+    def embed(self, ids, table, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET,
+              table_side: int = TLI_SIDE_TARGET) -> Dict[str, torch.Tensor]:
+        """Rows of ``table`` [V,H] for ``ids`` (any shape) of either vocabulary, times ``scale``, and the ids in
+        the table's vocabulary (-1, with a zero row, where there is none)."""
+        V = self.V_t if table_side == TLI_SIDE_TARGET else self.V_d
+        if table.dim() != 2 or table.shape[0] != V:
+            raise ValueError("table must be [%d, H]" % V)
+        rows = torch.empty(*ids.shape, table.shape[1], dtype=table.dtype, device=self.device)
+        table_ids = torch.empty(ids.shape, dtype=torch.int32, device=self.device)
+        args = make_embed_args(ids, table, rows.view(ids.numel(), table.shape[1]), scale, ids_side, table_side, table_ids)
+        tli_embed(self.ctx, args, torch.cuda.current_stream(self.device).cuda_stream)
+        return {"rows": rows, "table_ids": table_ids}
+
+    def embed_grad(self, ids, grad, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET,
+                   dtype: Optional[torch.dtype] = None) -> Dict[str, torch.Tensor]:
+        """Gradient of :meth:`embed` with respect to the table, [V,H] in ``dtype`` (default: the type of ``grad``)."""
+        N, H, dev = ids.numel(), grad.shape[-1], self.device
+        if tuple(grad.shape) != tuple(ids.shape) + (H,):
+            raise ValueError("grad must have the shape of ids, and H")
+        V = self.V_t if table_side == TLI_SIDE_TARGET else self.V_d
+        out = torch.empty(V, H, dtype=dtype or grad.dtype, device=dev)
+        ws = self._scratch(tli_embed_grad_workspace_bytes(self.ctx, N, H), "tli_embed_grad_workspace_bytes")
+        args = make_embed_grad_args(ids, grad if grad.dim() == 2 else grad.reshape(N, H), out, ws, scale, ids_side, table_side)
+        tli_embed_grad(self.ctx, args, torch.cuda.current_stream(dev).cuda_stream)
+        return {"grad": out}
 
     def rates(self, target_logits, drafter_logits, temperature) -> Dict[str, torch.Tensor]:
         """Expected acceptance rates per draft position (mass, alpha_union, alpha_tli); device tensors."""
