@@ -462,13 +462,14 @@ template <int GT, int OT, bool VEC> int launch_grad_sums(const GradParams &P, cu
     return TLI_OK;
 }
 
-template <int OT> int launch_grad(GradParams &P, int gdtype, int num_sms, cudaStream_t stream) {
+template <int OT> int launch_grad(GradParams &P, int gdtype, int device, int num_sms, cudaStream_t stream) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     pdl_config(cfg, attr, stream);
     const size_t smem = sizeof(int) * kSortWarps * kDigits;
-    cudaError_t e = cudaFuncSetAttribute(tli_grad_sort_kernel<OT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(tli_grad_scatter_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    static SmemAllowed allowed_sort, allowed_scatter;
+    cudaError_t e = allowed_sort.set(reinterpret_cast<const void *>(tli_grad_sort_kernel<OT>), smem, device);
+    if (e == cudaSuccess) e = allowed_scatter.set(reinterpret_cast<const void *>(tli_grad_scatter_kernel), smem, device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
     cfg.blockDim = dim3(kSortThreads);
     cfg.gridDim = dim3(num_sms); cfg.dynamicSmemBytes = smem;
@@ -564,8 +565,8 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *a, void *cuda_stream
     P.count = reinterpret_cast<int *>(ws + L.count);
     P.piece = reinterpret_cast<float *>(ws + L.piece);
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-    return a->out_dtype == TLI_F32 ? launch_grad<TLI_F32>(P, a->grad_dtype, ctx->num_sms, stream)
-                                   : launch_grad<TLI_BF16>(P, a->grad_dtype, ctx->num_sms, stream);
+    return a->out_dtype == TLI_F32 ? launch_grad<TLI_F32>(P, a->grad_dtype, ctx->device, ctx->num_sms, stream)
+                                   : launch_grad<TLI_BF16>(P, a->grad_dtype, ctx->device, ctx->num_sms, stream);
 }
 
 }  // extern "C"

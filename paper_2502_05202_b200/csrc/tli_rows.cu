@@ -24,22 +24,30 @@
 // rounding.  An fp64 weight costs 13 fp64 operations; one pass over a row is then bound by the fp64 pipe only
 // for 16-bit rows that need the whole mass.
 
+#include <cuda_bf16.h>
+#include <algorithm>
+#include <atomic>
+
 namespace {
 
 constexpr int kRowThreads = 256;                     // scan and mask kernels
 constexpr int kRowWarps = kRowThreads / 32;
-constexpr int kPickThreads = 512;
+constexpr int kPickThreads = 256;                    // pick and spread kernels
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMaxGroups = 8192;                     // group maxima a pick CTA holds (coarser groups beyond)
-constexpr int kListCap = 2048;                       // elements the sort takes
+constexpr int kListCap = 4096;                       // elements a block searches in shared memory
+constexpr int kSample = 16384;                       // elements of a row that stand for it where the border is guessed
 constexpr int kBins = 1024;
 
 struct __align__(16) StripSum { double S; float m; int pad; };       // sum of 2^((z - m) s) over a strip, m its largest
 struct __align__(16) RowBorder { float z; int id; int mode; int pad; };
 enum : int { BORDER_APPLY = 0, BORDER_COPY = 1 };
+// What the pick kernel leaves to the spread and settle kernels: ids above (zhi, bid) are kept, below zlo none is.
+struct __align__(16) RowPlan { double Z; float zlo, zhi; int bid, kind; float m, zmin; int listed, pad; };
+enum : int { PLAN_BRACKET = 0, PLAN_DRAW = 1 };                      // the border is in between; it is (zhi, bid)
 
 struct RowsParams {
-    int B, R, V, nstrip, coarse, sample;
+    int B, R, V, nstrip, ulog, coarse, sample;
     const void *z; long long sb, sr;
     const uint32_t *mask;                  // ids that can be kept; NULL: every id of the row
     const float *tau; const int *top_k; const float *top_p; const float *min_p; const float *u;
@@ -47,6 +55,9 @@ struct RowsParams {
     void *gmax;                            // [rows][nstrip * 32] in the rows' type
     StripSum *ssum;                        // [rows][nstrip]
     RowBorder *border;                     // [rows]
+    RowPlan *plan;                         // [rows]
+    int *todo;                             // [1 + rows]: how many rows the spread and settle kernels have, and which
+    unsigned long long *lists; int listcap;    // [rows][listcap]
     void *out; long long osb, osr;
 };
 
@@ -70,9 +81,12 @@ __device__ __forceinline__ double exp2_neg(double x, const double *tab) {
     q *= tab[n & 15];
     return __hiloint2double(__double2hiint(q) + ((n >> 4) << 20), __double2loint(q));
 }
+__device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }     // of a normal number
+__device__ __forceinline__ double two_to(int n) { return __hiloint2double((n + 1023) << 20, 0); }
 // w(z) = exp((z - m)/tau), s = log2(e)/tau; 0 below cut (2^-1020 of the largest; -inf among them)
 struct Weights {
     double m, s; float cut; const double *tab;
+    Weights() = default;
     __device__ __forceinline__ Weights(float m_, float tau, const double *tab_) {
         m = m_; s = 1.4426950408889634074 / tau; tab = tab_;
         cut = fmaxf(__double2float_ru(m - 1020.0 / s), -FLT_MAX);        // rounded up: z >= cut stays in exp2_neg's range
@@ -96,13 +110,31 @@ template <int DT> __device__ __forceinline__ uint4 mask_vector(uint4 raw, const 
     }
     return raw;
 }
+// A vector at an end of a row: what lies outside the row reads as -inf.  Out of line: two vectors of a row come here.
+template <int DT> __device__ __noinline__ uint4 ragged_vector(const void *row, int e0, int V) {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (DT == TLI_F32) {
+            const int e = e0 + k;
+            w[k] = e >= 0 && e < V ? __ldcg(reinterpret_cast<const unsigned *>(row) + e) : 0xff800000u;
+        } else {
+            const int e = e0 + 2 * k;
+            const unsigned short *h = reinterpret_cast<const unsigned short *>(row);
+            const uint32_t lo = e >= 0 && e < V ? __ldcg(h + e) : 0xff80u, hi = e + 1 >= 0 && e + 1 < V ? __ldcg(h + e + 1) : 0xff80u;
+            w[k] = lo | hi << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // Vector v of a row; ids outside the row or outside the mask read as -inf.
 template <int DT>
 __device__ __forceinline__ uint4 row_vector(const RowView<DT> &rv, const uint32_t *mask, int v, int nvec) {
     constexpr uint32_t NI = Elt<DT>::kNegInfWord;
     if (v >= nvec) return make_uint4(NI, NI, NI, NI);
-    const uint4 raw = rv.load(v);
-    return mask ? mask_vector<DT>(raw, mask, rv.first_elem(v)) : raw;
+    const int e0 = rv.first_elem(v);
+    const uint4 raw = e0 >= 0 && e0 + Elt<DT>::kPerVec <= rv.V ? __ldg(rv.vec0 + v) : ragged_vector<DT>(rv.row, e0, rv.V);
+    return mask ? mask_vector<DT>(raw, mask, e0) : raw;
 }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
@@ -157,6 +189,12 @@ struct RowAsk {
         p_on = p < 1.f;
         min_on = least > 0.f;
     }
+    // min-p as a logit: z >= m + tau ln(min_p), in fp64, to the next value of the row's type above
+    template <int DT> __device__ __forceinline__ float zmin(float m) const {
+        if (!min_on) return -FLT_MAX;
+        const float f = __double2float_ru(static_cast<double>(m) + static_cast<double>(tau) * log(static_cast<double>(least)));
+        return DT == TLI_BF16 ? __bfloat162float(__float2bfloat16_ru(f)) : f;
+    }
     __device__ __forceinline__ bool plain() const { return !k_on && !p_on && !min_on; }
     // the mass of the whole row is asked for
     __device__ __forceinline__ bool whole_mass(int sample) const {
@@ -165,12 +203,14 @@ struct RowAsk {
 };
 
 template <int DT, int U>
-__global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const RowsParams P) {
+__global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const __grid_constant__ RowsParams P) {
     __shared__ double tab[16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int row = blockIdx.y, b = row / P.R;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int strip = blockIdx.x * kRowWarps + warp;
+    if (blockIdx.x == 0 && row == 0 && threadIdx.x == 0) *P.todo = 0;
     const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
     const int nvec = rv.nvec(), v0 = strip * (32 * U) + lane;
     uint4 raw[U];
@@ -193,10 +233,14 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const RowsPa
     double acc = 0.0;
     if (ms > -INFINITY && ms < INFINITY) {                         // NaN: not compared, the row is flagged later
         const Weights w(ms, ask.tau, tab);
-#pragma unroll
+        // (unrolled the code would not fit the instruction cache)
+#pragma unroll 1
         for (int q = 0; q < U; ++q) {
+            uint4 r = raw[0];
+#pragma unroll
+            for (int k = 1; k < U; ++k) if (k == q) r = raw[k];
             float z[Elt<DT>::kPerVec];
-            unpack<DT>(raw[q], z);
+            unpack<DT>(r, z);
 #pragma unroll
             for (int i = 0; i < Elt<DT>::kPerVec; ++i) acc += w(z[i]);
         }
@@ -208,624 +252,1141 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const RowsPa
     }
 }
 
-// ---- block-wide steps of the pick kernel (all threads call them; each begins and ends with a barrier) ----
+// ---- logits as integers ----
 
-struct PickShared {
-    double tab[16];
-    double wsum[kPickWarps];
-    unsigned long long wsum_u[kPickWarps];
-    int wsum_i[kPickWarps];
-    double bd[2];
-    unsigned long long bu[2];
-    int bi[4];
-};
-
-// inclusive prefix over the block's threads; total in `total`
-template <typename T> __device__ __forceinline__ T block_scan(T x, T *slots, T &total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const T y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();
-    if (lane == 31) slots[warp] = x;
-    __syncthreads();
-    T before = 0, all = 0;
-#pragma unroll
-    for (int i = 0; i < kPickWarps; ++i) {
-        const T t = slots[i];
-        if (i < warp) before += t;
-        all += t;
-    }
-    total = all;
-    __syncthreads();
-    return x + before;
+// monotone; -0 and +0 alike; 16 bits for bf16
+template <int DT> __device__ __forceinline__ uint32_t logit_key(float z) {
+    const uint32_t u = __float_as_uint(z + 0.f);
+    const uint32_t k = u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+    return DT == TLI_BF16 ? k >> 16 : k;
 }
-__device__ __forceinline__ int block_max_int(int x, int *slots) {
+template <int DT> __device__ __forceinline__ float key_logit(uint32_t k) {
+    if (DT == TLI_BF16) return __uint_as_float(((k & 0x8000u) ? k ^ 0x8000u : ~k & 0xffffu) << 16);
+    return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
+}
+// an element as one integer that falls along the order (logit descending, id ascending); never 0
+using u64 = unsigned long long;
+constexpr uint32_t kIdMask = (1u << 20) - 1u;
+static_assert(TLI_MAX_V <= (1 << 20), "an id has 20 bits in a list element");
+template <int DT> __device__ __forceinline__ u64 element_of(float z, int id) {
+    return (static_cast<u64>(logit_key<DT>(z)) << 20) | (kIdMask - static_cast<uint32_t>(id));
+}
+template <int DT> __device__ __forceinline__ float element_logit(u64 e) { return key_logit<DT>(static_cast<uint32_t>(e >> 20)); }
+__device__ __forceinline__ int element_id(u64 e) { return static_cast<int>(kIdMask - (static_cast<uint32_t>(e) & kIdMask)); }
+
+// ---- the state of a pick or settle block ----
+//
+// These two kernels run each of their steps once or a few times per row, so what they cost is the fetching of their code:
+// with every step inlined and unrolled they were 300 to 540 KB and took two to ten times as long.  The steps are
+// functions that are called, their loops are not unrolled, and the block's state is in shared memory instead of registers.
+
+struct PickState {
+    double tab[16];
+    u64 slot[kPickWarps];
+    u64 found, before;
+    int bin, listed;
+    // the row
+    Weights w;
+    const uint4 *vec0; const void *row; const uint32_t *mask;
+    int head, V, nvec, nstrip, ulog, coarse, ngroups, ng;
+    float m;
+};
+__shared__ PickState S;
+// Dynamic shared memory: the elements that may lie at the border and their weights (or a sample of the row), three words per
+// bin of a histogram (zero between uses), the strip sums, the row's group maxima, the numbers of the groups to read again.
+extern __shared__ __align__(16) unsigned char pick_smem[];
+constexpr size_t pick_smem_bytes(int nstrip, int ngroups) {
+    return kListCap * 16 + kBins * 12 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6;
+}
+constexpr size_t kPickSmemMax = pick_smem_bytes((TLI_MAX_V + 6) / (4 * 32 * 8) + 1, kMaxGroups);
+static_assert(kSample * 4 <= kListCap * 16, "the sample takes the place of the list");
+__device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem); }
+__device__ __forceinline__ u64 *masses() { return list() + kListCap; }
+__device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem); }
+__device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem + kListCap * 16); }
+__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kListCap * 16 + kBins * 12); }
+__device__ __forceinline__ float *group_max() { return reinterpret_cast<float *>(strips() + S.nstrip); }
+__device__ __forceinline__ unsigned short *group_list() { return reinterpret_cast<unsigned short *>(group_max() + S.ngroups); }
+
+template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b) {      // (visible after the next barrier)
+    for (int i = threadIdx.x; i < 3 * kBins / 4; i += kPickThreads) reinterpret_cast<uint4 *>(bins())[i] = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) {
+        const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
+        S.vec0 = rv.vec0; S.row = rv.row; S.head = rv.head; S.V = P.V; S.nvec = rv.nvec(); S.mask = P.mask;
+        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse;
+        S.ngroups = (P.nstrip + P.coarse - 1) / P.coarse * 32;
+    }
+}
+template <int DT> __device__ __forceinline__ uint4 state_vector(int v) {      // vector v of the block's row
+    constexpr uint32_t NI = Elt<DT>::kNegInfWord;
+    if (v >= S.nvec) return make_uint4(NI, NI, NI, NI);
+    const int e0 = v * Elt<DT>::kPerVec - S.head;
+    const uint4 raw = e0 >= 0 && e0 + Elt<DT>::kPerVec <= S.V ? __ldg(S.vec0 + v) : ragged_vector<DT>(S.row, e0, S.V);
+    return S.mask ? mask_vector<DT>(raw, S.mask, e0) : raw;
+}
+template <int DT> __device__ __forceinline__ float vector_element(const uint4 &r, int i) {               // i not known in advance
+    if (DT == TLI_F32) return __uint_as_float(i < 2 ? (i == 0 ? r.x : r.y) : (i == 2 ? r.z : r.w));
+    const uint32_t x = i < 4 ? (i < 2 ? r.x : r.y) : (i < 6 ? r.z : r.w);
+    return i & 1 ? bf16_hi(x) : bf16_lo(x);
+}
+
+// ---- block-wide steps (every thread of the block calls them) ----
+
+__device__ __noinline__ int block_max(int x) {
     x = __reduce_max_sync(0xffffffffu, x);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) slots[threadIdx.x >> 5] = x;
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<int *>(S.slot)[threadIdx.x >> 5] = x;
     __syncthreads();
-    int r = slots[0];
+    const int4 a = reinterpret_cast<const int4 *>(S.slot)[0], b = reinterpret_cast<const int4 *>(S.slot)[1];
+    return max(max(max(a.x, a.y), max(a.z, a.w)), max(max(b.x, b.y), max(b.z, b.w)));
+}
+__device__ __forceinline__ int block_min(int x) { return ~block_max(~x); }
+__device__ __noinline__ int block_sum(int x) {
+    x = __reduce_add_sync(0xffffffffu, x);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) reinterpret_cast<int *>(S.slot)[threadIdx.x >> 5] = x;
+    __syncthreads();
+    const int4 a = reinterpret_cast<const int4 *>(S.slot)[0], b = reinterpret_cast<const int4 *>(S.slot)[1];
+    return a.x + a.y + a.z + a.w + b.x + b.y + b.z + b.w;
+}
+template <typename T> struct Prefix { T before, total; };
+template <typename T> __device__ __noinline__ Prefix<T> block_prefix(T x) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    T incl = x;
 #pragma unroll
-    for (int i = 1; i < kPickWarps; ++i) r = max(r, slots[i]);
+    for (int o = 1; o < 32; o <<= 1) {
+        const T y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    T *slot = reinterpret_cast<T *>(S.slot);
+    __syncthreads();
+    if (lane == 31) slot[warp] = incl;
+    __syncthreads();
+    Prefix<T> p;
+    p.before = 0; p.total = 0;
+#pragma unroll
+    for (int i = 0; i < kPickWarps; ++i) {
+        const T t = slot[i];
+        if (i < warp) p.before += t;
+        p.total += t;
+    }
+    p.before += incl - x;
+    return p;
+}
+
+// First bin at which the running measure, from `before`, reaches `want` (-1 if none does), the measure in front of it (or of everything)
+// and its own.
+// A bin's measure is w0 + (w1 << shift) + (w2 << 40).  The bins come back zero unless they are to be kept.
+struct BinAt { int bin; u64 before, measure; };
+static_assert(kBins == 4 * kPickThreads, "four bins per thread");
+__device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool keep) {
+    __syncthreads();
+    uint4 *w = reinterpret_cast<uint4 *>(bins()) + threadIdx.x;
+    const uint4 a = w[0], b = w[kBins / 4], c = w[kBins / 2];
+    if (!keep) { w[0] = make_uint4(0, 0, 0, 0); w[kBins / 4] = w[0]; w[kBins / 2] = w[0]; }
+    auto value = [shift](unsigned lo, unsigned mid, unsigned hi) { return lo + (static_cast<u64>(mid) << shift) + (static_cast<u64>(hi) << 40); };
+    const u64 x0 = value(a.x, b.x, c.x), x1 = value(a.y, b.y, c.y), x2 = value(a.z, b.z, c.z), x3 = value(a.w, b.w, c.w);
+    const u64 mine = x0 + x1 + x2 + x3;
+    const Prefix<u64> p = block_prefix(mine);
+    u64 run = before + p.before;
+    if (run < want && run + mine >= want) {                        // at most one thread
+        int k = 0;
+        u64 x = x0;
+        if (run + x < want) { run += x; x = x1; k = 1; if (run + x < want) { run += x; x = x2; k = 2; if (run + x < want) { run += x; x = x3; k = 3; } } }
+        S.bin = threadIdx.x * 4 + k;
+        S.before = run;
+        S.found = x;
+    }
+    __syncthreads();
+    BinAt r;
+    const bool any = before < want && before + p.total >= want;
+    r.bin = any ? S.bin : -1;
+    r.before = any ? S.before : before + p.total;
+    r.measure = any ? S.found : 0;
     __syncthreads();
     return r;
 }
-__device__ __forceinline__ int block_min_int(int x, int *slots) { return -block_max_int(-x, slots); }
+__device__ __forceinline__ int bin_shift(u64 range) { return range < kBins ? 0 : 54 - __clzll(range); }      // (range >> shift) < 1024
+__device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^60, in three words of 20 bits: 4096 cannot overflow 32
+    unsigned *w = bins() + k;
+    atomicAdd(w, static_cast<uint32_t>(f) & 0xfffffu);
+    atomicAdd(w + kBins, static_cast<uint32_t>(f >> 20) & 0xfffffu);
+    const uint32_t c = static_cast<uint32_t>(f >> 40);
+    if (c) atomicAdd(w + 2 * kBins, c);
+}
 
-// bitonic sort of a[0 .. n), n a power of two, descending.  Pairs at most 32 apart stay inside one warp's 64
-// elements, so only the wider steps need a block barrier.
-__device__ __forceinline__ void sort_descending(unsigned long long *a, int n) {
-    __syncthreads();
-    for (int size = 2; size <= n; size <<= 1) {
-        for (int stride = size >> 1; stride > 0; stride >>= 1) {
-            if (stride > 32) __syncthreads(); else __syncwarp();
-            for (int i = threadIdx.x; i < (n >> 1); i += kPickThreads) {
-                const int x = 2 * i - (i & (stride - 1)), y = x + stride;
-                const unsigned long long ax = a[x], ay = a[y];
-                const bool down = (x & size) == 0;
-                if ((ax < ay) == down) { a[x] = ay; a[y] = ax; }
+// Among the n listed elements that are >= edge, in their order (BY_ID: in increasing id): the one at which the running
+// measure (their number; BY_MASS: their fixed-point mass) reaches `want`, coming from `before`; 0 if none does.  A histogram
+// of 1024 bins over the interval that is left, from the element `first` on, until it holds one.
+enum : int { BY_MASS = 1, BY_ID = 2 };
+__device__ __noinline__ u64 find_element(int n, u64 edge, u64 want, u64 before, u64 first, u64 range, int how) {
+    u64 low = 0;
+    auto pos = [&](u64 e) { return (how & BY_ID) ? static_cast<u64>(element_id(e)) : first - e; };
+    for (;;) {
+        const int shift = bin_shift(range);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kPickThreads) {
+            const u64 e = list()[i], p = pos(e) - low;
+            if (e >= edge && p <= range) {
+                if (how & BY_MASS) add_mass(static_cast<int>(p >> shift), masses()[i]);
+                else atomicAdd(bins() + static_cast<int>(p >> shift), 1u);
             }
-            if (stride > 32) __syncthreads();
+        }
+        const BinAt at = find_bin(want, before, 20, false);
+        if (at.bin < 0) return 0;
+        before = at.before;
+        low += static_cast<u64>(at.bin) << shift;
+        range = min(range - (static_cast<u64>(at.bin) << shift), (1ull << shift) - 1);
+        int inside = 0;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kPickThreads) {
+            const u64 e = list()[i];
+            if (e >= edge && pos(e) - low <= range) { ++inside; S.found = e; }       // (used if it is the only one)
+        }
+        if (block_sum(inside) == 1) {
+            const u64 e = S.found;
+            __syncthreads();
+            return e;
         }
     }
-    __syncthreads();
 }
 
-__device__ __forceinline__ uint32_t logit_key(float z) {           // monotone; -0 and +0 alike
-    const uint32_t u = __float_as_uint(z + 0.f);
-    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ float key_logit(uint32_t k) {
-    return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
-}
-// bin of a logit by its distance below the largest: 32 bins per factor of two, 2^-16 .. 2^16
-__device__ __forceinline__ int distance_bin(float m, float z) {
-    const int e = static_cast<int>(__float_as_uint(m - z) >> 18) - ((127 - 16) << 5);
-    return min(max(e, 0), kBins - 1);
-}
+// ---- steps of the pick kernel ----
 
-// The pick kernel's shared memory: the elements to sort (or the strip sums), histograms (count, two words of mass),
-// the row's group maxima and the numbers of the groups to read again.
-size_t pick_smem_bytes(int ngroups) { return kListCap * 8 + kBins * 12 + static_cast<size_t>(ngroups) * 6; }
-constexpr size_t kPickSmemMax = kListCap * 8 + kBins * 12 + kMaxGroups * 6;
-
-template <int DT, int U> struct Pick {
-    const RowsParams &P;
-    PickShared &sh;
-    float *sg;                           // [ngroups]
-    unsigned short *glist;               // [ng]
-    unsigned *cnt, *mlo, *mhi;           // [kBins]
-    unsigned long long *list;            // [kListCap]
-    double *strips;                      // the same memory
-    const RowView<DT> rv;
-    const int row, nvec, ngroups;
-    int ng;
-    float m;
-
-    __device__ __forceinline__ Pick(const RowsParams &P_, PickShared &sh_, unsigned char *smem, int row_, int b)
-        : P(P_), sh(sh_), rv(P_.z, b * P_.sb + (row_ - b * P_.R) * P_.sr, P_.V), row(row_), nvec(rv.nvec()),
-          ngroups((P_.nstrip + P_.coarse - 1) / P_.coarse * 32), ng(0) {
-        list = reinterpret_cast<unsigned long long *>(smem);
-        strips = reinterpret_cast<double *>(list);
-        cnt = reinterpret_cast<unsigned *>(list + kListCap);
-        mlo = cnt + kBins; mhi = mlo + kBins;
-        sg = reinterpret_cast<float *>(mhi + kBins);
-        glist = reinterpret_cast<unsigned short *>(sg + ngroups);
-        m = 0.f;
-    }
-
-    // group maxima into shared memory, their maximum into m; false if a NaN or +inf is among them
-    __device__ __forceinline__ bool load_groups() {
-        const size_t base = static_cast<size_t>(row) * P.nstrip * 32;
-        int best = INT_MIN;
-        bool bad = false;
-        for (int g = threadIdx.x; g < ngroups; g += kPickThreads) {
-            float x;
-            if (P.coarse == 1) {
-                x = load_group<DT>(P.gmax, base + g);
-            } else {
-                x = -INFINITY;
-                const int s0 = (g >> 5) * P.coarse;
-                for (int c = 0; c < P.coarse && s0 + c < P.nstrip; ++c)
-                    x = max_nan(x, load_group<DT>(P.gmax, base + static_cast<size_t>(s0 + c) * 32 + (g & 31)));
+// group maxima into shared memory; this thread's largest comes back (NaN if a NaN is among them)
+template <int DT> __device__ __noinline__ float load_groups(const void *gmax, size_t base) {
+    float best = -INFINITY;
+    const int ngroups = S.ngroups, coarse = S.coarse;
+    float *sg = group_max();
+    if (coarse == 1) {
+#pragma unroll 1
+        for (int g0 = threadIdx.x; g0 < ngroups; g0 += 8 * kPickThreads) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = g0 + i * kPickThreads < ngroups ? load_group<DT>(gmax, base + g0 + i * kPickThreads) : -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (g0 + i * kPickThreads < ngroups) sg[g0 + i * kPickThreads] = x[i];
+                best = max_nan(best, x[i]);
             }
+        }
+    } else {
+#pragma unroll 1
+        for (int g = threadIdx.x; g < ngroups; g += kPickThreads) {
+            float x = -INFINITY;
+            const int s0 = (g >> 5) * coarse;
+#pragma unroll 1
+            for (int c = 0; c < coarse && s0 + c < S.nstrip; ++c) x = max_nan(x, load_group<DT>(gmax, base + static_cast<size_t>(s0 + c) * 32 + (g & 31)));
             sg[g] = x;
-            bad |= !(x < INFINITY);
-            best = max(best, float_order(x));
+            best = max_nan(best, x);
         }
-        if (__syncthreads_or(bad)) return false;
-        m = order_float(block_max_int(best, sh.wsum_i));
-        return true;
     }
+    return best;
+}
 
-    // numbers of the groups whose maximum is at least `floor`, in an order that depends on the row only
-    __device__ __forceinline__ void list_groups(float floor) {
-        int mine = 0, total;
-        for (int g = threadIdx.x; g < ngroups; g += kPickThreads) mine += sg[g] >= floor;
-        int at = block_scan(mine, sh.wsum_i, total) - mine;
-        for (int g = threadIdx.x; g < ngroups; g += kPickThreads)
-            if (sg[g] >= floor) glist[at++] = static_cast<unsigned short>(g);
-        ng = total;
-        __syncthreads();
+// numbers of the groups whose maximum is at least `floor`, in any order; tmax: the largest of this thread's
+__device__ __noinline__ void list_groups(float floor, float tmax) {
+    const float *sg = group_max();
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) S.ng = 0;
+    __syncthreads();
+    int mine = 0;
+    if (tmax >= floor) {
+#pragma unroll 4
+        for (int g = threadIdx.x; g < S.ngroups; g += kPickThreads) mine += sg[g] >= floor;
     }
+    if (__any_sync(0xffffffffu, mine != 0)) {
+        int at = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += y;
+        }
+        int base = 0;
+        if (lane == 31) base = atomicAdd(&S.ng, at);
+        at += __shfl_sync(0xffffffffu, base, 31) - mine;
+        if (mine) {
+            unsigned short *out = group_list();
+#pragma unroll 1
+            for (int g = threadIdx.x; g < S.ngroups; g += kPickThreads)
+                if (sg[g] >= floor) out[at++] = static_cast<unsigned short>(g);
+        }
+    }
+    __syncthreads();
+}
+// the t-th vector of the listed groups (S.coarse << S.ulog of them each)
+__device__ __forceinline__ int listed_vector(int t) {
+    const int per = S.coarse << S.ulog;
+    const int k = S.coarse == 1 ? t >> S.ulog : t / per, j = t - k * per, g = group_list()[k];
+    return ((((g >> 5) * S.coarse + (j >> S.ulog)) << S.ulog) + (j & ((1 << S.ulog) - 1))) * 32 + (g & 31);
+}
 
-    // f(z, id) for every element of the listed groups (elements outside the row or the mask come as -inf)
-    template <typename F> __device__ __forceinline__ void each(F f) const {
-        const int per = P.coarse * U;
-        const int total = ng * per;
-        for (int t = threadIdx.x; t < total; t += kPickThreads) {
-            const int g = glist[t / per], j = t % per;
-            const int v = ((g >> 5) * P.coarse + j / U) * (32 * U) + (j % U) * 32 + (g & 31);
-            if (v >= nvec) continue;
-            float z[Elt<DT>::kPerVec];
-            unpack<DT>(row_vector<DT>(rv, P.mask, v, nvec), z);
-            const int e0 = rv.first_elem(v);
+// elements of the listed groups at or above zlow to the list, as far as they fit; returns how many there are.  One shared atomic
+// per warp and batch of vectors: as many on one address as there are elements cost more than the loads.
+template <int DT> __device__ __noinline__ int gather(float zlow) {
+    constexpr int B = 4, EPV = Elt<DT>::kPerVec;
+    const int lane = threadIdx.x & 31, total = S.ng * (S.coarse << S.ulog);
+    if (threadIdx.x == 0) S.listed = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int t0 = threadIdx.x; t0 - lane < total; t0 += B * kPickThreads) {
+        uint4 raw[B];
+        int v[B];
 #pragma unroll
-            for (int i = 0; i < Elt<DT>::kPerVec; ++i) f(z[i], e0 + i);
+        for (int k = 0; k < B; ++k) v[k] = t0 + k * kPickThreads < total ? listed_vector(t0 + k * kPickThreads) : S.nvec;
+#pragma unroll
+        for (int k = 0; k < B; ++k) raw[k] = state_vector<DT>(v[k]);
+        unsigned in = 0;
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            float z[EPV];
+            unpack<DT>(raw[k], z);
+#pragma unroll
+            for (int i = 0; i < EPV; ++i) in |= static_cast<unsigned>(z[i] >= zlow) << (k * EPV + i);
+        }
+        if (!__any_sync(0xffffffffu, in != 0)) continue;
+        int at = __popc(in);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += y;
+        }
+        int base = 0;
+        if (lane == 31) base = atomicAdd(&S.listed, at);
+        at += __shfl_sync(0xffffffffu, base, 31) - __popc(in);
+#pragma unroll 1
+        for (; in; in &= in - 1, ++at) {
+            const int bit = __ffs(in) - 1, k = bit / EPV, i = bit % EPV;
+            const uint4 r = k < 2 ? (k == 0 ? raw[0] : raw[1]) : (k == 2 ? raw[2] : raw[3]);
+            const int vk = k < 2 ? (k == 0 ? v[0] : v[1]) : (k == 2 ? v[2] : v[3]);
+            if (at < kListCap) list()[at] = element_of<DT>(vector_element<DT>(r, i), vk * EPV - S.head + i);
         }
     }
+    __syncthreads();
+    return S.listed;
+}
 
-    __device__ __forceinline__ void clear_bins(bool mass) {
-        for (int i = threadIdx.x; i < kBins; i += kPickThreads) {
-            cnt[i] = 0;
-            if (mass) { mlo[i] = 0; mhi[i] = 0; }
+// A floor under the border for a top-k of at most half as many as there are threads, from the threads' maxima (nearly as tight
+// as the groups' own): k of them are at or above it, so at least k elements are.  Steps down from m that double, then halve.
+__device__ __noinline__ float floor_from_threads(int k, float tmax) {
+    const float m = S.m;
+    float step = 1.f, low = m;
+    int n = 0;
+#pragma unroll 1
+    for (int i = 0; i < 40; ++i, step *= 2.f) {
+        low = m - step;
+        if (!(low >= -FLT_MAX)) return -INFINITY;
+        n = __syncthreads_count(tmax >= low);
+        if (n >= k) break;
+    }
+    if (n < k) return -INFINITY;
+    float high = m;                                                // (if fewer than k reach it; else the loop ends at once)
+#pragma unroll 1
+    for (int i = 0; i < 24 && n > k + k / 8 + 4; ++i) {
+        const float mid = low + 0.5f * (high - low);
+        if (mid <= low || mid >= high) break;
+        const int c = __syncthreads_count(tmax >= mid);
+        if (c >= k) { low = mid; n = c; } else high = mid;
+    }
+    return low;
+}
+
+// A floor under the border from the maxima of the groups: the smallest one among the first of 1024 equal parts of [q, m] that
+// hold `want` of them, by count or by mass (2^18 per unit of weight, rounded down, so never too much).  q: as far again below m as
+// the least of the threads' maxima.  -inf if they do not hold that much.
+__device__ __noinline__ float floor_from_groups(bool by_mass, unsigned want, float tmax) {
+    const float m = S.m, *sg = group_max();
+    const float least = order_float(block_min(float_order(tmax > -INFINITY ? tmax : m)));
+    const float q = fmaxf(least - (m - least), -FLT_MAX), step = (m - q) * (1.f / kBins);
+    if (!(step > 0.f) || !(step < INFINITY)) return -INFINITY;
+    const float per = 1.f / step, sf = static_cast<float>(S.w.s);
+#pragma unroll 2
+    for (int g = threadIdx.x; g < S.ngroups; g += kPickThreads) {
+        const float x = sg[g];
+        if (x >= q) {
+            const unsigned add = by_mass ? static_cast<unsigned>(ex2((x - m) * sf) * (262144.f * 0.9999f)) : 1u;
+            if (add) atomicAdd(bins() + min(static_cast<int>((m - x) * per), kBins - 1), add);
         }
-        __syncthreads();
     }
-    // first bin at which the running count (from `before`) reaches `want`; -1 if none does.  `before` becomes the
-    // count in front of that bin (or of everything).
-    __device__ __forceinline__ int find_count(unsigned long long want, unsigned long long &before) {
-        constexpr int per = kBins / kPickThreads;
-        unsigned long long x[per], mine = 0, total;
-#pragma unroll
-        for (int i = 0; i < per; ++i) { x[i] = cnt[threadIdx.x * per + i]; mine += x[i]; }
-        return find_bin<per>(x, mine, want, before, total);
+    const int bin = find_bin(want, 0, 20, false).bin;
+    if (bin < 0) return -INFINITY;
+    int low = INT_MAX;                                             // the smallest of these bins, by the same rounding that put it there
+#pragma unroll 2
+    for (int g = threadIdx.x; g < S.ngroups; g += kPickThreads) {
+        const float x = sg[g];
+        if (x >= q && min(static_cast<int>((m - x) * per), kBins - 1) <= bin) low = min(low, float_order(x));
     }
-    __device__ __forceinline__ int find_mass(unsigned long long want, unsigned long long &before) {
-        constexpr int per = kBins / kPickThreads;
-        unsigned long long x[per], mine = 0, total;
+    return order_float(block_min(low));
+}
+
+// ---- the border by digits of the key over the whole row ----
+//
+// For what the other ways leave: runs of equal logits longer than the list, a top-k of many thousands with top-p.  Every level
+// splits the interval of logits that holds the border into at most 1024 bins and reads again what groups reach it.  Masses are 64-bit
+// fixed-point numbers (two 32-bit shared atomics with a carry).
+
+enum : int { PASS_COUNT_KEYS, PASS_WEIGH_KEYS, PASS_WEIGH, PASS_COUNT, PASS_COUNT_IDS, PASS_LOWEST_ID };
+// One pass over the listed groups for the elements whose logit is in [low, high]: their number, mass or lowest id, or a histogram
+// of their keys down from `high`, or of their ids up from `base`.
+template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, float high, int shift, int base, double unit) {
+    constexpr int EPV = Elt<DT>::kPerVec;
+    const int total = S.ng * (S.coarse << S.ulog);
+    const uint32_t top = logit_key<DT>(high);
+    u64 mine = what == PASS_LOWEST_ID ? INT_MAX : 0;
+#pragma unroll 1
+    for (int t0 = threadIdx.x; t0 < total; t0 += 4 * kPickThreads) {
+        uint4 raw[4];
+        int v[4];
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
-            const int k = threadIdx.x * per + i;
-            x[i] = (static_cast<unsigned long long>(mhi[k]) << 32) + mlo[k];
-            mine += x[i];
+        for (int k = 0; k < 4; ++k) v[k] = t0 + k * kPickThreads < total ? listed_vector(t0 + k * kPickThreads) : S.nvec;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) raw[k] = state_vector<DT>(v[k]);
+        unsigned in = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float z[EPV];
+            unpack<DT>(raw[k], z);
+#pragma unroll
+            for (int i = 0; i < EPV; ++i) in |= static_cast<unsigned>(z[i] >= low && z[i] <= high) << (k * EPV + i);
         }
-        return find_bin<per>(x, mine, want, before, total);
-    }
-    template <int per>
-    __device__ __forceinline__ int find_bin(const unsigned long long (&x)[per], unsigned long long mine, unsigned long long want,
-                                            unsigned long long &before, unsigned long long &total) {
-        if (threadIdx.x == 0) sh.bi[0] = -1;
-        unsigned long long run = before + block_scan(mine, sh.wsum_u, total) - mine;
-        if (run < want && run + mine >= want) {                    // at most one thread
-#pragma unroll
-            for (int i = 0; i < per; ++i) {
-                if (run < want && run + x[i] >= want) { sh.bi[0] = threadIdx.x * per + i; sh.bu[0] = run; }
-                run += x[i];
+        if (what == PASS_COUNT) { mine += __popc(in); continue; }
+#pragma unroll 1
+        for (; in; in &= in - 1) {
+            const int bit = __ffs(in) - 1, k = bit / EPV, i = bit % EPV;
+            const float x = vector_element<DT>(k < 2 ? (k == 0 ? raw[0] : raw[1]) : (k == 2 ? raw[2] : raw[3]), i);
+            const int id = (k < 2 ? (k == 0 ? v[0] : v[1]) : (k == 2 ? v[2] : v[3])) * EPV - S.head + i;
+            if (what == PASS_LOWEST_ID) { mine = min(mine, static_cast<u64>(id)); continue; }
+            if (what == PASS_COUNT_IDS) {
+                if (id >= base && (id - base) >> shift < kBins) atomicAdd(bins() + ((id - base) >> shift), 1u);
+                continue;
             }
+            const u64 f = what == PASS_COUNT_KEYS ? 1ull : __double2ull_rn(S.w(x) * unit);
+            if (what == PASS_WEIGH) { mine += f; continue; }
+            const uint32_t j = (top - logit_key<DT>(x)) >> shift, lo = static_cast<uint32_t>(f);
+            const uint32_t old = atomicAdd(bins() + j, lo);
+            const uint32_t hi = static_cast<uint32_t>(f >> 32) + (old + lo < old ? 1u : 0u);
+            if (hi) atomicAdd(bins() + kBins + j, hi);
         }
-        __syncthreads();
-        const int bin = sh.bi[0];
-        before = bin < 0 ? before + total : sh.bu[0];
-        __syncthreads();
-        return bin;
     }
-
-    // A floor under the border from the group maxima: the smallest group maximum among the first bins that hold
-    // `want` of them (by count, or by fixed-point mass: 2^18 per unit of weight, rounded down, so never too much).
-    // Returns -FLT_MAX with ok = false if they do not hold that much.
-    __device__ __forceinline__ float floor_from_groups(bool by_mass, unsigned long long want, double s, bool &ok) {
-        clear_bins(false);
-        const float sf = static_cast<float>(s);
-        for (int g = threadIdx.x; g < ngroups; g += kPickThreads) {
-            const float x = sg[g];
-            if (x > -INFINITY) {
-                unsigned add = 1;
-                if (by_mass) add = static_cast<unsigned>(ex2((x - m) * sf) * (262144.f * 0.9999f));
-                if (add) atomicAdd(cnt + distance_bin(m, x), add);
+    if (what == PASS_WEIGH || what == PASS_COUNT) return block_prefix(mine).total;
+    if (what == PASS_LOWEST_ID) return static_cast<u64>(block_min(static_cast<int>(mine)));
+    return 0;
+}
+struct Border { float z; int id; };
+// The key at which the running measure, coming from `before`, reaches `want` within [lo, hi], and the measure in front of it; false if none does.
+template <int DT> __device__ __noinline__ bool key_by_digits(int what, uint32_t lo, uint32_t hi, double unit, u64 want, float tmax, uint32_t &key, u64 &before) {
+    list_groups(key_logit<DT>(lo), tmax);
+    for (;;) {
+        const int shift = bin_shift(hi - lo);
+        row_pass<DT>(what, key_logit<DT>(lo), key_logit<DT>(hi), shift, 0, unit);
+        const BinAt at = find_bin(want, before, 32, false);
+        before = at.before;
+        if (at.bin < 0) return false;
+        hi -= static_cast<uint32_t>(at.bin) << shift;
+        if (shift == 0) { key = hi; return true; }
+        const uint32_t width = (1u << shift) - 1u;
+        if (hi - lo > width) lo = hi - width;
+    }
+}
+// What is known of the border (of top-k where there is one, else of top-p): it is within [low, high], with `above` elements of `mass`
+// in front of them; low > high: nothing.  `Z`: mass of the row where there is no top-k.
+struct Hint { float low, high; u64 above; double mass; };
+template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &ask, float zmin, double Z, float tmax, const Hint &hint) {
+    const uint32_t top = logit_key<DT>(S.m), bottom = logit_key<DT>(-FLT_MAX);
+    const uint32_t near_lo = logit_key<DT>(hint.low), near_hi = logit_key<DT>(hint.high);
+    Border r;
+    r.z = -INFINITY; r.id = -1;                                    // everything finite
+    bool cut = false;                                              // something is left out
+    u64 take = 0, before = 0;                                      // how many of the elements at the border's logit are kept
+    uint32_t key = 0;
+    if (ask.k_on) {
+        if (hint.low <= hint.high && hint.above < static_cast<u64>(ask.k)) {
+            before = hint.above;
+            cut = key_by_digits<DT>(PASS_COUNT_KEYS, near_lo, near_hi, 1.0, ask.k, tmax, key, before);
+        }
+        if (!cut) {
+            before = 0;
+            cut = key_by_digits<DT>(PASS_COUNT_KEYS, bottom, top, 1.0, ask.k, tmax, key, before);
+        }
+        take = ask.k - before;
+    }
+    if (ask.p_on) {
+        if (ask.k_on) {                                            // the mass that top-k leaves: at most 2^20 weights up to 1
+            const double unit = 4398046511104.0;                   // 2^42
+            const uint32_t lo = cut ? key + 1 : bottom;
+            u64 above = 0;
+            if (lo <= top) {
+                list_groups(key_logit<DT>(lo), tmax);
+                above = row_pass<DT>(PASS_WEIGH, key_logit<DT>(lo), S.m, 0, 0, unit);
             }
+            Z = static_cast<double>(above) / unit + (cut ? static_cast<double>(take) * S.w(key_logit<DT>(key)) : 0.0);
         }
-        __syncthreads();
-        unsigned long long before = 0;
-        const int bin = find_count(want, before);
-        ok = bin >= 0;
-        if (!ok) return -FLT_MAX;
-        int low = INT_MAX;
-        for (int g = threadIdx.x; g < ngroups; g += kPickThreads) {
-            const float x = sg[g];
-            if (x > -INFINITY && distance_bin(m, x) <= bin) low = min(low, float_order(x));
+        const double unit = two_to(61 - exponent(Z));              // Z unit < 2^62
+        const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * Z * unit)));
+        const uint32_t lo = cut ? key + 1 : bottom;                // ties at the top-k border are counted apart
+        uint32_t k = 0;
+        bool by_p = false;
+        if (!ask.k_on && hint.low <= hint.high) {
+            before = __double2ull_rn(hint.mass * unit);
+            if (before < want) by_p = key_by_digits<DT>(PASS_WEIGH_KEYS, near_lo, near_hi, unit, want, tmax, k, before);
         }
-        return order_float(block_min_int(low, sh.wsum_i));
-    }
-
-    // The id of the n-th lowest id (n >= 1) among the elements equal to z: two levels of a histogram over ids.
-    __device__ __forceinline__ int nth_id_of(float z, unsigned long long n) {
-        int base = 0, shift = 0;
-        while ((P.V - 1) >> shift >= kBins) ++shift;
-        unsigned long long before = 0;
-        for (;;) {
-            clear_bins(false);
-            each([&](float x, int id) {
-                const int k = (id - base) >> shift;
-                if (x == z && id >= base && k < kBins) atomicAdd(cnt + k, 1u);
-            });
-            __syncthreads();
-            const int bin = find_count(n, before);
-            if (bin < 0) return INT_MAX;
-            base += bin << shift;
-            if (shift == 0) return base;
-            shift = max(0, shift - 10);
+        if (!by_p) {
+            before = 0;
+            by_p = lo <= top && key_by_digits<DT>(PASS_WEIGH_KEYS, lo, top, unit, want, tmax, k, before);
+        }
+        if (by_p) key = k;
+        if (by_p || cut) {
+            const u64 f = __double2ull_rn(S.w(key_logit<DT>(key)) * unit);
+            u64 need = 1;
+            if (want > before) need = f ? (want - before + f - 1) / f : ~0ull;
+            take = by_p ? max(need, 1ull) : min(max(need, 1ull), take);
+            cut = true;
         }
     }
-
-    // The border by digits of the key: every level splits the interval of logits that holds it into at most 1024
-    // bins.  Masses are 64-bit fixed-point numbers (two 32-bit shared atomics), so their sums do not depend on the
-    // order of the atomics.  `zlow`: no element below it can be kept.  `Z`: mass of the row where there is no top-k.
-    __device__ void border_by_digits(const RowAsk &ask, const Weights &w, float zlow, float zmin, double Z, float &bz, int &bid) {
-        list_groups(zlow);
-        const uint32_t top = logit_key(m), bottom = logit_key(zlow);
-        bz = -INFINITY; bid = -1;                                  // everything finite
-        bool cut = false;                                          // top-k leaves something out
-        unsigned long long ties = 0, take = 0;                     // elements at the border's logit, and how many are kept
-        uint32_t border = 0;
-        if (ask.k_on) {
-            uint32_t hi = top, lo = bottom;
-            unsigned long long before = 0;
+    if (cut) {
+        r.z = key_logit<DT>(key);
+        r.id = INT_MAX;
+        list_groups(r.z, tmax);
+        if (take < row_pass<DT>(PASS_COUNT, r.z, r.z, 0, 0, 0.0)) {
+            // the id of the last one that is kept, by digits of the id
+            int base = 0, shift = bin_shift(S.V - 1);
+            before = 0;
             for (;;) {
-                const uint32_t range = hi - lo;
-                const int shift = range < kBins ? 0 : 22 - __clz(range);
-                clear_bins(false);
-                each([&](float z, int) {
-                    const uint32_t key = logit_key(z);
-                    if (z >= zlow && key >= lo && key <= hi) atomicAdd(cnt + ((hi - key) >> shift), 1u);
-                });
-                __syncthreads();
-                const int bin = find_count(static_cast<unsigned long long>(ask.k), before);
-                if (bin < 0) break;                                // fewer than k finite logits
-                if (shift == 0) {
-                    cut = true;
-                    border = hi - bin; ties = cnt[bin]; take = ask.k - before;
-                    break;
-                }
-                hi -= static_cast<uint32_t>(bin) << shift;
-                const uint32_t width = (1u << shift) - 1u;
-                if (hi - lo > width) lo = hi - width;
+                row_pass<DT>(PASS_COUNT_IDS, r.z, r.z, shift, base, 0.0);
+                const BinAt at = find_bin(take, before, 32, false);
+                before = at.before;
+                base += at.bin << shift;
+                if (shift == 0) break;
+                shift = max(0, shift - 10);
             }
-            __syncthreads();
+            r.id = base;
+        }
+    }
+    if (ask.min_on && zmin > r.z) { r.z = zmin; r.id = INT_MAX; }
+    return r;
+}
+
+// ---- the border among thousands: a bracket from a sample ----
+
+// Two logits that the k-th largest (or the last one inside top-p) lies between but for bad luck, from up to 16384 elements
+// spread over the row: where the sample itself has that place, and four standard errors to both sides (fewer, if as many elements
+// as lie between would not fit `capacity`).  The sample is counted (weighed) in 1024 equal parts of the interval between its extremes.
+struct Bracket { float low, high; };
+template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity) {
+    constexpr int EPV = Elt<DT>::kPerVec, total = kSample / EPV;
+    const bool whole = S.nvec <= total;
+    const float m = S.m;
+    float least = INFINITY;
+    __syncthreads();
+#pragma unroll 8
+    for (int j = threadIdx.x; j < total; j += kPickThreads) {
+        const uint4 r = state_vector<DT>(whole ? j : static_cast<int>(static_cast<long long>(j) * S.nvec / total));
+        float z[EPV];
+        unpack<DT>(r, z);
+#pragma unroll
+        for (int k = 0; k < EPV; ++k) {
+            if (z[k] > -INFINITY) least = fminf(least, z[k]);
+            sample()[k * total + j] = z[k];
+        }
+    }
+    least = order_float(block_min(float_order(least)));
+    Bracket r;
+    r.low = -FLT_MAX; r.high = m;
+    const float width = (m - least) * (1.f / kBins), per_bin = 1.f / width;
+    if (!(width > 0.f) || !(width < INFINITY)) return r;           // (nothing seen but the largest value, or too wide for a float)
+    const double share = whole ? 1.0 : static_cast<double>(total) / S.nvec, spare = whole ? 0.0 : 4.0 * sqrt(1.0 - share);
+    const bool by_mass = !ask.k_on;
+    // by mass: (1-p) Z lies below the border, and the many small weights there are what a sample knows well; in units of
+    // 1/2^17 of it, each clipped at 1.9 (16384 of them fit 32 bits), from the smallest logit up
+    const float sf = static_cast<float>(S.w.s), unit = by_mass ? static_cast<float>(131072.0 / ((1.0 - static_cast<double>(ask.p)) * Z * share)) : 0.f;
+    auto bin_of = [&](float z) { return min(static_cast<int>((z - least) * per_bin), kBins - 1); };
+#pragma unroll 4
+    for (int j = threadIdx.x; j < kSample; j += kPickThreads) {
+        const float z = sample()[j];
+        if (!(z > -INFINITY)) continue;
+        if (by_mass) {
+            const unsigned add = __float2uint_rn(fminf(ex2((z - m) * sf) * unit, 249000.f));
+            if (add) atomicAdd(bins() + bin_of(z), add);
+        } else {
+            atomicAdd(bins() + (kBins - 1 - bin_of(z)), 1u);
+        }
+    }
+    double want, off;
+    if (by_mass) {
+        want = 131072.0;
+        const int place = find_bin(131072, 0, 20, true).bin;
+        float square = 0.f;
+#pragma unroll 4
+        for (int j = threadIdx.x; j < kSample; j += kPickThreads) {
+            const float z = sample()[j], a = ex2((z - m) * sf) * unit;
+            if (z > -INFINITY && (bin_of(z) <= place || place < 0)) square += a * a;
+        }
+        off = spare * sqrt(block_prefix(static_cast<double>(square)).total) + 600.0;
+    } else {
+        want = ask.k * share;
+        off = spare * (sqrt(want) + 1.0);
+    }
+    // the places in bins, by proportion inside a bin
+    auto place = [&](double at, bool keep) {
+        const BinAt f = find_bin(static_cast<u64>(fmax(1.0, at)), 0, 20, keep);
+        return f.bin < 0 ? -1.f : f.bin + static_cast<float>((at - static_cast<double>(f.before)) / static_cast<double>(f.measure));
+    };
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {
+        const float near = place(want - off, true), far = place(want + off, true);
+        r.low = -FLT_MAX; r.high = m;
+        if (by_mass) {
+            if (near > 0.f) r.low = least + near * width;
+            if (far >= 0.f) r.high = least + far * width;
+        } else {
+            if (far >= 0.f) r.low = m - far * width;
+            if (want - off >= 1.0 && near > 0.f) r.high = m - near * width;
+        }
+        if (round) break;
+        int inside = 0;
+#pragma unroll 4
+        for (int j = threadIdx.x; j < kSample; j += kPickThreads) inside += sample()[j] >= r.low && sample()[j] <= r.high;
+        const double expected = block_sum(inside) / share;
+        if (expected <= 0.9 * capacity) break;
+        off *= fmax(0.4, 0.8 * capacity / expected);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBins; i += kPickThreads) bins()[i] = 0;
+    r.high = fminf(r.high, m);
+    if (DT == TLI_BF16) {                                          // values of the row's type, so that keys and logits say the same
+        r.low = fmaxf(__bfloat162float(__float2bfloat16_rd(r.low)), -FLT_MAX);
+        r.high = __bfloat162float(__float2bfloat16_ru(r.high));
+    }
+    return r;
+}
+
+// ---- border and draw from the list ----
+
+// The border among the n listed elements (logits from ztop down to zlow), with `above` elements of mass `above_mass` in front of
+// them, all kept as far as the list reaches; if they number fewer than k, nothing below zlow could be kept either.  Elements >= edge
+// are kept, in the list and out of it (edge 0: the border is not here); where weights are needed, masses() has them in units of 1/unit.
+struct Edge { u64 edge; double unit; };
+template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask, bool draw, float zmin, double Z, int n, float ztop, float zlow, u64 above, double above_mass) {
+    const u64 first = element_of<DT>(ztop, 0), range = first - (static_cast<u64>(logit_key<DT>(zlow)) << 20);
+    Edge r;
+    r.edge = 1; r.unit = 1.0;
+    if (ask.k_on && above + n >= static_cast<u64>(ask.k)) {
+        r.edge = 0;
+        if (above >= static_cast<u64>(ask.k)) return r;
+        r.edge = find_element(n, 1, ask.k, above, first, range, 0);
+    }
+    if (ask.p_on || draw) {
+        // the masses' unit: every sum formed here stays below 2^60.  (Without Z: as many weights up to 1 as there are.)
+        const double most = ask.p_on && !ask.k_on ? Z : above_mass + fmin(static_cast<double>(n), ask.k_on ? static_cast<double>(ask.k) : static_cast<double>(n));
+        r.unit = two_to(59 - exponent(most));
+        u64 all = 0;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kPickThreads) {
+            const u64 f = list()[i] >= r.edge ? __double2ull_rn(S.w(element_logit<DT>(list()[i])) * r.unit) : 0ull;
+            masses()[i] = f;
+            all += f;
         }
         if (ask.p_on) {
-            double above = 0.0;
-            if (ask.k_on) {                                        // the mass that top-k leaves
-                double mine = 0.0;
-                each([&](float z, int) { if (!cut || logit_key(z) > border) mine += w(z); });
-                block_scan(mine, sh.wsum, above);
-                Z = above + (cut ? static_cast<double>(take) * w(key_logit(border)) : 0.0);
-            }
-            const int e = ilogb(Z) + 1;                            // Z < 2^e, in units of 2^(e-62) it fits
-            const double unit = scalbn(1.0, 62 - e);
-            const unsigned long long want = max(1ull, static_cast<unsigned long long>(ceil(static_cast<double>(ask.p) * Z * unit)));
-            uint32_t hi = top, lo = cut ? border + 1 : bottom;     // ties at the top-k border are counted apart
-            unsigned long long before = 0;
-            bool found = false;
-            if (lo <= hi) {
-                for (;;) {
-                    const uint32_t range = hi - lo;
-                    const int shift = range < kBins ? 0 : 22 - __clz(range);
-                    clear_bins(true);
-                    each([&](float z, int) {
-                        const uint32_t key = logit_key(z);
-                        if (z >= zlow && key >= lo && key <= hi) {
-                            const unsigned long long f = __double2ull_rn(w(z) * unit);
-                            const uint32_t k = (hi - key) >> shift, low = static_cast<uint32_t>(f);
-                            const uint32_t old = atomicAdd(mlo + k, low);
-                            const uint32_t high = static_cast<uint32_t>(f >> 32) + (old + low < old ? 1u : 0u);
-                            if (high) atomicAdd(mhi + k, high);
-                            if (shift == 0) atomicAdd(cnt + k, 1u);
-                        }
-                    });
-                    __syncthreads();
-                    const int bin = find_mass(want, before);
-                    if (bin < 0) break;
-                    if (shift == 0) {
-                        found = true;
-                        border = hi - bin; ties = cnt[bin];
-                        break;
-                    }
-                    hi -= static_cast<uint32_t>(bin) << shift;
-                    const uint32_t width = (1u << shift) - 1u;
-                    if (hi - lo > width) lo = hi - width;
-                }
-                __syncthreads();
-            }
-            if (found || cut) {
-                const unsigned long long f = __double2ull_rn(w(key_logit(border)) * unit);
-                unsigned long long need = want > before && f ? (want - before + f - 1) / f : 1ull;
-                if (want > before && !f) need = ~0ull;
-                take = min(max(need, 1ull), found ? ties : take);
-                cut = true;
-            }
+            const u64 before = __double2ull_rn(above_mass * r.unit);
+            const double mass = ask.k_on ? static_cast<double>(before + block_prefix(all).total) : Z * r.unit;
+            const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * mass)));
+            const u64 edge = above > 0 && before >= want ? 0ull : find_element(n, r.edge, want, before, first, range, BY_MASS);
+            r.edge = edge;
+            if (edge == 0) return r;
         }
-        if (cut) { bz = key_logit(border); bid = take >= ties ? INT_MAX : nth_id_of(bz, take); }
-        if (ask.min_on && zmin > bz) { bz = zmin; bid = INT_MAX; }
     }
+    if (ask.min_on) r.edge = max(r.edge, static_cast<u64>(logit_key<DT>(zmin)) << 20);
+    return r;
+}
+template <int DT> __device__ __forceinline__ Border border_of(u64 edge) {
+    Border r;
+    r.z = edge > 1 ? element_logit<DT>(edge) : -INFINITY;
+    r.id = edge > 1 ? element_id(edge) : -1;
+    return r;
+}
 
-    // The id that owns u * total over the kept elements, from a sum per strip.
-    __device__ void draw_by_strips(const RowAsk &ask, const Weights &w, float bz, int bid, float u, int &token, double &prob) {
-        auto kept = [&](float z, int id) { return z > bz || (z == bz && id <= bid); };
-        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        if (ask.whole_mass(P.sample) && bz == -INFINITY) {
-            for (int i = threadIdx.x; i < P.nstrip; i += kPickThreads) {
-                const StripSum ss = P.ssum[static_cast<size_t>(row) * P.nstrip + i];
-                strips[i] = ss.S > 0.0 && ss.m >= w.cut ? ss.S * exp2_neg((static_cast<double>(ss.m) - w.m) * w.s, w.tab) : 0.0;
-            }
-        } else {
-            for (int i = warp; i < P.nstrip; i += kPickWarps) {
-                double acc = 0.0;
-                if (sg[i / P.coarse * 32 + lane] >= bz) {
-                    for (int q = 0; q < U; ++q) {
-                        const int v = i * (32 * U) + q * 32 + lane;
-                        float z[Elt<DT>::kPerVec];
-                        unpack<DT>(row_vector<DT>(rv, P.mask, v, nvec), z);
-                        const int e0 = rv.first_elem(v);
-#pragma unroll
-                        for (int j = 0; j < Elt<DT>::kPerVec; ++j)
-                            if (kept(z[j], e0 + j)) acc += w(z[j]);
-                    }
-                }
-                acc = warp_sum(acc);
-                if (lane == 0) strips[i] = acc;
-            }
+struct Draw { int token; double prob; };
+// Border and draw from a list of at most one element per thread: every thread counts, and weighs, what is in front of its own
+// element, in the order of the logits and then in that of the ids.  Two trips through the list against ten block-wide steps.
+template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk &ask, bool draw, float u, float zmin, double Z, int n, Border &border) {
+    const int tid = threadIdx.x;
+    const u64 e = tid < n ? list()[tid] : 0ull;
+    // the masses' unit: every sum formed here stays below 2^60
+    const double unit = two_to(59 - exponent(ask.p_on && !ask.k_on ? Z : static_cast<double>(n)));
+    const bool weigh = ask.p_on || draw;
+    const double w = e && weigh ? S.w(element_logit<DT>(e)) : 0.0;
+    const u64 f = __double2ull_rn(w * unit);
+    masses()[tid] = f;
+    __syncthreads();
+    int rank = 0;
+    u64 ahead = 0;
+    if (e) {
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const bool before = list()[j] > e;
+            rank += before;
+            ahead += before ? masses()[j] : 0ull;
         }
-        __syncthreads();
-        const int per = (P.nstrip + kPickThreads - 1) / kPickThreads, first = threadIdx.x * per;
-        double mine = 0.0, total;
-        int last = -1;
-        for (int i = first; i < min(first + per, P.nstrip); ++i) {
-            mine += strips[i];
-            if (strips[i] > 0.0) last = i;
-        }
-        double run = block_scan(mine, sh.wsum, total) - mine;
-        const double target = static_cast<double>(u) * total;
-        last = block_max_int(last, sh.wsum_i);
-        int hit = INT_MAX;
-        for (int i = first; i < min(first + per, P.nstrip); ++i) {
-            if (strips[i] > 0.0 && run + strips[i] > target) { hit = i; break; }
-            run += strips[i];
-        }
-        const int strip = min(block_min_int(hit, sh.wsum_i), last);       // rounding can leave none above the target
-        if (strip == hit || (hit == INT_MAX && strip == last && first <= last && last < first + per)) {
-            double before = 0.0;                                   // the owner of the strip says what lies in front of it
-            if (strip == hit) before = run; else before = run - strips[last];
-            sh.bd[0] = before;
-        }
-        __syncthreads();
-        if (warp == 0) {
-            double base = sh.bd[0], w_last = 0.0, w_hit = 0.0;
-            int id_last = -1, id_hit = -1;
-            for (int q = 0; q < U && id_hit < 0; ++q) {
-                const int v = strip * (32 * U) + q * 32 + lane;
-                float z[Elt<DT>::kPerVec];
-                double x[Elt<DT>::kPerVec], sum = 0.0;
-                unpack<DT>(row_vector<DT>(rv, P.mask, v, nvec), z);
-                const int e0 = rv.first_elem(v);
-                int id_mine = -1;
-                double w_mine = 0.0;
-#pragma unroll
-                for (int j = 0; j < Elt<DT>::kPerVec; ++j) {
-                    x[j] = kept(z[j], e0 + j) ? w(z[j]) : 0.0;
-                    sum += x[j];
-                    if (x[j] > 0.0) { id_mine = e0 + j; w_mine = x[j]; }
-                }
-                double incl = sum;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double y = __shfl_up_sync(0xffffffffu, incl, o);
-                    if (lane >= o) incl += y;
-                }
-                const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + incl > target);
-                const unsigned some = __ballot_sync(0xffffffffu, sum > 0.0);
-                if (some) {
-                    const int src = 31 - __clz(some);
-                    id_last = __shfl_sync(0xffffffffu, id_mine, src);
-                    w_last = __shfl_sync(0xffffffffu, w_mine, src);
-                }
-                if (over) {
-                    const int src = __ffs(over) - 1;
-                    double c = base + (incl - sum);
-                    int id = id_mine;
-                    double wt = w_mine;
-#pragma unroll
-                    for (int j = Elt<DT>::kPerVec - 1; j >= 0; --j) {      // smallest j whose running sum exceeds the target
-                        double cj = c;
-#pragma unroll
-                        for (int i = 0; i <= j; ++i) cj += x[i];
-                        if (x[j] > 0.0 && cj > target) { id = e0 + j; wt = x[j]; }
-                    }
-                    id_hit = __shfl_sync(0xffffffffu, id, src);
-                    w_hit = __shfl_sync(0xffffffffu, wt, src);
-                }
-                base += __shfl_sync(0xffffffffu, incl, 31);
-            }
-            if (lane == 0) {
-                sh.bi[1] = id_hit >= 0 ? id_hit : id_last;
-                sh.bd[1] = (id_hit >= 0 ? w_hit : w_last) / total;
-            }
-        }
-        __syncthreads();
-        token = sh.bi[1];
-        prob = sh.bd[1];
     }
-};
+    const int k = ask.k_on ? min(ask.k, n) : n;
+    u64 want = ~0ull;
+    if (ask.p_on) {
+        if (e && rank == k - 1) S.before = ahead + f;              // the mass that top-k leaves
+        __syncthreads();
+        want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * (ask.k_on ? static_cast<double>(S.before) : Z * unit))));
+    }
+    const bool kept = e && rank < k && (ask.p_on ? ahead < want : true) && (ask.min_on ? rank == 0 || element_logit<DT>(e) >= zmin : true);
+    const int count = __syncthreads_count(kept);
+    if (e && rank == count - 1) { S.found = e; S.before = ahead + f; }
+    __syncthreads();
+    const u64 edge = S.found, total = S.before;
+    border.z = element_logit<DT>(edge);
+    border.id = element_id(edge);
+    // fewer kept than asked for: only min-p or the end of the row can be the reason, and both hold below the list too
+    Draw d = {-1, 0.0};
+    if (!draw) return d;
+    const u64 target = static_cast<u64>(static_cast<double>(u) * static_cast<double>(total));
+    u64 own = f;
+    if (target == 0) {                                             // the lowest id that has any weight
+        own = w > 0.0;
+        masses()[tid] = own;
+        __syncthreads();
+    }
+    if (kept) {
+        u64 before = 0;
+        const uint32_t id = static_cast<uint32_t>(e) & kIdMask;    // (falls as the id grows)
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) {
+            const u64 x = list()[j];
+            before += x >= edge && (static_cast<uint32_t>(x) & kIdMask) > id ? masses()[j] : 0ull;
+        }
+        if (before <= target && target < before + own) S.found = e;
+    }
+    __syncthreads();
+    const u64 hit = S.found;
+    d.token = element_id(hit);
+    d.prob = S.w(element_logit<DT>(hit)) * unit / static_cast<double>(total);
+    return d;
+}
 
-template <int DT, int U>
-__global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const RowsParams P) {
-    extern __shared__ __align__(16) unsigned char pick_smem[];
-    __shared__ PickShared sh;
+// The id that owns u * total among the listed elements >= edge.
+template <int DT> __device__ __noinline__ Draw draw_from_list(float u, int n, u64 edge, double unit) {
+    u64 mine = 0;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= edge) mine += masses()[i];
+    const u64 total = block_prefix(mine).total, target = static_cast<u64>(static_cast<double>(u) * static_cast<double>(total));
+    u64 hit;
+    if (target > 0) {
+        hit = find_element(n, edge, min(target + 1, total), 0, 0, S.V - 1, BY_MASS | BY_ID);
+    } else {                                                       // the lowest id that has any weight
+        int low = INT_MAX;
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kPickThreads)
+            if (list()[i] >= edge && element_logit<DT>(list()[i]) >= S.w.cut) low = min(low, element_id(list()[i]));
+        low = block_min(low);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += kPickThreads)
+            if (list()[i] >= edge && element_id(list()[i]) == low) S.found = list()[i];
+        __syncthreads();
+        hit = S.found;
+    }
+    Draw d;
+    d.token = element_id(hit);
+    d.prob = S.w(element_logit<DT>(hit)) * unit / static_cast<double>(total);
+    return d;
+}
+
+// The id that owns u * total over what (bz, bid) keeps of the row, from strips(), a sum per strip.
+template <int DT> __device__ __noinline__ Draw draw_by_strips(Border border, float u) {
+    constexpr int EPV = Elt<DT>::kPerVec;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();
+    const int per = (S.nstrip + kPickThreads - 1) / kPickThreads, first = threadIdx.x * per, end = min(first + per, S.nstrip);
+    double mine = 0.0;
+    int last = -1;
+#pragma unroll 1
+    for (int i = first; i < end; ++i) {
+        mine += strips()[i];
+        if (strips()[i] > 0.0) last = i;
+    }
+    const Prefix<double> p = block_prefix(mine);
+    const double target = static_cast<double>(u) * p.total;
+    last = block_max(last);
+    double run = p.before;
+    int hit = INT_MAX;
+#pragma unroll 1
+    for (int i = first; i < end; ++i) {
+        if (strips()[i] > 0.0 && run + strips()[i] > target) { hit = i; break; }
+        run += strips()[i];
+    }
+    const int lowest = block_min(hit), strip = min(lowest, last);  // rounding can leave none above the target
+    double *before = reinterpret_cast<double *>(&S.before);        // what lies in front of the strip: its owner says
+    if (strip == hit) *before = run;
+    else if (lowest == INT_MAX && first <= last && last < end) *before = run - strips()[last];
+    __syncthreads();
+    if (warp == 0) {
+        double base = *before, w_last = 0.0, w_hit = 0.0;
+        int id_last = -1, id_hit = -1;
+#pragma unroll 1
+        for (int q = 0; q < (1 << S.ulog) && id_hit < 0; ++q) {
+            const int v = (strip << (5 + S.ulog)) + q * 32 + lane, e0 = v * EPV - S.head;
+            const uint4 r = state_vector<DT>(v);
+            double x[EPV], sum = 0.0, w_mine = 0.0;
+            int id_mine = -1;
+#pragma unroll
+            for (int j = 0; j < EPV; ++j) {
+                const float z = vector_element<DT>(r, j);
+                x[j] = z > border.z || (z == border.z && e0 + j <= border.id) ? S.w(z) : 0.0;
+                sum += x[j];
+                if (x[j] > 0.0) { id_mine = e0 + j; w_mine = x[j]; }
+            }
+            double incl = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + incl > target), some = __ballot_sync(0xffffffffu, sum > 0.0);
+            if (some) {
+                const int src = 31 - __clz(some);
+                id_last = __shfl_sync(0xffffffffu, id_mine, src);
+                w_last = __shfl_sync(0xffffffffu, w_mine, src);
+            }
+            if (over) {
+                double c = base + (incl - sum), wt = w_mine;
+                int id = -1;
+#pragma unroll
+                for (int j = 0; j < EPV; ++j) {                    // the first whose running sum exceeds the target
+                    c += x[j];
+                    if (id < 0 && x[j] > 0.0 && c > target) { id = e0 + j; wt = x[j]; }
+                }
+                if (id < 0) id = id_mine;
+                const int src = __ffs(over) - 1;
+                id_hit = __shfl_sync(0xffffffffu, id, src);
+                w_hit = __shfl_sync(0xffffffffu, wt, src);
+            }
+            base += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0) {
+            S.found = static_cast<u64>(id_hit >= 0 ? id_hit : id_last);
+            *before = (id_hit >= 0 ? w_hit : w_last) / p.total;
+        }
+    }
+    __syncthreads();
+    Draw d;
+    d.token = static_cast<int>(S.found);
+    d.prob = *before;
+    return d;
+}
+
+__device__ __noinline__ void finish_row(const RowsParams &P, int row, int status, int mode, Border border, int token, double prob) {
+    if (threadIdx.x != 0) return;
+    if (P.status) P.status[row] = status;
+    if (P.sample) {
+        P.tokens[row] = token;
+        if (P.prob) P.prob[row] = static_cast<float>(prob);
+    } else {
+        RowBorder rb; rb.z = border.z; rb.id = border.id; rb.mode = mode; rb.pad = 0;
+        P.border[row] = rb;
+    }
+}
+// leaves the row to the spread and settle kernels
+__device__ __noinline__ void plan_row(const RowsParams &P, int row, int kind, float zlo, float zhi, int bid, float zmin, double Z) {
+    if (threadIdx.x != 0) return;
+    RowPlan pl;
+    pl.Z = Z; pl.zlo = zlo; pl.zhi = zhi; pl.bid = bid; pl.kind = kind; pl.m = S.m; pl.zmin = zmin; pl.listed = 0; pl.pad = 0;
+    P.plan[row] = pl;
+    P.todo[1 + atomicAdd(P.todo, 1)] = row;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
-    exp2_table_init(sh.tab, tid);
+    exp2_table_init(S.tab, tid);
+    enter_row<DT>(P, row, b);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const RowAsk ask(P, b);
-    Pick<DT, U> pk(P, sh, pick_smem, row, b);
+    const float u = P.sample ? __ldg(P.u + row) : 0.f;
+    const Border all = {-INFINITY, -1};
 
-    int status = 0, token = -1, mode = BORDER_APPLY, bid = -1;
-    float bz = -INFINITY;
-    double prob = 0.0;
-    auto finish = [&]() {
-        if (tid != 0) return;
-        if (P.status) P.status[row] = status;
-        if (P.sample) {
-            P.tokens[row] = token;
-            if (P.prob) P.prob[row] = static_cast<float>(prob);
-        } else {
-            RowBorder rb; rb.z = bz; rb.id = bid; rb.mode = mode; rb.pad = 0;
-            P.border[row] = rb;
-        }
-    };
-
-    if (ask.bad_tau) status |= TLI_ROW_BAD_TEMPERATURE;
-    if (ask.bad_filter) status |= TLI_ROW_BAD_FILTER;
-    if (status) { mode = BORDER_COPY; finish(); return; }
-    if (!pk.load_groups()) { status = TLI_ROW_NONFINITE; mode = BORDER_COPY; finish(); return; }
-    const float m = pk.m;
-    if (!(m > -INFINITY)) { status = TLI_ROW_FALLBACK; finish(); return; }     // no id to keep
+    __syncthreads();
+    const float tmax = load_groups<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32);
+    const int bad = (ask.bad_tau ? TLI_ROW_BAD_TEMPERATURE : 0) | (ask.bad_filter ? TLI_ROW_BAD_FILTER : 0);
+    if (bad) { finish_row(P, row, bad, BORDER_COPY, all, -1, 0.0); return; }
+    // NaN lies above +inf, and that above every finite number, in this order
+    const float m = order_float(block_max(tmax != tmax ? INT_MAX : float_order(tmax)));
+    if (!(m < INFINITY)) { finish_row(P, row, TLI_ROW_NONFINITE, BORDER_COPY, all, -1, 0.0); return; }
+    if (!(m > -INFINITY)) { finish_row(P, row, TLI_ROW_FALLBACK, BORDER_APPLY, all, -1, 0.0); return; }      // no id to keep
+    if (tid == 0) {
+        S.m = m;
+        if (!ask.one) S.w = Weights(m, ask.tau, S.tab);
+    }
 
     if (ask.one) {                                                 // the lowest id at the largest logit
-        pk.list_groups(m);
-        int best = INT_MAX;
-        pk.each([&](float z, int id) { if (z == m) best = min(best, id); });
-        bz = m; bid = token = block_min_int(best, sh.wsum_i);
-        prob = 1.0;
-        finish();
+        list_groups(m, tmax);
+        Border first;
+        first.z = m;
+        first.id = static_cast<int>(row_pass<DT>(PASS_LOWEST_ID, m, m, 0, 0, 0.0));
+        finish_row(P, row, 0, BORDER_APPLY, first, first.id, 1.0);
         return;
     }
-    const Weights w(m, ask.tau, sh.tab);
-    // min-p as a logit: z >= m + tau ln(min_p), in fp64, to the next float above
-    const float zmin = ask.min_on ? __double2float_ru(static_cast<double>(m) + static_cast<double>(ask.tau) * log(static_cast<double>(ask.least))) : -FLT_MAX;
-    if (ask.plain()) {
-        if (P.sample) { const float u = __ldg(P.u + row); pk.draw_by_strips(ask, w, bz, bid, u, token, prob); }
-        finish();
-        return;
-    }
+    __syncthreads();
     double Z = 0.0;
-    if (ask.p_on && !ask.k_on) {
+    if (ask.whole_mass(P.sample)) {                                // the strips' sums at the row's own largest logit
         double mine = 0.0;
+#pragma unroll 1
         for (int i = tid; i < P.nstrip; i += kPickThreads) {
             const StripSum ss = P.ssum[static_cast<size_t>(row) * P.nstrip + i];
-            if (ss.S > 0.0 && ss.m >= w.cut) mine += ss.S * exp2_neg((static_cast<double>(ss.m) - w.m) * w.s, w.tab);
+            const double x = ss.S > 0.0 && ss.m >= S.w.cut ? ss.S * exp2_neg((static_cast<double>(ss.m) - S.w.m) * S.w.s, S.tab) : 0.0;
+            strips()[i] = x;
+            mine += x;
         }
-        block_scan(mine, sh.wsum, Z);
+        Z = block_prefix(mine).total;
     }
+    Draw d = {-1, 0.0};
+    if (ask.plain()) {
+        if (P.sample) d = draw_by_strips<DT>(all, u);
+        finish_row(P, row, 0, BORDER_APPLY, all, d.token, d.prob);
+        return;
+    }
+    const float zmin = ask.zmin<DT>(m);
 
     // a floor under everything that can be kept
-    float floor = -FLT_MAX;
-    bool ok = true;
-    if (ask.k_on) floor = pk.floor_from_groups(false, ask.k, w.s, ok);
-    else if (ask.p_on) floor = pk.floor_from_groups(true, static_cast<unsigned long long>(ceil(static_cast<double>(ask.p) * Z * 262144.0)), w.s, ok);
-    if (!ok && ask.p_on && !ask.k_on) {
-        // ids of weight below (1-p) Z / V weigh less than (1-p) Z together: the border is at or above that weight
-        const double t = log((1.0 - static_cast<double>(ask.p)) * Z / P.V) * ask.tau * (1.0 + 1e-9);
-        floor = fmaxf(-FLT_MAX, __double2float_rd(static_cast<double>(m) + fmin(t, 0.0) - 1e-6 * fabs(static_cast<double>(m))));
+    float floor = -INFINITY;
+    if (ask.k_on) {
+        floor = ask.k <= kPickThreads / 2 ? floor_from_threads(ask.k, tmax) : floor_from_groups(false, ask.k, tmax);
+        if (floor == -INFINITY && P.V > kListCap && ask.k <= kListCap * 3 / 4) {       // too few groups for that many: from a sample
+            floor = bracket<DT>(ask, Z, kListCap - ask.k).low;
+            if (floor == -FLT_MAX) floor = -INFINITY;
+        }
+    } else if (ask.p_on && Z < 8192.0) {
+        floor = floor_from_groups(true, static_cast<unsigned>(ceil(static_cast<double>(ask.p) * Z * 262144.0)), tmax);
     }
-    const float zlow = ask.p_on ? floor : fmaxf(floor, zmin);
-    bool drawn = false, found = false;
-    if (ok) {
-        pk.list_groups(zlow);
-        if (tid == 0) sh.bi[2] = 0;
-        __syncthreads();
-        pk.each([&](float z, int id) {
-            if (z >= zlow) {
-                const int at = atomicAdd(&sh.bi[2], 1);
-                if (at < kListCap)
-                    pk.list[at] = (static_cast<unsigned long long>(logit_key(z)) << 32) | static_cast<uint32_t>(~id);
-            }
-        });
-        __syncthreads();
-        const int N = sh.bi[2];
-        if (N <= kListCap) {
-            int n2 = 32;
-            while (n2 < N) n2 <<= 1;
-            for (int i = N + tid; i < n2; i += kPickThreads) pk.list[i] = 0;
-            sort_descending(pk.list, n2);                          // by (logit descending, id ascending)
-            const int per = max(1, n2 / kPickThreads), first = tid * per;
-            const int limit = ask.k_on ? min(N, ask.k) : N;
-            double x[kListCap / kPickThreads], mine = 0.0, all;
+    const bool ok = floor > -INFINITY || (!ask.k_on && !ask.p_on);
+    const float zlow = ask.p_on ? fmaxf(floor, -FLT_MAX) : fmaxf(floor, zmin);
+    list_groups(zlow, tmax);
+    // every listed group has an element; without a floor only short and mostly masked rows are worth a try
+    const int n = S.ng <= (ok || P.V <= kListCap ? kListCap : 256) ? gather<DT>(zlow) : INT_MAX;
+    // (fewer than k above a sampled floor: there may be more below it)
+    const bool whole = !(ask.k_on && n < ask.k && zlow == floor);
+    Border border;
+    if (n <= kPickThreads && whole) {
+        d = pick_from_short_list<DT>(ask, P.sample, u, zmin, Z, n, border);
+        finish_row(P, row, 0, BORDER_APPLY, border, d.token, d.prob);
+        return;
+    }
+    if (n <= kListCap && whole) {
+        const Edge at = border_in_list<DT>(ask, P.sample, zmin, Z, n, m, zlow, 0, 0.0);
+        if (at.edge) {
+            if (P.sample) d = draw_from_list<DT>(u, n, at.edge, at.unit);
+            finish_row(P, row, 0, BORDER_APPLY, border_of<DT>(at.edge), d.token, d.prob);
+            return;
+        }
+    }
+    if (ask.k_on || ask.p_on) {
+        const Bracket br = bracket<DT>(ask, Z, P.listcap);
+        plan_row(P, row, PLAN_BRACKET, br.low, br.high, -1, zmin, Z);
+        return;
+    }
+    border.z = zmin; border.id = INT_MAX;                          // min-p alone: the border is known
+    if (P.sample) plan_row(P, row, PLAN_DRAW, INFINITY, border.z, border.id, zmin, 0.0);
+    else finish_row(P, row, 0, BORDER_APPLY, border, -1, 0.0);
+}
+
+// ---- rows whose kept set has thousands of elements ----
+
+// Each strip of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed; what lies from there down to
+// zlo goes to the row's list.  Weights cost 13 fp64 operations whether one lane of a warp wants them or 32, so the kept
+// logits are queued per warp and weighed 32 at a time.
+constexpr int kQueue = 32 * 9, kStash = 96;              // 31 and a vector of each lane; 64 and one element of each lane
+template <int DT, int U>
+__global__ void __launch_bounds__(kRowThreads) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
+    constexpr int EPV = Elt<DT>::kPerVec;
+    __shared__ float queues[kRowWarps][kQueue];
+    __shared__ u64 stashes[kRowWarps][kStash];
+    __shared__ double tab[16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int rows = __ldcg(P.todo);
+    if (rows == 0) return;
+    exp2_table_init(tab, threadIdx.x);
+    __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float *queue = queues[warp];
+    u64 *stash = stashes[warp];
+    const long long tasks = static_cast<long long>(rows) * P.nstrip;
+#pragma unroll 1
+    for (long long task = static_cast<long long>(blockIdx.x) * kRowWarps + warp; task < tasks; task += static_cast<long long>(gridDim.x) * kRowWarps) {
+        const int row = __ldcg(P.todo + 1 + static_cast<int>(task / P.nstrip)), strip = static_cast<int>(task % P.nstrip), b = row / P.R;
+        RowPlan *plan = P.plan + row;
+        const float gm = load_group<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32 + strip * 32 + lane);
+        const float zlo = __ldcg(&plan->zlo), zhi = __ldcg(&plan->zhi), m = __ldcg(&plan->m);
+        const int bid = __ldcg(&plan->bid);
+        const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
+        const int nvec = rv.nvec(), v0 = strip * (32 * U) + lane;
+        const bool want = gm >= fminf(zhi, zlo);
+        double acc = 0.0;
+        int queued = 0, stashed = 0, count = 0;
+        auto flush = [&]() {                                       // the stash to the row's list
+            __syncwarp();
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&plan->listed, stashed);
+            at = __shfl_sync(0xffffffffu, at, 0);
+            for (int i = lane; i < stashed; i += 32)
+                if (at + i < P.listcap) __stcg(P.lists + static_cast<size_t>(row) * P.listcap + at + i, stash[i]);
+            stashed = 0;
+            __syncwarp();
+        };
+        if (__any_sync(0xffffffffu, want)) {
+            const Weights w(m, __ldg(P.tau + b), tab);
+            const bool weigh = P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f);
+            uint4 raw[U];
 #pragma unroll
-            for (int i = 0; i < kListCap / kPickThreads; ++i) {
-                x[i] = (i < per && first + i < limit) ? w(key_logit(static_cast<uint32_t>(pk.list[first + i] >> 32))) : 0.0;
-                mine += x[i];
-            }
-            double run = block_scan(mine, sh.wsum, all) - mine;
-            const double mass = static_cast<double>(ask.p) * (ask.k_on ? all : Z);
-            found = !(ask.p_on && !ask.k_on && all < mass);        // (the floor is conservative; this holds but for rounding)
-            if (found) {
-                int count = 0, n;
+            for (int q = 0; q < U; ++q) raw[q] = row_vector<DT>(rv, P.mask, want ? v0 + q * 32 : nvec, nvec);
+#pragma unroll 1
+            for (int q = 0; q < U; ++q) {
+                const uint4 r = raw[0];
 #pragma unroll
-                for (int i = 0; i < kListCap / kPickThreads; ++i) {
-                    if (i < per && first + i < limit) {
-                        const float z = key_logit(static_cast<uint32_t>(pk.list[first + i] >> 32));
-                        const bool in = first + i == 0 || ((!ask.p_on || run < mass) && z >= zmin);
-                        count += in;
-                    }
-                    run += x[i];
+                for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
+                float z[EPV];
+                unpack<DT>(r, z);
+                const int e0 = rv.first_elem(v0 + q * 32);
+                unsigned near = 0;
+#pragma unroll
+                for (int i = 0; i < EPV; ++i) {
+                    const bool kept = z[i] > zhi || (z[i] == zhi && e0 + i <= bid);
+                    const unsigned who = __ballot_sync(0xffffffffu, kept);
+                    if (kept) queue[queued + __popc(who & ((1u << lane) - 1u))] = z[i];
+                    queued += __popc(who);
+                    near |= static_cast<unsigned>(!kept && z[i] >= zlo) << i;
                 }
-                block_scan(count, sh.wsum_i, n);
-                const unsigned long long edge = pk.list[n - 1];
-                bz = key_logit(static_cast<uint32_t>(edge >> 32));
-                bid = static_cast<int>(~static_cast<uint32_t>(edge));
+                while (__any_sync(0xffffffffu, near != 0)) {       // one of each lane at a time
+                    if (stashed > kStash - 32) flush();
+                    const unsigned who = __ballot_sync(0xffffffffu, near != 0);
+                    if (near) {
+                        const int i = __ffs(near) - 1;
+                        stash[stashed + __popc(who & ((1u << lane) - 1u))] = element_of<DT>(vector_element<DT>(r, i), e0 + i);
+                        near &= near - 1;
+                    }
+                    stashed += __popc(who);
+                }
+                __syncwarp();
+                while (queued >= 32) {
+                    queued -= 32; count += 32;
+                    if (weigh) acc += w(queue[queued + lane]);
+                }
+                __syncwarp();
+            }
+            count += queued;
+            if (weigh && lane < queued) acc += w(queue[lane]);
+            if (stashed) flush();
+            __syncwarp();
+        }
+        acc = warp_sum(acc);
+        if (lane == 0) {
+            StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
+            __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
+        }
+    }
+}
+
+// Such a row's border in its list, and the draw.
+template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, RowPlan *plan, int row, int b) {
+    constexpr int EPV = Elt<DT>::kPerVec;
+    const int tid = threadIdx.x;
+    const RowAsk ask(P, b);
+    const float zmin = __ldcg(&plan->zmin), zlo = __ldcg(&plan->zlo), zhi = __ldcg(&plan->zhi);
+    const double Z = __ldcg(&plan->Z);
+    u64 above = 0;
+    double mass = 0.0;
+#pragma unroll 1
+    for (int i = tid; i < P.nstrip; i += kPickThreads) {
+        const double2 raw = __ldcg(reinterpret_cast<const double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + i));
+        const StripSum ss = *reinterpret_cast<const StripSum *>(&raw);
+        strips()[i] = ss.S;
+        mass += ss.S;
+        above += ss.pad;
+    }
+    above = block_prefix(above).total;
+    mass = block_prefix(mass).total;
+    Border border = {zhi, __ldcg(&plan->bid)};
+    if (__ldcg(&plan->kind) == PLAN_BRACKET) {
+        const int n = static_cast<int>(__ldcg(&plan->listed));
+        Edge at = {0, 1.0};
+        if (n <= P.listcap) {
+#pragma unroll 1
+            for (int i = tid; i < n; i += kPickThreads) list()[i] = __ldcg(P.lists + static_cast<size_t>(row) * P.listcap + i);
+            __syncthreads();
+            // (fewer than k in all is not something the bracket can say)
+            if (!ask.k_on || above + n >= static_cast<u64>(ask.k)) at = border_in_list<DT>(ask, P.sample, zmin, Z, n, zhi, zlo, above, mass);
+        }
+        border = border_of<DT>(at.edge);
+        if (at.edge && border.z <= zhi) {
+            if (P.sample) {
+                // the kept elements of the list join their strips, in fixed point so that their order does not matter
+                u64 *extra = reinterpret_cast<u64 *>(bins());      // (1040 words at most)
+#pragma unroll 1
+                for (int i = tid; i < P.nstrip; i += kPickThreads) extra[i] = 0;
                 __syncthreads();
-                if (P.sample) {                                    // the same elements by id
-                    for (int i = tid; i < n2; i += kPickThreads) {
-                        const unsigned long long e = pk.list[i];
-                        pk.list[i] = i < n ? (e << 32) | (e >> 32) : 0ull;
+#pragma unroll 1
+                for (int i = tid; i < n; i += kPickThreads)
+                    if (list()[i] >= at.edge) atomicAdd(extra + ((element_id(list()[i]) + S.head) / EPV >> (5 + S.ulog)), masses()[i]);
+                __syncthreads();
+#pragma unroll 1
+                for (int i = tid; i < P.nstrip; i += kPickThreads) strips()[i] += static_cast<double>(extra[i]) / at.unit;
+            }
+        } else {                                                   // bad luck, or min-p above the bracket: the long way
+            const float tmax = load_groups<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32);
+            __syncthreads();
+            const Hint hint = {zlo, zhi, above, mass};
+            border = border_by_digits<DT>(ask, zmin, Z, tmax, hint);
+            if (P.sample) {
+                __syncthreads();
+#pragma unroll 1
+                for (int s = tid >> 5; s < P.nstrip; s += kPickWarps) {
+                    double acc = 0.0;
+#pragma unroll 1
+                    for (int t = tid & 31; t < (32 << S.ulog) * EPV; t += 32) {
+                        const int id = (s << (5 + S.ulog)) * EPV - S.head + t;
+                        if (id < 0 || id >= P.V || (P.mask && !(__ldg(P.mask + (id >> 5)) >> (id & 31) & 1u))) continue;
+                        const float z = load_elt<DT>(S.row, id);
+                        if (z > border.z || (z == border.z && id <= border.id)) acc += S.w(z);
                     }
-                    int n3 = 32;
-                    while (n3 < n) n3 <<= 1;
-                    sort_descending(pk.list, n3);                  // ~id descending: id ascending
-                    const int per3 = max(1, n3 / kPickThreads), first3 = tid * per3;
-                    mine = 0.0;
-#pragma unroll
-                    for (int i = 0; i < kListCap / kPickThreads; ++i) {
-                        x[i] = (i < per3 && first3 + i < n) ? w(key_logit(static_cast<uint32_t>(pk.list[first3 + i]))) : 0.0;
-                        mine += x[i];
-                    }
-                    run = block_scan(mine, sh.wsum, all) - mine;
-                    const double target = static_cast<double>(__ldg(P.u + row)) * all;
-                    int hit = INT_MAX, last = -1;
-#pragma unroll
-                    for (int i = 0; i < kListCap / kPickThreads; ++i) {
-                        run += x[i];
-                        if (x[i] > 0.0) {
-                            last = first3 + i;
-                            if (hit == INT_MAX && run > target) hit = first3 + i;
-                        }
-                    }
-                    last = block_max_int(last, sh.wsum_i);
-                    hit = min(block_min_int(hit, sh.wsum_i), last);
-                    const unsigned long long e = pk.list[hit];
-                    token = static_cast<int>(~static_cast<uint32_t>(e >> 32));
-                    prob = w(key_logit(static_cast<uint32_t>(e))) / all;
-                    drawn = true;
+                    acc = warp_sum(acc);
+                    if ((tid & 31) == 0) strips()[s] = acc;
                 }
             }
         }
+    }
+    Draw d = {-1, 0.0};
+    if (P.sample) d = draw_by_strips<DT>(border, __ldg(P.u + row));
+    finish_row(P, row, 0, BORDER_APPLY, border, d.token, d.prob);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kPickThreads) tli_rows_settle_kernel(const __grid_constant__ RowsParams P) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int rows = __ldcg(P.todo);
+    if (rows == 0) return;
+    exp2_table_init(S.tab, threadIdx.x);
+#pragma unroll 1
+    for (int i = blockIdx.x; i < rows; i += gridDim.x) {
+        const int row = __ldcg(P.todo + 1 + i), b = row / P.R;
+        RowPlan *plan = P.plan + row;
+        __syncthreads();                                           // the shared memory is free again
+        if (threadIdx.x == 0) {
+            S.m = __ldcg(&plan->m);
+            S.w = Weights(S.m, __ldg(P.tau + b), S.tab);
+        }
+        enter_row<DT>(P, row, b);
         __syncthreads();
+        settle_row<DT>(P, plan, row, b);
     }
-    if (!found) {
-        if (ask.k_on || ask.p_on) pk.border_by_digits(ask, w, zlow, zmin, Z, bz, bid);
-        else { bz = zmin; bid = INT_MAX; }
-    }
-    if (P.sample && !drawn) {
-        const float u = __ldg(P.u + row);
-        pk.draw_by_strips(ask, w, bz, bid, u, token, prob);
-    }
-    finish();
 }
 
 template <int DT, int U>
-__global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const RowsParams P) {
+__global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const __grid_constant__ RowsParams P) {
     constexpr uint32_t NI = Elt<DT>::kNegInfWord;
     constexpr int EPV = Elt<DT>::kPerVec;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -900,14 +1461,14 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const RowsPa
 
 // ---- host ----
 
-struct RowsLayout { int U, nstrip, coarse; size_t gmax, ssum, border, total; };
+struct RowsLayout { int U, nstrip, coarse, listcap; size_t gmax, ssum, border, plan, todo, lists, total; };
 
 // Groups of 8 vectors; of 4 where a row has at most 8192 vectors, so that a short row still has enough groups for
 // a top-k of a few hundred.
 RowsLayout rows_layout(long long rows, int V, int dtype) {
     RowsLayout L;
     const int nvec = chunks_per_row(V, dtype, 1);
-    L.U = nvec <= 8192 ? 4 : 8;
+    L.U = nvec <= 4096 ? 2 : nvec <= 8192 ? 4 : 8;
     L.nstrip = (nvec + 32 * L.U - 1) / (32 * L.U);
     L.coarse = (L.nstrip * 32 + kMaxGroups - 1) / kMaxGroups;
     const size_t elt = dtype == TLI_F32 ? 4 : 2;
@@ -915,6 +1476,11 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.gmax = off; off = align_up(off + elt * rows * L.nstrip * 32, 256);
     L.ssum = off; off = align_up(off + sizeof(StripSum) * rows * L.nstrip, 256);
     L.border = off; off = align_up(off + sizeof(RowBorder) * rows, 256);
+    L.plan = off; off = align_up(off + sizeof(RowPlan) * rows, 256);
+    L.todo = off; off = align_up(off + sizeof(int) * (rows + 1), 256);
+    // bracketed elements of a row: a sample of 16384 puts the border within about V/64 of them
+    L.listcap = V <= kListCap ? 0 : std::min(kListCap, std::max(2048, V / 32));
+    L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
     L.total = off;
     return L;
 }
@@ -926,7 +1492,19 @@ size_t rows_workspace(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, i
     return rows_layout(static_cast<long long>(B) * R, side == TLI_SIDE_TARGET ? ctx->V_t : ctx->V_d, dtype).total;
 }
 
-template <int DT, int U> int launch_rows(const RowsParams &P, cudaStream_t stream) {
+// Raises a kernel's limit of dynamic shared memory once per device.
+struct SmemAllowed {
+    std::atomic<unsigned long long> devices{0};
+    cudaError_t set(const void *fn, size_t bytes, int device) {
+        const unsigned long long bit = 1ull << (device & 63);
+        if (device < 64 && (devices.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+        if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+};
+
+template <int DT, int U> int launch_rows(const RowsParams &P, int device, int num_sms, cudaStream_t stream) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cudaLaunchAttribute attr[1];
@@ -937,11 +1515,24 @@ template <int DT, int U> int launch_rows(const RowsParams &P, cudaStream_t strea
     cfg.gridDim = dim3((P.nstrip + kRowWarps - 1) / kRowWarps, rows); cfg.blockDim = dim3(kRowThreads);
     cudaError_t e = cudaLaunchKernelEx(&cfg, tli_rows_scan_kernel<DT, U>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_scan_kernel");
-    e = cudaFuncSetAttribute(tli_rows_pick_kernel<DT, U>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPickSmemMax));
+    const size_t smem = pick_smem_bytes(P.nstrip, (P.nstrip + P.coarse - 1) / P.coarse * 32);
+    static SmemAllowed allowed, allowed_settle;
+    e = allowed.set(reinterpret_cast<const void *>(tli_rows_pick_kernel<DT>), kPickSmemMax, device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
-    cfg.gridDim = dim3(rows); cfg.blockDim = dim3(kPickThreads); cfg.dynamicSmemBytes = pick_smem_bytes((P.nstrip + P.coarse - 1) / P.coarse * 32);
-    e = cudaLaunchKernelEx(&cfg, tli_rows_pick_kernel<DT, U>, P);
+    cfg.gridDim = dim3(rows); cfg.blockDim = dim3(kPickThreads); cfg.dynamicSmemBytes = smem;
+    e = cudaLaunchKernelEx(&cfg, tli_rows_pick_kernel<DT>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_pick_kernel");
+    if (P.listcap > 0 && (P.top_k || P.top_p || P.min_p)) {        // (short rows and unfiltered ones are done)
+        e = allowed_settle.set(reinterpret_cast<const void *>(tli_rows_settle_kernel<DT>), kPickSmemMax, device);
+        if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+        const long long blocks = (static_cast<long long>(rows) * P.nstrip + kRowWarps - 1) / kRowWarps;
+        cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(blocks, 4LL * num_sms))); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = 0;
+        e = cudaLaunchKernelEx(&cfg, tli_rows_spread_kernel<DT, U>, P);
+        if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_spread_kernel");
+        cfg.gridDim = dim3(std::min<unsigned>(rows, 2u * num_sms)); cfg.blockDim = dim3(kPickThreads); cfg.dynamicSmemBytes = smem;
+        e = cudaLaunchKernelEx(&cfg, tli_rows_settle_kernel<DT>, P);
+        if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_settle_kernel");
+    }
     if (!P.sample) {
         cfg.gridDim = dim3((P.nstrip + kRowWarps - 1) / kRowWarps, rows); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = 0;
         e = cudaLaunchKernelEx(&cfg, tli_rows_mask_kernel<DT, U>, P);
@@ -955,12 +1546,18 @@ int run_rows(RowsParams &P, const tli_ctx *ctx, int32_t dtype, int32_t side, voi
     P.mask = side == TLI_SIDE_TARGET ? nullptr : ctx->d_mask;
     const RowsLayout L = rows_layout(static_cast<long long>(P.B) * P.R, P.V, dtype);
     char *ws = reinterpret_cast<char *>(workspace);
-    P.nstrip = L.nstrip; P.coarse = L.coarse;
+    P.nstrip = L.nstrip; P.coarse = L.coarse; P.ulog = L.U == 2 ? 1 : L.U == 4 ? 2 : 3;
     P.gmax = ws + L.gmax;
     P.ssum = reinterpret_cast<StripSum *>(ws + L.ssum);
     P.border = reinterpret_cast<RowBorder *>(ws + L.border);
-    if (dtype == TLI_F32) return L.U == 4 ? launch_rows<TLI_F32, 4>(P, stream) : launch_rows<TLI_F32, 8>(P, stream);
-    return L.U == 4 ? launch_rows<TLI_BF16, 4>(P, stream) : launch_rows<TLI_BF16, 8>(P, stream);
+    P.plan = reinterpret_cast<RowPlan *>(ws + L.plan);
+    P.todo = reinterpret_cast<int *>(ws + L.todo);
+    P.lists = reinterpret_cast<unsigned long long *>(ws + L.lists);
+    P.listcap = L.listcap;
+#define TLI_ROWS(U) (dtype == TLI_F32 ? launch_rows<TLI_F32, U>(P, ctx->device, ctx->num_sms, stream) \
+                                     : launch_rows<TLI_BF16, U>(P, ctx->device, ctx->num_sms, stream))
+    return L.U == 2 ? TLI_ROWS(2) : L.U == 4 ? TLI_ROWS(4) : TLI_ROWS(8);
+#undef TLI_ROWS
 }
 
 // What tli_sample() and tli_filter() check alike.
