@@ -42,8 +42,8 @@ constexpr int kBins = 1024;
 struct __align__(16) StripSum { double S; float m; int pad; };       // sum of 2^((z - m) s) over a strip, m its largest
 struct __align__(16) RowBorder { float z; int id; int mode; int pad; };
 enum : int { BORDER_APPLY = 0, BORDER_COPY = 1 };
-// What the pick kernel leaves to the spread and settle kernels: ids above (zhi, bid) are kept, below zlo none is.
-struct __align__(16) RowPlan { double Z; float zlo, zhi; int bid, kind; float m, zmin; int listed, pad; };
+// What the pick kernel leaves to the spread kernel: ids above (zhi, bid) are kept, below zlo none is.
+struct __align__(16) RowPlan { double Z; float zlo, zhi; int bid, kind; float m, zmin; int listed, done; };
 enum : int { PLAN_BRACKET = 0, PLAN_DRAW = 1 };                      // the border is in between; it is (zhi, bid)
 
 struct RowsParams {
@@ -56,7 +56,7 @@ struct RowsParams {
     StripSum *ssum;                        // [rows][nstrip]
     RowBorder *border;                     // [rows]
     RowPlan *plan;                         // [rows]
-    int *todo;                             // [1 + rows]: how many rows the spread and settle kernels have, and which
+    int *todo;                             // [2 + rows]: how many rows the spread kernel has, and which; behind them its next task
     unsigned long long *lists; int listcap;    // [rows][listcap]
     void *out; long long osb, osr;
 };
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const __grid
     const int row = blockIdx.y, b = row / P.R;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int strip = blockIdx.x * kRowWarps + warp;
-    if (blockIdx.x == 0 && row == 0 && threadIdx.x == 0) *P.todo = 0;
+    if (blockIdx.x == 0 && row == 0 && threadIdx.x == 0) { *P.todo = 0; P.todo[1 + P.B * P.R] = 0; }
     const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
     const int nvec = rv.nvec(), v0 = strip * (32 * U) + lane;
     uint4 raw[U];
@@ -288,32 +288,35 @@ struct PickState {
     // the row
     Weights w;
     const uint4 *vec0; const void *row; const uint32_t *mask;
-    int head, V, nvec, nstrip, ulog, coarse, ngroups, ng;
+    int head, V, nvec, nstrip, ulog, coarse, ngroups;
+    int ng;                  // groups listed; -1: the whole row is
+    int room;                // 8-byte words between the list's start and the strip sums
     float m;
 };
 __shared__ PickState S;
-// Dynamic shared memory: the elements that may lie at the border and their weights (or a sample of the row), three words per
-// bin of a histogram (zero between uses), the strip sums, the row's group maxima, the numbers of the groups to read again.
+// Dynamic shared memory: three words per bin of a histogram (zero between uses), the strip sums, the elements that may lie at
+// the border; in the pick kernel also the row's group maxima, the numbers of the groups to read again, and room behind the list for
+// a sample of the row.
 extern __shared__ __align__(16) unsigned char pick_smem[];
-constexpr size_t pick_smem_bytes(int nstrip, int ngroups) {
-    return kListCap * 16 + kBins * 12 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6;
-}
-constexpr size_t kPickSmemMax = pick_smem_bytes((TLI_MAX_V + 6) / (4 * 32 * 8) + 1, kMaxGroups);
-static_assert(kSample * 4 <= kListCap * 16, "the sample takes the place of the list");
-__device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem); }
-__device__ __forceinline__ u64 *masses() { return list() + kListCap; }
-__device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem); }
-__device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem + kListCap * 16); }
-__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kListCap * 16 + kBins * 12); }
+constexpr size_t settle_smem_bytes(int nstrip) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8; }
+constexpr size_t pick_smem_bytes(int nstrip, int ngroups) { return kBins * 12 + kSample * 4 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6; }
+constexpr int kMaxRowStrips = (TLI_MAX_V + 6) / (4 * 32 * 8) + 1;
+constexpr size_t kPickSmemMax = pick_smem_bytes(kMaxRowStrips, kMaxGroups), kSettleSmemMax = settle_smem_bytes(kMaxRowStrips);
+static_assert(kSample * 4 >= kListCap * 8, "the sample's room holds the list");
+__device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem); }
+__device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem + kBins * 12); }
+__device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem + kBins * 12); }
+__device__ __forceinline__ u64 *masses() { return list() + kPickThreads; }                // of a short list
+__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12) + S.room; }
 __device__ __forceinline__ float *group_max() { return reinterpret_cast<float *>(strips() + S.nstrip); }
 __device__ __forceinline__ unsigned short *group_list() { return reinterpret_cast<unsigned short *>(group_max() + S.ngroups); }
 
-template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b) {      // (visible after the next barrier)
+template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b, int room) {      // (visible after the next barrier)
     for (int i = threadIdx.x; i < 3 * kBins / 4; i += kPickThreads) reinterpret_cast<uint4 *>(bins())[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) {
         const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
         S.vec0 = rv.vec0; S.row = rv.row; S.head = rv.head; S.V = P.V; S.nvec = rv.nvec(); S.mask = P.mask;
-        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse;
+        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse; S.room = room; S.ng = -1;
         S.ngroups = (P.nstrip + P.coarse - 1) / P.coarse * 32;
     }
 }
@@ -407,6 +410,8 @@ __device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool kee
     return r;
 }
 __device__ __forceinline__ int bin_shift(u64 range) { return range < kBins ? 0 : 54 - __clzll(range); }      // (range >> shift) < 1024
+// an element's weight in units of 1/unit; sums of it do not depend on their order
+template <int DT> __device__ __forceinline__ u64 mass_of(u64 e, double unit) { return __double2ull_rn(S.w(element_logit<DT>(e)) * unit); }
 __device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^60, in three words of 20 bits: 4096 cannot overflow 32
     unsigned *w = bins() + k;
     atomicAdd(w, static_cast<uint32_t>(f) & 0xfffffu);
@@ -419,7 +424,7 @@ __device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^60, i
 // measure (their number; BY_MASS: their fixed-point mass) reaches `want`, coming from `before`; 0 if none does.  A histogram
 // of 1024 bins over the interval that is left, from the element `first` on, until it holds one.
 enum : int { BY_MASS = 1, BY_ID = 2 };
-__device__ __noinline__ u64 find_element(int n, u64 edge, u64 want, u64 before, u64 first, u64 range, int how) {
+template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 want, u64 before, u64 first, u64 range, int how, double unit) {
     u64 low = 0;
     auto pos = [&](u64 e) { return (how & BY_ID) ? static_cast<u64>(element_id(e)) : first - e; };
     for (;;) {
@@ -428,7 +433,7 @@ __device__ __noinline__ u64 find_element(int n, u64 edge, u64 want, u64 before, 
         for (int i = threadIdx.x; i < n; i += kPickThreads) {
             const u64 e = list()[i], p = pos(e) - low;
             if (e >= edge && p <= range) {
-                if (how & BY_MASS) add_mass(static_cast<int>(p >> shift), masses()[i]);
+                if (how & BY_MASS) add_mass(static_cast<int>(p >> shift), mass_of<DT>(e, unit));
                 else atomicAdd(bins() + static_cast<int>(p >> shift), 1u);
             }
         }
@@ -514,8 +519,10 @@ __device__ __noinline__ void list_groups(float floor, float tmax) {
     }
     __syncthreads();
 }
-// the t-th vector of the listed groups (S.coarse << S.ulog of them each)
+// vectors of the listed groups (S.coarse << S.ulog of them each), and the t-th of them
+__device__ __forceinline__ int listed_vectors() { return S.ng < 0 ? S.nvec : S.ng * (S.coarse << S.ulog); }
 __device__ __forceinline__ int listed_vector(int t) {
+    if (S.ng < 0) return t;
     const int per = S.coarse << S.ulog;
     const int k = S.coarse == 1 ? t >> S.ulog : t / per, j = t - k * per, g = group_list()[k];
     return ((((g >> 5) * S.coarse + (j >> S.ulog)) << S.ulog) + (j & ((1 << S.ulog) - 1))) * 32 + (g & 31);
@@ -525,7 +532,7 @@ __device__ __forceinline__ int listed_vector(int t) {
 // per warp and batch of vectors: as many on one address as there are elements cost more than the loads.
 template <int DT> __device__ __noinline__ int gather(float zlow) {
     constexpr int B = 4, EPV = Elt<DT>::kPerVec;
-    const int lane = threadIdx.x & 31, total = S.ng * (S.coarse << S.ulog);
+    const int lane = threadIdx.x & 31, total = listed_vectors();
     if (threadIdx.x == 0) S.listed = 0;
     __syncthreads();
 #pragma unroll 1
@@ -622,15 +629,15 @@ __device__ __noinline__ float floor_from_groups(bool by_mass, unsigned want, flo
 // ---- the border by digits of the key over the whole row ----
 //
 // For what the other ways leave: runs of equal logits longer than the list, a top-k of many thousands with top-p.  Every level
-// splits the interval of logits that holds the border into at most 1024 bins and reads again what groups reach it.  Masses are 64-bit
+// splits the interval of logits that holds the border into at most 1024 bins and reads the row again.  Masses are 64-bit
 // fixed-point numbers (two 32-bit shared atomics with a carry).
 
 enum : int { PASS_COUNT_KEYS, PASS_WEIGH_KEYS, PASS_WEIGH, PASS_COUNT, PASS_COUNT_IDS, PASS_LOWEST_ID };
-// One pass over the listed groups for the elements whose logit is in [low, high]: their number, mass or lowest id, or a histogram
+// One pass over the row (or its listed groups) for the elements whose logit is in [low, high]: their number, mass or lowest id, or a histogram
 // of their keys down from `high`, or of their ids up from `base`.
 template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, float high, int shift, int base, double unit) {
     constexpr int EPV = Elt<DT>::kPerVec;
-    const int total = S.ng * (S.coarse << S.ulog);
+    const int total = listed_vectors();
     const uint32_t top = logit_key<DT>(high);
     u64 mine = what == PASS_LOWEST_ID ? INT_MAX : 0;
 #pragma unroll 1
@@ -674,8 +681,7 @@ template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, floa
 }
 struct Border { float z; int id; };
 // The key at which the running measure, coming from `before`, reaches `want` within [lo, hi], and the measure in front of it; false if none does.
-template <int DT> __device__ __noinline__ bool key_by_digits(int what, uint32_t lo, uint32_t hi, double unit, u64 want, float tmax, uint32_t &key, u64 &before) {
-    list_groups(key_logit<DT>(lo), tmax);
+template <int DT> __device__ __noinline__ bool key_by_digits(int what, uint32_t lo, uint32_t hi, double unit, u64 want, uint32_t &key, u64 &before) {
     for (;;) {
         const int shift = bin_shift(hi - lo);
         row_pass<DT>(what, key_logit<DT>(lo), key_logit<DT>(hi), shift, 0, unit);
@@ -691,7 +697,7 @@ template <int DT> __device__ __noinline__ bool key_by_digits(int what, uint32_t 
 // What is known of the border (of top-k where there is one, else of top-p): it is within [low, high], with `above` elements of `mass`
 // in front of them; low > high: nothing.  `Z`: mass of the row where there is no top-k.
 struct Hint { float low, high; u64 above; double mass; };
-template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &ask, float zmin, double Z, float tmax, const Hint &hint) {
+template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &ask, float zmin, double Z, const Hint &hint) {
     const uint32_t top = logit_key<DT>(S.m), bottom = logit_key<DT>(-FLT_MAX);
     const uint32_t near_lo = logit_key<DT>(hint.low), near_hi = logit_key<DT>(hint.high);
     Border r;
@@ -702,11 +708,11 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
     if (ask.k_on) {
         if (hint.low <= hint.high && hint.above < static_cast<u64>(ask.k)) {
             before = hint.above;
-            cut = key_by_digits<DT>(PASS_COUNT_KEYS, near_lo, near_hi, 1.0, ask.k, tmax, key, before);
+            cut = key_by_digits<DT>(PASS_COUNT_KEYS, near_lo, near_hi, 1.0, ask.k, key, before);
         }
         if (!cut) {
             before = 0;
-            cut = key_by_digits<DT>(PASS_COUNT_KEYS, bottom, top, 1.0, ask.k, tmax, key, before);
+            cut = key_by_digits<DT>(PASS_COUNT_KEYS, bottom, top, 1.0, ask.k, key, before);
         }
         take = ask.k - before;
     }
@@ -715,10 +721,7 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
             const double unit = 4398046511104.0;                   // 2^42
             const uint32_t lo = cut ? key + 1 : bottom;
             u64 above = 0;
-            if (lo <= top) {
-                list_groups(key_logit<DT>(lo), tmax);
-                above = row_pass<DT>(PASS_WEIGH, key_logit<DT>(lo), S.m, 0, 0, unit);
-            }
+            if (lo <= top) above = row_pass<DT>(PASS_WEIGH, key_logit<DT>(lo), S.m, 0, 0, unit);
             Z = static_cast<double>(above) / unit + (cut ? static_cast<double>(take) * S.w(key_logit<DT>(key)) : 0.0);
         }
         const double unit = two_to(61 - exponent(Z));              // Z unit < 2^62
@@ -728,11 +731,11 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
         bool by_p = false;
         if (!ask.k_on && hint.low <= hint.high) {
             before = __double2ull_rn(hint.mass * unit);
-            if (before < want) by_p = key_by_digits<DT>(PASS_WEIGH_KEYS, near_lo, near_hi, unit, want, tmax, k, before);
+            if (before < want) by_p = key_by_digits<DT>(PASS_WEIGH_KEYS, near_lo, near_hi, unit, want, k, before);
         }
         if (!by_p) {
             before = 0;
-            by_p = lo <= top && key_by_digits<DT>(PASS_WEIGH_KEYS, lo, top, unit, want, tmax, k, before);
+            by_p = lo <= top && key_by_digits<DT>(PASS_WEIGH_KEYS, lo, top, unit, want, k, before);
         }
         if (by_p) key = k;
         if (by_p || cut) {
@@ -746,7 +749,6 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
     if (cut) {
         r.z = key_logit<DT>(key);
         r.id = INT_MAX;
-        list_groups(r.z, tmax);
         if (take < row_pass<DT>(PASS_COUNT, r.z, r.z, 0, 0, 0.0)) {
             // the id of the last one that is kept, by digits of the id
             int base = 0, shift = bin_shift(S.V - 1);
@@ -864,7 +866,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
 
 // The border among the n listed elements (logits from ztop down to zlow), with `above` elements of mass `above_mass` in front of
 // them, all kept as far as the list reaches; if they number fewer than k, nothing below zlow could be kept either.  Elements >= edge
-// are kept, in the list and out of it (edge 0: the border is not here); where weights are needed, masses() has them in units of 1/unit.
+// are kept, in the list and out of it (edge 0: the border is not here).  unit: for masses, so that no sum of them reaches 2^60.
 struct Edge { u64 edge; double unit; };
 template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask, bool draw, float zmin, double Z, int n, float ztop, float zlow, u64 above, double above_mass) {
     const u64 first = element_of<DT>(ztop, 0), range = first - (static_cast<u64>(logit_key<DT>(zlow)) << 20);
@@ -873,24 +875,23 @@ template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask,
     if (ask.k_on && above + n >= static_cast<u64>(ask.k)) {
         r.edge = 0;
         if (above >= static_cast<u64>(ask.k)) return r;
-        r.edge = find_element(n, 1, ask.k, above, first, range, 0);
+        r.edge = find_element<DT>(n, 1, ask.k, above, first, range, 0, 0.0);
     }
     if (ask.p_on || draw) {
-        // the masses' unit: every sum formed here stays below 2^60.  (Without Z: as many weights up to 1 as there are.)
+        // (without Z: as many weights up to 1 as there are)
         const double most = ask.p_on && !ask.k_on ? Z : above_mass + fmin(static_cast<double>(n), ask.k_on ? static_cast<double>(ask.k) : static_cast<double>(n));
         r.unit = two_to(59 - exponent(most));
-        u64 all = 0;
-#pragma unroll 1
-        for (int i = threadIdx.x; i < n; i += kPickThreads) {
-            const u64 f = list()[i] >= r.edge ? __double2ull_rn(S.w(element_logit<DT>(list()[i])) * r.unit) : 0ull;
-            masses()[i] = f;
-            all += f;
-        }
         if (ask.p_on) {
             const u64 before = __double2ull_rn(above_mass * r.unit);
-            const double mass = ask.k_on ? static_cast<double>(before + block_prefix(all).total) : Z * r.unit;
+            double mass = Z * r.unit;
+            if (ask.k_on) {                                        // the mass that top-k leaves
+                u64 all = 0;
+#pragma unroll 1
+                for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], r.unit);
+                mass = static_cast<double>(before + block_prefix(all).total);
+            }
             const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * mass)));
-            const u64 edge = above > 0 && before >= want ? 0ull : find_element(n, r.edge, want, before, first, range, BY_MASS);
+            const u64 edge = above > 0 && before >= want ? 0ull : find_element<DT>(n, r.edge, want, before, first, range, BY_MASS, r.unit);
             r.edge = edge;
             if (edge == 0) return r;
         }
@@ -973,11 +974,11 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
 template <int DT> __device__ __noinline__ Draw draw_from_list(float u, int n, u64 edge, double unit) {
     u64 mine = 0;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= edge) mine += masses()[i];
+    for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= edge) mine += mass_of<DT>(list()[i], unit);
     const u64 total = block_prefix(mine).total, target = static_cast<u64>(static_cast<double>(u) * static_cast<double>(total));
     u64 hit;
     if (target > 0) {
-        hit = find_element(n, edge, min(target + 1, total), 0, 0, S.V - 1, BY_MASS | BY_ID);
+        hit = find_element<DT>(n, edge, min(target + 1, total), 0, 0, S.V - 1, BY_MASS | BY_ID, unit);
     } else {                                                       // the lowest id that has any weight
         int low = INT_MAX;
 #pragma unroll 1
@@ -1090,11 +1091,11 @@ __device__ __noinline__ void finish_row(const RowsParams &P, int row, int status
         P.border[row] = rb;
     }
 }
-// leaves the row to the spread and settle kernels
+// leaves the row to the spread kernel
 __device__ __noinline__ void plan_row(const RowsParams &P, int row, int kind, float zlo, float zhi, int bid, float zmin, double Z) {
     if (threadIdx.x != 0) return;
     RowPlan pl;
-    pl.Z = Z; pl.zlo = zlo; pl.zhi = zhi; pl.bid = bid; pl.kind = kind; pl.m = S.m; pl.zmin = zmin; pl.listed = 0; pl.pad = 0;
+    pl.Z = Z; pl.zlo = zlo; pl.zhi = zhi; pl.bid = bid; pl.kind = kind; pl.m = S.m; pl.zmin = zmin; pl.listed = 0; pl.done = 0;
     P.plan[row] = pl;
     P.todo[1 + atomicAdd(P.todo, 1)] = row;
 }
@@ -1103,7 +1104,7 @@ template <int DT>
 __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
     exp2_table_init(S.tab, tid);
-    enter_row<DT>(P, row, b);
+    enter_row<DT>(P, row, b, kSample / 2);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const RowAsk ask(P, b);
@@ -1196,98 +1197,78 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
 
 // ---- rows whose kept set has thousands of elements ----
 
-// Each strip of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed; what lies from there down to
+// One strip of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed; what lies from there down to
 // zlo goes to the row's list.  Weights cost 13 fp64 operations whether one lane of a warp wants them or 32, so the kept
 // logits are queued per warp and weighed 32 at a time.
 constexpr int kQueue = 32 * 9, kStash = 96;              // 31 and a vector of each lane; 64 and one element of each lane
-template <int DT, int U>
-__global__ void __launch_bounds__(kRowThreads) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
+static_assert(kPickWarps * (kQueue * 4 + kStash * 8) <= kListCap * 8, "queues and stashes take the place of the list");
+template <int DT, int U> __device__ __forceinline__ void spread_strip(const RowsParams &P, RowPlan *plan, int row, int strip, float zlo, float zhi, int bid, bool weigh) {
     constexpr int EPV = Elt<DT>::kPerVec;
-    __shared__ float queues[kRowWarps][kQueue];
-    __shared__ u64 stashes[kRowWarps][kStash];
-    __shared__ double tab[16];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int rows = __ldcg(P.todo);
-    if (rows == 0) return;
-    exp2_table_init(tab, threadIdx.x);
-    __syncthreads();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float *queue = queues[warp];
-    u64 *stash = stashes[warp];
-    const long long tasks = static_cast<long long>(rows) * P.nstrip;
+    u64 *stash = list() + warp * kStash;
+    float *queue = reinterpret_cast<float *>(list() + kPickWarps * kStash) + warp * kQueue;
+    const float gm = load_group<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32 + strip * 32 + lane);
+    const int nvec = S.nvec, v0 = strip * (32 * U) + lane;
+    const bool want = gm >= fminf(zhi, zlo);
+    double acc = 0.0;
+    int queued = 0, stashed = 0, count = 0;
+    auto flush = [&]() {                                           // the stash to the row's list
+        __syncwarp();
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&plan->listed, stashed);
+        at = __shfl_sync(0xffffffffu, at, 0);
+        for (int i = lane; i < stashed; i += 32)
+            if (at + i < P.listcap) __stcg(P.lists + static_cast<size_t>(row) * P.listcap + at + i, stash[i]);
+        stashed = 0;
+        __syncwarp();
+    };
+    if (__any_sync(0xffffffffu, want)) {
+        uint4 raw[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) raw[q] = state_vector<DT>(want ? v0 + q * 32 : nvec);
 #pragma unroll 1
-    for (long long task = static_cast<long long>(blockIdx.x) * kRowWarps + warp; task < tasks; task += static_cast<long long>(gridDim.x) * kRowWarps) {
-        const int row = __ldcg(P.todo + 1 + static_cast<int>(task / P.nstrip)), strip = static_cast<int>(task % P.nstrip), b = row / P.R;
-        RowPlan *plan = P.plan + row;
-        const float gm = load_group<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32 + strip * 32 + lane);
-        const float zlo = __ldcg(&plan->zlo), zhi = __ldcg(&plan->zhi), m = __ldcg(&plan->m);
-        const int bid = __ldcg(&plan->bid);
-        const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
-        const int nvec = rv.nvec(), v0 = strip * (32 * U) + lane;
-        const bool want = gm >= fminf(zhi, zlo);
-        double acc = 0.0;
-        int queued = 0, stashed = 0, count = 0;
-        auto flush = [&]() {                                       // the stash to the row's list
-            __syncwarp();
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&plan->listed, stashed);
-            at = __shfl_sync(0xffffffffu, at, 0);
-            for (int i = lane; i < stashed; i += 32)
-                if (at + i < P.listcap) __stcg(P.lists + static_cast<size_t>(row) * P.listcap + at + i, stash[i]);
-            stashed = 0;
-            __syncwarp();
-        };
-        if (__any_sync(0xffffffffu, want)) {
-            const Weights w(m, __ldg(P.tau + b), tab);
-            const bool weigh = P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f);
-            uint4 raw[U];
+        for (int q = 0; q < U; ++q) {
+            const uint4 r = raw[0];
 #pragma unroll
-            for (int q = 0; q < U; ++q) raw[q] = row_vector<DT>(rv, P.mask, want ? v0 + q * 32 : nvec, nvec);
-#pragma unroll 1
-            for (int q = 0; q < U; ++q) {
-                const uint4 r = raw[0];
+            for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
+            float z[EPV];
+            unpack<DT>(r, z);
+            const int e0 = (v0 + q * 32) * EPV - S.head;
+            unsigned near = 0;
 #pragma unroll
-                for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
-                float z[EPV];
-                unpack<DT>(r, z);
-                const int e0 = rv.first_elem(v0 + q * 32);
-                unsigned near = 0;
-#pragma unroll
-                for (int i = 0; i < EPV; ++i) {
-                    const bool kept = z[i] > zhi || (z[i] == zhi && e0 + i <= bid);
-                    const unsigned who = __ballot_sync(0xffffffffu, kept);
-                    if (kept) queue[queued + __popc(who & ((1u << lane) - 1u))] = z[i];
-                    queued += __popc(who);
-                    near |= static_cast<unsigned>(!kept && z[i] >= zlo) << i;
-                }
-                while (__any_sync(0xffffffffu, near != 0)) {       // one of each lane at a time
-                    if (stashed > kStash - 32) flush();
-                    const unsigned who = __ballot_sync(0xffffffffu, near != 0);
-                    if (near) {
-                        const int i = __ffs(near) - 1;
-                        stash[stashed + __popc(who & ((1u << lane) - 1u))] = element_of<DT>(vector_element<DT>(r, i), e0 + i);
-                        near &= near - 1;
-                    }
-                    stashed += __popc(who);
-                }
-                __syncwarp();
-                while (queued >= 32) {
-                    queued -= 32; count += 32;
-                    if (weigh) acc += w(queue[queued + lane]);
-                }
-                __syncwarp();
+            for (int i = 0; i < EPV; ++i) {
+                const bool kept = z[i] > zhi || (z[i] == zhi && e0 + i <= bid);
+                const unsigned who = __ballot_sync(0xffffffffu, kept);
+                if (kept) queue[queued + __popc(who & ((1u << lane) - 1u))] = z[i];
+                queued += __popc(who);
+                near |= static_cast<unsigned>(!kept && z[i] >= zlo) << i;
             }
-            count += queued;
-            if (weigh && lane < queued) acc += w(queue[lane]);
-            if (stashed) flush();
+            while (__any_sync(0xffffffffu, near != 0)) {           // one of each lane at a time
+                if (stashed > kStash - 32) flush();
+                const unsigned who = __ballot_sync(0xffffffffu, near != 0);
+                if (near) {
+                    const int i = __ffs(near) - 1;
+                    stash[stashed + __popc(who & ((1u << lane) - 1u))] = element_of<DT>(vector_element<DT>(r, i), e0 + i);
+                    near &= near - 1;
+                }
+                stashed += __popc(who);
+            }
+            __syncwarp();
+            while (queued >= 32) {
+                queued -= 32; count += 32;
+                if (weigh) acc += S.w(queue[queued + lane]);
+            }
             __syncwarp();
         }
-        acc = warp_sum(acc);
-        if (lane == 0) {
-            StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
-            __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
-        }
+        count += queued;
+        if (weigh && lane < queued) acc += S.w(queue[lane]);
+        if (stashed) flush();
+        __syncwarp();
+    }
+    acc = warp_sum(acc);
+    if (lane == 0) {
+        StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
+        __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
     }
 }
 
@@ -1331,16 +1312,14 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
                 __syncthreads();
 #pragma unroll 1
                 for (int i = tid; i < n; i += kPickThreads)
-                    if (list()[i] >= at.edge) atomicAdd(extra + ((element_id(list()[i]) + S.head) / EPV >> (5 + S.ulog)), masses()[i]);
+                    if (list()[i] >= at.edge) atomicAdd(extra + ((element_id(list()[i]) + S.head) / EPV >> (5 + S.ulog)), mass_of<DT>(list()[i], at.unit));
                 __syncthreads();
 #pragma unroll 1
                 for (int i = tid; i < P.nstrip; i += kPickThreads) strips()[i] += static_cast<double>(extra[i]) / at.unit;
             }
         } else {                                                   // bad luck, or min-p above the bracket: the long way
-            const float tmax = load_groups<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32);
-            __syncthreads();
             const Hint hint = {zlo, zhi, above, mass};
-            border = border_by_digits<DT>(ask, zmin, Z, tmax, hint);
+            border = border_by_digits<DT>(ask, zmin, Z, hint);
             if (P.sample) {
                 __syncthreads();
 #pragma unroll 1
@@ -1364,23 +1343,41 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
     finish_row(P, row, 0, BORDER_APPLY, border, d.token, d.prob);
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kPickThreads) tli_rows_settle_kernel(const __grid_constant__ RowsParams P) {
+// The rows that the pick kernel left, by all blocks: each takes eight strips at a time (the next ones when it is done: the block
+// that ends last with a row settles it, which takes as long as several strips).
+template <int DT, int U>
+__global__ void __launch_bounds__(kPickThreads, 3) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
+    const int tid = threadIdx.x;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = __ldcg(P.todo);
     if (rows == 0) return;
-    exp2_table_init(S.tab, threadIdx.x);
-#pragma unroll 1
-    for (int i = blockIdx.x; i < rows; i += gridDim.x) {
-        const int row = __ldcg(P.todo + 1 + i), b = row / P.R;
-        RowPlan *plan = P.plan + row;
+    const int nchunk = (P.nstrip + kPickWarps - 1) / kPickWarps;
+    exp2_table_init(S.tab, tid);
+    int *next = P.todo + 1 + P.B * P.R;
+    for (;;) {
         __syncthreads();                                           // the shared memory is free again
-        if (threadIdx.x == 0) {
+        if (tid == 0) S.listed = atomicAdd(next, 1);
+        __syncthreads();
+        const int task = S.listed;
+        if (task >= rows * nchunk) return;
+        const int row = __ldcg(P.todo + 1 + task / nchunk), b = row / P.R;
+        RowPlan *plan = P.plan + row;
+        const float zlo = __ldcg(&plan->zlo), zhi = __ldcg(&plan->zhi);
+        const int bid = __ldcg(&plan->bid);
+        if (tid == 0) {
             S.m = __ldcg(&plan->m);
             S.w = Weights(S.m, __ldg(P.tau + b), S.tab);
         }
-        enter_row<DT>(P, row, b);
+        enter_row<DT>(P, row, b, kListCap);
         __syncthreads();
+        const int strip = task % nchunk * kPickWarps + (tid >> 5);
+        if (strip < P.nstrip) spread_strip<DT, U>(P, plan, row, strip, zlo, zhi, bid, P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f));
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) S.listed = atomicAdd(&plan->done, 1);
+        __syncthreads();
+        if (S.listed != nchunk - 1) continue;
+        __threadfence();
         settle_row<DT>(P, plan, row, b);
     }
 }
@@ -1477,7 +1474,7 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.ssum = off; off = align_up(off + sizeof(StripSum) * rows * L.nstrip, 256);
     L.border = off; off = align_up(off + sizeof(RowBorder) * rows, 256);
     L.plan = off; off = align_up(off + sizeof(RowPlan) * rows, 256);
-    L.todo = off; off = align_up(off + sizeof(int) * (rows + 1), 256);
+    L.todo = off; off = align_up(off + sizeof(int) * (rows + 2), 256);
     // bracketed elements of a row: a sample of 16384 puts the border within about V/64 of them
     L.listcap = V <= kListCap ? 0 : std::min(kListCap, std::max(2048, V / 32));
     L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
@@ -1516,22 +1513,20 @@ template <int DT, int U> int launch_rows(const RowsParams &P, int device, int nu
     cudaError_t e = cudaLaunchKernelEx(&cfg, tli_rows_scan_kernel<DT, U>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_scan_kernel");
     const size_t smem = pick_smem_bytes(P.nstrip, (P.nstrip + P.coarse - 1) / P.coarse * 32);
-    static SmemAllowed allowed, allowed_settle;
+    static SmemAllowed allowed, allowed_spread;
     e = allowed.set(reinterpret_cast<const void *>(tli_rows_pick_kernel<DT>), kPickSmemMax, device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
     cfg.gridDim = dim3(rows); cfg.blockDim = dim3(kPickThreads); cfg.dynamicSmemBytes = smem;
     e = cudaLaunchKernelEx(&cfg, tli_rows_pick_kernel<DT>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_pick_kernel");
     if (P.listcap > 0 && (P.top_k || P.top_p || P.min_p)) {        // (short rows and unfiltered ones are done)
-        e = allowed_settle.set(reinterpret_cast<const void *>(tli_rows_settle_kernel<DT>), kPickSmemMax, device);
+        e = allowed_spread.set(reinterpret_cast<const void *>(tli_rows_spread_kernel<DT, U>), kSettleSmemMax, device);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
-        const long long blocks = (static_cast<long long>(rows) * P.nstrip + kRowWarps - 1) / kRowWarps;
-        cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(blocks, 4LL * num_sms))); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = 0;
+        const long long blocks = static_cast<long long>(rows) * ((P.nstrip + kPickWarps - 1) / kPickWarps);
+        cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(blocks, 3LL * num_sms))); cfg.blockDim = dim3(kPickThreads);
+        cfg.dynamicSmemBytes = settle_smem_bytes(P.nstrip);
         e = cudaLaunchKernelEx(&cfg, tli_rows_spread_kernel<DT, U>, P);
         if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_spread_kernel");
-        cfg.gridDim = dim3(std::min<unsigned>(rows, 2u * num_sms)); cfg.blockDim = dim3(kPickThreads); cfg.dynamicSmemBytes = smem;
-        e = cudaLaunchKernelEx(&cfg, tli_rows_settle_kernel<DT>, P);
-        if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_settle_kernel");
     }
     if (!P.sample) {
         cfg.gridDim = dim3((P.nstrip + kRowWarps - 1) / kRowWarps, rows); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = 0;
