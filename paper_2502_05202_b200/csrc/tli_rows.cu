@@ -21,7 +21,7 @@
 //
 // Weights and sums are fp64: the ids that come out are exact decisions (which id owns v * total, which one is
 // the last inside top-p), and with 10^5 candidates an fp32 sum (2^-24 relative) would decide some of them by
-// rounding.  An fp64 weight costs 13 fp64 operations; one pass over a row is then bound by the fp64 pipe only
+// rounding.  An fp64 weight costs 12 fp64 operations; one pass over a row is then bound by the fp64 pipe only
 // for 16-bit rows that need the whole mass.
 
 #include <cuda_bf16.h>
@@ -30,7 +30,7 @@
 
 namespace {
 
-constexpr int kRowThreads = 256;                     // scan and mask kernels
+constexpr int kRowThreads = 128;                     // scan and mask kernels
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kPickThreads = 256;                    // pick and spread kernels
 constexpr int kPickWarps = kPickThreads / 32;
@@ -63,23 +63,34 @@ struct RowsParams {
 
 // ---- weights ----
 
-// 2^(i/16); 16 doubles are one word line, so 32 lanes with any indices read it without a bank conflict
+// 2^(i/16), less i/16 in the exponent field (see exp2_parts); 16 doubles are one line of banks, so 32 lanes with any indices
+// read it without a conflict
 __device__ __forceinline__ void exp2_table_init(double *tab, int tid) {
-    if (tid < 16) tab[tid] = exp2(tid / 16.0);
+    if (tid < 16) {
+        const double t = exp2(tid / 16.0);
+        tab[tid] = __hiloint2double(__double2hiint(t) - (tid << 16), __double2loint(t));
+    }
 }
-// 2^x for x in [-1021, 0]: x = n + i/16 + r, |r| <= 1/32, Taylor in r ln 2 to the sixth power
-// (next term (ln2/32)^7/7! = 4e-16).
-__device__ __forceinline__ double exp2_neg(double x, const double *tab) {
+// 2^x for x in [-1021, 0] as a product q * t: x = n/16 + r, |r| <= 1/32; q = 2^r by its Taylor series in r ln 2 to the fifth power
+// (next term (ln2/32)^6/6! = 1.4e-13), t = 2^(n/16) = tab[n mod 16] with n/16 added to the exponent field (the table's entry lacks
+// what the low four bits of n would add).  On this part an fp64 instruction holds the issue port for two cycles: the 12 of a
+// weight and five others are what bounds a pass that weighs a whole row.
+__device__ __forceinline__ void exp2_parts(double x, const double *tab, double &q, double &t) {
     constexpr double L = 0.693147180559945309417232;
-    constexpr double c2 = L * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5, c6 = c5 * L / 6;
+    constexpr double c2 = L * L / 2, c3 = c2 * L / 3, c4 = c3 * L / 4, c5 = c4 * L / 5;
     constexpr double magic = 6755399441055744.0;                     // 1.5 * 2^52
-    const double t = fma(x, 16.0, magic);
-    const double r = fma(t - magic, -0.0625, x);
-    const int n = __double2loint(t);
-    double q = fma(r, c6, c5);
-    q = fma(q, r, c4); q = fma(q, r, c3); q = fma(q, r, c2); q = fma(q, r, L); q = fma(q, r, 1.0);
-    q *= tab[n & 15];
-    return __hiloint2double(__double2hiint(q) + ((n >> 4) << 20), __double2loint(q));
+    const double k = fma(x, 16.0, magic);
+    const double r = fma(k - magic, -0.0625, x);
+    const int n = __double2loint(k);
+    t = tab[n & 15];
+    t = __hiloint2double(__double2hiint(t) + (n << 16), __double2loint(t));
+    q = fma(r, c5, c4);
+    q = fma(q, r, c3); q = fma(q, r, c2); q = fma(q, r, L); q = fma(q, r, 1.0);
+}
+__device__ __forceinline__ double exp2_neg(double x, const double *tab) {
+    double q, t;
+    exp2_parts(x, tab, q, t);
+    return q * t;
 }
 __device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }     // of a normal number
 __device__ __forceinline__ double two_to(int n) { return __hiloint2double((n + 1023) << 20, 0); }
@@ -94,6 +105,13 @@ struct Weights {
     __device__ __forceinline__ double operator()(float z) const {
         const double w = exp2_neg((static_cast<double>(z) - m) * s, tab);
         return z >= cut ? w : 0.0;
+    }
+    // acc + w(z), where w(z) is 0 + w(cut): for sums that hold a weight of 1, if w(cut) is nothing beside it
+    __device__ __forceinline__ bool cut_is_nothing() const { return (m - static_cast<double>(cut)) * s > 200.0; }
+    __device__ __forceinline__ double add(double acc, float z) const {
+        double q, t;
+        exp2_parts((static_cast<double>(fmaxf(z, cut)) - m) * s, tab, q, t);
+        return fma(q, t, acc);
     }
 };
 
@@ -233,16 +251,24 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const __grid
     double acc = 0.0;
     if (ms > -INFINITY && ms < INFINITY) {                         // NaN: not compared, the row is flagged later
         const Weights w(ms, ask.tau, tab);
-        // (unrolled the code would not fit the instruction cache)
+        if (w.cut_is_nothing()) {
+#pragma unroll
+            for (int q = 0; q < U; ++q) {
+                float z[Elt<DT>::kPerVec];
+                unpack<DT>(raw[q], z);
+#pragma unroll
+                for (int i = 0; i < Elt<DT>::kPerVec; ++i) acc = w.add(acc, z[i]);
+            }
+        } else {                                                   // tau below a step of the largest logit, or logits near the lowest value
 #pragma unroll 1
-        for (int q = 0; q < U; ++q) {
-            uint4 r = raw[0];
+            for (int q = 0; q < U; ++q) {
+                float z[Elt<DT>::kPerVec];
+                unpack<DT>(raw[0], z);
 #pragma unroll
-            for (int k = 1; k < U; ++k) if (k == q) r = raw[k];
-            float z[Elt<DT>::kPerVec];
-            unpack<DT>(r, z);
+                for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
 #pragma unroll
-            for (int i = 0; i < Elt<DT>::kPerVec; ++i) acc += w(z[i]);
+                for (int i = 0; i < Elt<DT>::kPerVec; ++i) acc += w(z[i]);
+            }
         }
     }
     acc = warp_sum(acc);
@@ -1198,7 +1224,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
 // ---- rows whose kept set has thousands of elements ----
 
 // One strip of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed; what lies from there down to
-// zlo goes to the row's list.  Weights cost 13 fp64 operations whether one lane of a warp wants them or 32, so the kept
+// zlo goes to the row's list.  A weight costs 12 fp64 operations whether one lane of a warp wants them or 32, so the kept
 // logits are queued per warp and weighed 32 at a time.
 constexpr int kQueue = 32 * 9, kStash = 96;              // 31 and a vector of each lane; 64 and one element of each lane
 static_assert(kPickWarps * (kQueue * 4 + kStash * 8) <= kListCap * 8, "queues and stashes take the place of the list");

@@ -732,6 +732,15 @@ def tli_selftest_bounded_wait(ctx: int, polls: int = 2000, stream: Optional[int]
     return out.value == 1
 
 
+def _current_device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _raw_stream(index: int) -> int:
+    """The current stream of a device as an int, without an object for it."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
 class Verifier:
     """Convenience owner of one context plus its scratch and output tensors."""
 
@@ -742,6 +751,7 @@ class Verifier:
         if tiled:
             tli_set_tiled(self.ctx, True)
         self._ws: Optional[torch.Tensor] = None
+        self._index, self._lib, self._plans = int(device), load(), {}
 
     def close(self) -> None:
         if self.ctx:
@@ -779,63 +789,141 @@ class Verifier:
         tli_draft_sample(self.ctx, args)
         return out
 
-    def _scratch(self, need: int, where: str) -> torch.Tensor:
-        """Scratch of one call that may overlap others on this context: its own, not the shared one."""
-        if need == 0:
-            raise TLIError(TLI_ERR_UNSUPPORTED, where)
-        return torch.empty(need, dtype=torch.uint8, device=self.device)
+    # The calls below may overlap others on this context, so each has scratch of its own, from torch's allocator on the
+    # current stream (which also serves a capture).  What depends on shapes alone is worked out once per shape.
+
+    def _plan(self, kind: str, key, make):
+        plan = self._plans.get((kind, key))
+        if plan is None:
+            if len(self._plans) > 1000:
+                self._plans.clear()
+            plan = self._plans[(kind, key)] = make()
+        return plan
+
+    def _call(self, name: str, args) -> None:
+        fn = getattr(self._lib, name)
+        if _current_device() == self._index:
+            rc = fn(self.ctx, ctypes.byref(args), _raw_stream(self._index))
+        else:
+            with torch.cuda.device(self._index):
+                rc = fn(self.ctx, ctypes.byref(args), _raw_stream(self._index))
+        if rc != TLI_OK:
+            raise TLIError(rc, name)
+
+    def _row_plan(self, logits, side):
+        """(B, R, shape of a per-sequence tensor, shape of a per-row one, scratch bytes, filled argument structs)."""
+        B, R, _ = logits.shape
+        dt = _logit_dtype(logits)
+        _check_rows(self.ctx, logits, side, ())
+        need = tli_sample_workspace_bytes(self.ctx, B, R, dt, side)
+        if need == 0 or tli_filter_workspace_bytes(self.ctx, B, R, dt, side) != need:
+            raise TLIError(TLI_ERR_UNSUPPORTED, "tli_sample_workspace_bytes")
+        sb, sr, _ = logits.stride()
+        sample = tli_sample_args(B=B, R=R, dtype=dt, side=side, stride_b=sb, stride_r=sr, workspace_bytes=need)
+        filt = tli_filter_args(B=B, R=R, dtype=dt, side=side, stride_b=sb, stride_r=sr, workspace_bytes=need)
+        return B, R, (B,), (B, R), need, bytes(sample), bytes(filt)
+
+    def _rows(self, logits, side, temperature, top_k, top_p, min_p):
+        if logits.dim() != 3:
+            raise ValueError("logits must be [B, R, V]")
+        plan = self._plan("rows", (logits.shape, logits.stride(), logits.dtype, side), lambda: self._row_plan(logits, side))
+        on = self._index
+        if logits.get_device() != on:
+            raise ValueError("logits must be on %s" % self.device)
+        shape = plan[2]
+        for t, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
+            if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != on or not t.is_contiguous()):
+                raise ValueError("temperature, top_k, top_p and min_p must be contiguous float32, int32, float32 and float32 "
+                                 "tensors of shape %s on %s" % (shape, self.device))
+        return plan
 
     def sample(self, logits, temperature, uniforms, side: int = TLI_SIDE_TARGET, top_k=None, top_p=None,
                min_p=None) -> Dict[str, torch.Tensor]:
         """Draw one id per row of ``logits`` [B,R,V] under temperature, top-k, top-p and min-p (per sequence,
         ``None`` = off); on the drafter side from the ids inside the intersection.  Returns device tensors."""
-        B, R = logits.shape[0], logits.shape[1]
+        _, _, _, shape, need, template, _ = self._rows(logits, side, temperature, top_k, top_p, min_p)
+        if uniforms.dtype is not torch.float32 or uniforms.shape != shape or uniforms.get_device() != self._index or not uniforms.is_contiguous():
+            raise ValueError("uniforms must be a contiguous float32 tensor of shape %s on %s" % (shape, self.device))
         dev = self.device
-        out = {"tokens": torch.empty(B, R, dtype=torch.int32, device=dev),
-               "prob": torch.empty(B, R, dtype=torch.float32, device=dev),
-               "status": torch.empty(B, R, dtype=torch.int32, device=dev)}
-        ws = self._scratch(tli_sample_workspace_bytes(self.ctx, B, R, _logit_dtype(logits), side), "tli_sample_workspace_bytes")
-        args = make_sample_args(self.ctx, logits, temperature, uniforms, out["tokens"], ws, side, top_k, top_p, min_p,
-                                out["prob"], out["status"])
-        tli_sample(self.ctx, args, torch.cuda.current_stream(dev).cuda_stream)
-        return out
+        tokens = torch.empty(shape, dtype=torch.int32, device=dev)
+        prob = torch.empty(shape, dtype=torch.float32, device=dev)
+        status = torch.empty(shape, dtype=torch.int32, device=dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        a = tli_sample_args.from_buffer_copy(template)
+        a.logits = logits.data_ptr()
+        a.temperature = temperature.data_ptr()
+        a.top_k = None if top_k is None else top_k.data_ptr()
+        a.top_p = None if top_p is None else top_p.data_ptr()
+        a.min_p = None if min_p is None else min_p.data_ptr()
+        a.uniforms = uniforms.data_ptr()
+        a.tokens, a.prob, a.status, a.workspace = tokens.data_ptr(), prob.data_ptr(), status.data_ptr(), ws.data_ptr()
+        self._call("tli_sample", a)
+        return {"tokens": tokens, "prob": prob, "status": status}
 
     def filter(self, logits, temperature, side: int = TLI_SIDE_TARGET, top_k=None, top_p=None, min_p=None,
                out=None) -> Dict[str, torch.Tensor]:
         """The rows of ``logits`` [B,R,V] with -inf outside the kept set (``out=logits``: in place)."""
-        B, R = logits.shape[0], logits.shape[1]
+        _, _, _, shape, need, _, template = self._rows(logits, side, temperature, top_k, top_p, min_p)
+        dev = self.device
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
-        status = torch.empty(B, R, dtype=torch.int32, device=self.device)
-        ws = self._scratch(tli_filter_workspace_bytes(self.ctx, B, R, _logit_dtype(logits), side), "tli_filter_workspace_bytes")
-        args = make_filter_args(self.ctx, logits, temperature, out, ws, side, top_k, top_p, min_p, status)
-        tli_filter(self.ctx, args, torch.cuda.current_stream(self.device).cuda_stream)
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+        elif out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index or (out.shape[2] > 1 and out.stride(2) != 1):
+            raise ValueError("out must have the logits' type, shape and device, and a contiguous vocabulary axis")
+        status = torch.empty(shape, dtype=torch.int32, device=dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        a = tli_filter_args.from_buffer_copy(template)
+        a.logits = logits.data_ptr()
+        a.temperature = temperature.data_ptr()
+        a.top_k = None if top_k is None else top_k.data_ptr()
+        a.top_p = None if top_p is None else top_p.data_ptr()
+        a.min_p = None if min_p is None else min_p.data_ptr()
+        a.out, a.status, a.workspace = out.data_ptr(), status.data_ptr(), ws.data_ptr()
+        a.out_stride_b, a.out_stride_r, _ = out.stride()
+        self._call("tli_filter", a)
         return {"logits": out, "status": status}
+
+    def _table_rows(self, side: int) -> int:
+        if side not in (TLI_SIDE_TARGET, TLI_SIDE_DRAFTER):
+            raise ValueError("a side must be TLI_SIDE_TARGET or TLI_SIDE_DRAFTER")
+        return self.V_t if side == TLI_SIDE_TARGET else self.V_d
+
+    def _ids(self, ids) -> None:
+        if ids.dtype is not torch.int32 or ids.get_device() != self._index or not ids.is_contiguous():
+            raise ValueError("ids must be a contiguous int32 tensor on %s" % self.device)
 
     def embed(self, ids, table, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET,
               table_side: int = TLI_SIDE_TARGET) -> Dict[str, torch.Tensor]:
         """Rows of ``table`` [V,H] for ``ids`` (any shape) of either vocabulary, times ``scale``, and the ids in
         the table's vocabulary (-1, with a zero row, where there is none)."""
-        V = self.V_t if table_side == TLI_SIDE_TARGET else self.V_d
-        if table.dim() != 2 or table.shape[0] != V:
-            raise ValueError("table must be [%d, H]" % V)
-        rows = torch.empty(*ids.shape, table.shape[1], dtype=table.dtype, device=self.device)
-        table_ids = torch.empty(ids.shape, dtype=torch.int32, device=self.device)
-        args = make_embed_args(ids, table, rows.view(ids.numel(), table.shape[1]), scale, ids_side, table_side, table_ids)
-        tli_embed(self.ctx, args, torch.cuda.current_stream(self.device).cuda_stream)
+        self._ids(ids)
+        V, dev = self._table_rows(table_side), self.device
+        if table.dim() != 2 or table.shape[0] != V or table.get_device() != self._index:
+            raise ValueError("table must be [%d, H] on %s" % (V, dev))
+        stride, H = _matrix("table", table), table.shape[1]
+        rows = torch.empty((*ids.shape, H), dtype=table.dtype, device=dev)
+        table_ids = torch.empty(ids.shape, dtype=torch.int32, device=dev)
+        self._call("tli_embed", tli_embed_args(ids.numel(), H, _logit_dtype(table), ids_side, table_side, ids.data_ptr(), table.data_ptr(),
+                                               stride, scale, rows.data_ptr(), H, table_ids.data_ptr()))
         return {"rows": rows, "table_ids": table_ids}
 
     def embed_grad(self, ids, grad, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET,
                    dtype: Optional[torch.dtype] = None) -> Dict[str, torch.Tensor]:
         """Gradient of :meth:`embed` with respect to the table, [V,H] in ``dtype`` (default: the type of ``grad``)."""
-        N, H, dev = ids.numel(), grad.shape[-1], self.device
-        if tuple(grad.shape) != tuple(ids.shape) + (H,):
-            raise ValueError("grad must have the shape of ids, and H")
-        V = self.V_t if table_side == TLI_SIDE_TARGET else self.V_d
-        out = torch.empty(V, H, dtype=dtype or grad.dtype, device=dev)
-        ws = self._scratch(tli_embed_grad_workspace_bytes(self.ctx, N, H), "tli_embed_grad_workspace_bytes")
-        args = make_embed_grad_args(ids, grad if grad.dim() == 2 else grad.reshape(N, H), out, ws, scale, ids_side, table_side)
-        tli_embed_grad(self.ctx, args, torch.cuda.current_stream(dev).cuda_stream)
+        self._ids(ids)
+        N, V, dev = ids.numel(), self._table_rows(table_side), self.device
+        H = grad.shape[-1]
+        if grad.shape != (*ids.shape, H) or grad.get_device() != self._index:
+            raise ValueError("grad must have the shape of ids, and H, on %s" % dev)
+        if grad.dim() != 2:
+            grad = grad.reshape(N, H)
+        stride = _matrix("grad", grad)
+        out = torch.empty((V, H), dtype=dtype or grad.dtype, device=dev)
+        need = self._plan("grad", (N, H), lambda: tli_embed_grad_workspace_bytes(self.ctx, N, H))
+        if need == 0:
+            raise TLIError(TLI_ERR_UNSUPPORTED, "tli_embed_grad_workspace_bytes")
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._call("tli_embed_grad", tli_embed_grad_args(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
+                                                         grad.data_ptr(), stride, scale, out.data_ptr(), H, ws.data_ptr(), need))
         return {"grad": out}
 
     def rates(self, target_logits, drafter_logits, temperature) -> Dict[str, torch.Tensor]:
