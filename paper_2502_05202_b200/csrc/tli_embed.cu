@@ -7,8 +7,8 @@
 //   gradient               dW[v] = scale * sum over the tokens i with t(ids[i]) = v of g[i], every row written.
 //       tli_grad_sort_kernel     tokens by (table id, position), least significant digit first, two digits of ten bits,
 //                                stable, so that every sum below has one order whatever the timing; the other CTAs of
-//                                the same grid fill dW with zeros meanwhile (the dense write is the floor).
-//       tli_grad_count_kernel, tli_grad_scatter_kernel   the same sort over several CTAs for many tokens.
+//                                the same grid fill dW with zeros meanwhile (the dense write is the floor); one cluster of eight.
+//       tli_grad_count_kernel, tli_grad_scatter_kernel   the same sort over more CTAs for many tokens.
 //       tli_grad_sum_kernel      a window of sorted tokens per group of threads: rows whose tokens all lie in the
 //                                window are written, the pieces of a row that crosses a window go to the workspace.
 //       tli_grad_join_kernel     adds the pieces of such a row in window order.
@@ -20,7 +20,9 @@ constexpr int kEmbThreads = 256;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 1024;
+constexpr int kSortCluster = 8;
 constexpr int kSumThreads = 128;
+constexpr int kSumMinTx = 4;               // threads across a row at least (32 windows of 2 KB of keys and positions in a block)
 
 // table id of a token, -1 if it has none
 __device__ __forceinline__ int table_id(const int *map, int n_ids, int id) {
@@ -68,7 +70,7 @@ constexpr int kEmbUnroll = 4;
 
 // VEC: rows of both sides lie on 16-byte boundaries and H is a whole number of vectors; otherwise element by element
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kEmbThreads) tli_embed_kernel(const EmbedParams P) {
+__global__ void __launch_bounds__(kEmbThreads) tli_embed_kernel(const __grid_constant__ EmbedParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const long long task = static_cast<long long>(blockIdx.x) * (kEmbThreads / 32) + (threadIdx.x >> 5);
     const int i = static_cast<int>(task / P.chunks), chunk = static_cast<int>(task % P.chunks), lane = threadIdx.x & 31;
@@ -99,7 +101,7 @@ __global__ void __launch_bounds__(kEmbThreads) tli_embed_kernel(const EmbedParam
 }
 
 struct GradParams {
-    int N, H, n_ids, V, groups, tile;      // groups: CTAs of the sort; tile: tokens of one of them
+    int N, H, n_ids, V, groups, tile, clustered;      // groups: CTAs of the sort (one cluster or not); tile: tokens of one of them
     int window, nwin, tx;                  // sorted tokens per window; threads across a row
     const int *map, *ids;
     const void *g; long long gs;
@@ -112,7 +114,7 @@ struct GradParams {
 };
 
 // One digit of the sort for tokens [first, last) of the source, by one CTA.  pass 0 takes the ids, pass 1 what
-// pass 0 left.  `before` [kDigits] in shared memory: where the digit's tokens of this CTA begin.
+// pass 0 left.
 struct SortShared { int wsum[kSortWarps]; };
 
 __device__ __forceinline__ int sort_key(const GradParams &P, int pass, int i, int &pos) {
@@ -143,60 +145,91 @@ __device__ __forceinline__ int sort_scan(int x, SortShared &sh, int &total) {   
     return x + before;
 }
 
-__device__ void sort_digit(const GradParams &P, int pass, int cta, int n, int *cnt, SortShared &sh) {
+// the lanes of the warp that hold the same digit (-1 for none), by a ballot per bit: __match_any_sync takes a step per distinct value
+__device__ __forceinline__ unsigned same_digit(int d) {
+    unsigned peers = __ballot_sync(0xffffffffu, d >= 0);
+#pragma unroll
+    for (int b = 0; b < 10; ++b) {
+        const bool bit = d >> b & 1;
+        const unsigned with = __ballot_sync(0xffffffffu, bit);
+        peers &= bit ? with : ~with;
+    }
+    return peers;
+}
+// cnt: [warps][kDigits] counters and [kDigits] first places.  A warp has eight tokens per lane on their way at a time: one at a time,
+// a digit of 16 384 tokens takes 16 trips to L2 and back in a row.
+constexpr int kSortBatch = 8;
+template <bool CLUSTER> __device__ __forceinline__ int sort_digit(const GradParams &P, int pass, int cta, int n, int *cnt, SortShared &sh) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int first = min(n, cta * P.tile), last = min(n, first + P.tile);
     const int chunk = ((last - first + kSortWarps - 1) / kSortWarps + 31) & ~31;     // a warp's tokens, in order
     const int w0 = min(last, first + warp * chunk), w1 = min(last, w0 + chunk);
-    for (int i = tid; i < kSortWarps * kDigits; i += kSortThreads) cnt[i] = 0;
+    const int warps = chunk ? (last - first + chunk - 1) / chunk : 0;                // that have any
+    int *base = cnt + kSortWarps * kDigits, *mine = cnt + warp * kDigits;
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) cnt[w * kDigits + tid] = 0;
     __syncthreads();
-    int *mine = cnt + warp * kDigits;
-    for (int i = w0 + lane; i < w1; i += 32) {
-        int pos;
-        const int key = sort_key(P, pass, i, pos);
-        if (key >= 0) atomicAdd(mine + digit_of(pass, key), 1);
+#pragma unroll 1
+    for (int i0 = w0 + lane; i0 < w1; i0 += 32 * kSortBatch) {
+        int key[kSortBatch], pos;
+#pragma unroll
+        for (int j = 0; j < kSortBatch; ++j) key[j] = i0 + j * 32 < w1 ? sort_key(P, pass, i0 + j * 32, pos) : -1;
+#pragma unroll
+        for (int j = 0; j < kSortBatch; ++j)
+            if (key[j] >= 0) atomicAdd(mine + digit_of(pass, key[j]), 1);
     }
     __syncthreads();
     // thread d: digit d
     int sum = 0, others = 0, all = 0;
-    for (int w = 0; w < kSortWarps; ++w) {
+#pragma unroll 8
+    for (int w = 0; w < warps; ++w) {
         const int c = cnt[w * kDigits + tid];
         cnt[w * kDigits + tid] = sum;
         sum += c;
     }
-    if (P.groups > 1) {
-        for (int c = 0; c < P.groups; ++c) {
-            const int x = __ldcg(P.count + c * kDigits + tid);
-            if (c < cta) others += x;
-            all += x;
-        }
-    } else {
-        all = sum;
+    if (CLUSTER) {
+        __stcg(P.count + cta * kDigits + tid, sum);
+        cluster_barrier();
+    }
+#pragma unroll 8
+    for (int c = 0; c < P.groups; ++c) {
+        const int x = __ldcg(P.count + c * kDigits + tid);
+        if (c < cta) others += x;
+        all += x;
     }
     int total;
-    const int base = sort_scan(all, sh, total) - all + others;
+    base[tid] = sort_scan(all, sh, total) - all + others;
     if (pass == 0 && cta == 0 && tid == 0) *P.n_valid = total;
-    for (int w = 0; w < kSortWarps; ++w) cnt[w * kDigits + tid] += base;
     __syncthreads();
-    for (int i0 = w0; i0 < w1; i0 += 32) {
-        const int i = i0 + lane;
-        int pos = 0;
-        const int key = i < w1 ? sort_key(P, pass, i, pos) : -1;
-        const int d = key >= 0 ? digit_of(pass, key) : -1;
-        const unsigned peers = __match_any_sync(0xffffffffu, d);
-        const int rank = __popc(peers & ((1u << lane) - 1u));
-        int at = 0;
-        if (d >= 0) at = mine[d] + rank;
-        __syncwarp();
-        if (d >= 0 && rank == 0) mine[d] += __popc(peers);
-        __syncwarp();
-        if (d >= 0) {
-            __stcg(P.key[pass] + at, key);
-            __stcg(P.pos[pass] + at, pos);
+#pragma unroll 1
+    for (int i0 = w0 + lane; i0 - lane < w1; i0 += 32 * kSortBatch) {
+        int key[kSortBatch], pos[kSortBatch];
+#pragma unroll
+        for (int j = 0; j < kSortBatch; ++j) {
+            key[j] = -1; pos[j] = 0;
+            if (i0 + j * 32 < w1) key[j] = sort_key(P, pass, i0 + j * 32, pos[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kSortBatch; ++j) {
+            const int d = key[j] >= 0 ? digit_of(pass, key[j]) : -1;
+            const unsigned peers = same_digit(d);
+            const int rank = __popc(peers & ((1u << lane) - 1u));
+            int at = 0;
+            if (d >= 0) at = mine[d] + rank;
+            __syncwarp();
+            if (d >= 0) {
+                if (rank == 0) mine[d] = at + __popc(peers);
+                at += base[d];
+                __stcg(P.key[pass] + at, key[j]);
+                __stcg(P.pos[pass] + at, pos[j]);
+            }
+            __syncwarp();
         }
     }
-    __syncthreads();
+    if (CLUSTER) cluster_barrier(); else __syncthreads();
+    return total;
 }
+constexpr size_t kSortSmem = sizeof(int) * (kSortWarps + 1) * kDigits;
 
 // dW = 0, by CTAs [0, n) of a grid
 template <int OT>
@@ -217,21 +250,24 @@ __device__ void fill_zero(const GradParams &P, unsigned cta, unsigned n) {
     }
 }
 
+// The first cluster sorts, the others fill dW with zeros.  (Two passes of one cluster of eight and two barriers each against
+// eight more launches; the fill hides it up to some 10^5 tokens.)
 template <int OT>
-__global__ void __launch_bounds__(kSortThreads) tli_grad_sort_kernel(const GradParams P) {
+__global__ void __launch_bounds__(kSortThreads) tli_grad_sort_kernel(const __grid_constant__ GradParams P) {
     extern __shared__ __align__(16) int sort_smem[];
     __shared__ SortShared sh;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const unsigned sorters = P.groups == 1 ? 1u : 0u;
+    const unsigned sorters = P.clustered ? kSortCluster : 0u;
     if (blockIdx.x < sorters) {
-        sort_digit(P, 0, 0, P.N, sort_smem, sh);
-        sort_digit(P, 1, 0, __ldcg(P.n_valid), sort_smem, sh);
+        const int cta = static_cast<int>(cluster_cta_rank());
+        const int n = sort_digit<true>(P, 0, cta, P.N, sort_smem, sh);
+        sort_digit<true>(P, 1, cta, n, sort_smem, sh);
         return;
     }
     fill_zero<OT>(P, blockIdx.x - sorters, gridDim.x - sorters);
 }
 
-__global__ void __launch_bounds__(kSortThreads) tli_grad_count_kernel(const GradParams P, int pass) {
+__global__ void __launch_bounds__(kSortThreads) tli_grad_count_kernel(const __grid_constant__ GradParams P, int pass) {
     __shared__ int cnt[kDigits];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     cnt[threadIdx.x] = 0;
@@ -247,11 +283,11 @@ __global__ void __launch_bounds__(kSortThreads) tli_grad_count_kernel(const Grad
     P.count[blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
 }
 
-__global__ void __launch_bounds__(kSortThreads) tli_grad_scatter_kernel(const GradParams P, int pass) {
+__global__ void __launch_bounds__(kSortThreads) tli_grad_scatter_kernel(const __grid_constant__ GradParams P, int pass) {
     extern __shared__ __align__(16) int sort_smem[];
     __shared__ SortShared sh;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    sort_digit(P, pass, blockIdx.x, pass == 0 ? P.N : __ldcg(P.n_valid), sort_smem, sh);
+    sort_digit<false>(P, pass, blockIdx.x, pass == 0 ? P.N : __ldcg(P.n_valid), sort_smem, sh);
 }
 
 // ---- sums over the sorted tokens ----
@@ -329,43 +365,48 @@ template <int GT, bool VEC> struct Columns {
 };
 
 constexpr int kSumBatch = 8;               // rows of the gradient a thread has in flight
+constexpr int kMaxWindow = 256;
 
+// The windows of a block: their tokens' keys, with the one in front and the one behind (-1 where there is none), and positions.
 template <int GT, int OT, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const GradParams P) {
+__global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const __grid_constant__ GradParams P) {
+    extern __shared__ __align__(16) int window_smem[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int n = __ldcg(P.n_valid);
-    const int win = blockIdx.x * (kSumThreads / P.tx) + threadIdx.x / P.tx;
+    const int n = __ldcg(P.n_valid), ty = threadIdx.x / P.tx, tx = threadIdx.x % P.tx;
+    const int win = blockIdx.x * (kSumThreads / P.tx) + ty;
+    const int a = min(n, win * P.window), count = min(n, a + P.window) - a;
+    int *key = window_smem + ty * (2 * P.window + 2), *pos = key + P.window + 2;
+    for (int i = tx; i < P.window + 2; i += P.tx) {
+        const int at = a - 1 + i;
+        key[i] = at >= 0 && at < n ? __ldcg(P.key[1] + at) : -1;
+        if (i < P.window) pos[i] = a + i < n ? __ldcg(P.pos[1] + a + i) : 0;
+    }
+    __syncthreads();
     const Columns<GT, VEC> c(P, blockIdx.y);
-    const int a = win * P.window, e = min(n, a + P.window);
-    if (win >= P.nwin || a >= e || !c.any(P)) return;
-    const int *key = P.key[1], *pos = P.pos[1];
+    if (win >= P.nwin || count <= 0 || !c.any(P)) return;
     constexpr int kN = Columns<GT, VEC>::kN;
     float acc[kN] = {};
-    bool from_before = a > 0 && __ldcg(key + a - 1) == __ldcg(key + a);
-    int cur = __ldcg(key + a);
+    bool from_before = key[0] == key[1];
+    int cur = key[1];
     auto flush = [&](bool goes_on) {
         if (from_before) c.put(P, P.piece + (static_cast<size_t>(win) * 2) * P.H, acc);          // (it may go on as well)
         else if (goes_on) c.put(P, P.piece + (static_cast<size_t>(win) * 2 + 1) * P.H, acc);
         else c.template store<OT>(P, cur, acc);
     };
-    for (int i = a; i < e; i += kSumBatch) {
+#pragma unroll 1
+    for (int i = 0; i < count; i += kSumBatch) {
         float x[kSumBatch][kN];
-        int k[kSumBatch];
+#pragma unroll
+        for (int j = 0; j < kSumBatch; ++j) c.load(P, pos[min(i + j, count - 1)], x[j]);
 #pragma unroll
         for (int j = 0; j < kSumBatch; ++j) {
-            k[j] = -1;
-            if (i + j < e) {
-                k[j] = __ldcg(key + i + j);
-                c.load(P, __ldcg(pos + i + j), x[j]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < kSumBatch; ++j) {
-            if (k[j] < 0) break;
-            if (k[j] != cur) {
+            if (i + j >= count) break;
+            const int k = key[1 + i + j];
+            if (k != cur) {
                 flush(false);
                 from_before = false;
-                cur = k[j];
+                cur = k;
 #pragma unroll
                 for (int q = 0; q < kN; ++q) acc[q] = x[j][q];
             } else {
@@ -374,48 +415,65 @@ __global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const GradPar
             }
         }
     }
-    flush(e < n && __ldcg(key + e) == cur);
+    flush(key[1 + count] == cur);
 }
 
-// The row that begins in a window and goes on in the next ones.
+// The row that begins in a window and goes on in the next ones: their pieces in order, eight on their way at a time.
 template <int GT, int OT, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) tli_grad_join_kernel(const GradParams P) {
+__global__ void __launch_bounds__(kSumThreads) tli_grad_join_kernel(const __grid_constant__ GradParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int n = __ldcg(P.n_valid);
-    int win = blockIdx.x * (kSumThreads / P.tx) + threadIdx.x / P.tx;
+    const int win = blockIdx.x * (kSumThreads / P.tx) + threadIdx.x / P.tx;
     const Columns<GT, VEC> c(P, blockIdx.y);
-    const int a = win * P.window, e = min(n, a + P.window);
-    if (win >= P.nwin || a >= e || e >= n || !c.any(P)) return;
+    const int a = win * P.window, e = a + P.window;
+    if (win >= P.nwin || e >= n || !c.any(P)) return;
     const int *key = P.key[1];
-    const int cur = __ldcg(key + e - 1);
-    if (__ldcg(key + e) != cur) return;                            // ends in this window
-    if (a > 0 && __ldcg(key + a - 1) == cur) return;               // began before it
-    constexpr int kN = Columns<GT, VEC>::kN;
+    const int cur = __ldcg(key + e - 1), next = __ldcg(key + e), before = a > 0 ? __ldcg(key + a - 1) : -1;
+    if (next != cur || before == cur) return;                      // ends in this window, or began before it
+    constexpr int kN = Columns<GT, VEC>::kN, kBatch = 8;
     float acc[kN] = {};
     c.add(P, P.piece + (static_cast<size_t>(win) * 2 + 1) * P.H, acc);
-    int at = e;
-    do {
-        ++win;
-        c.add(P, P.piece + (static_cast<size_t>(win) * 2) * P.H, acc);
-        at = min(n, at + P.window);
-    } while (at < n && __ldcg(key + at) == cur && __ldcg(key + at - 1) == cur);
+    bool more = true;
+#pragma unroll 1
+    for (int w = win + 1; more; w += kBatch) {
+        bool in[kBatch];
+        float x[kBatch][kN];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int first = (w + j) * P.window;                  // a window that begins with the row has a piece of it
+            in[j] = first < n && __ldcg(key + first) == cur;
+#pragma unroll
+            for (int q = 0; q < kN; ++q) x[j][q] = 0.f;
+            // (pieces of windows behind the row's end are stale or foreign, but there: they are read and not used)
+            if (w + j < P.nwin) c.add(P, P.piece + (static_cast<size_t>(w + j) * 2) * P.H, x[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            more = more && in[j];
+            if (more) {
+#pragma unroll
+                for (int q = 0; q < kN; ++q) acc[q] += x[j][q];
+            }
+        }
+    }
     c.template store<OT>(P, cur, acc);
 }
 
 // ---- host ----
 
-constexpr int kSortOneCta = 65536;         // tokens one CTA sorts (it runs beside the zero fill)
+constexpr int kSortOneCluster = 131072;    // tokens one cluster sorts (it runs beside the zero fill)
 constexpr int kSortTile = 16384;           // tokens per CTA beyond that
 
-struct GradLayout { int groups, tile, window, nwin; size_t key0, pos0, key1, pos1, n_valid, count, piece, total; };
+struct GradLayout { int groups, tile, clustered, window, nwin; size_t key0, pos0, key1, pos1, n_valid, count, piece, total; };
 
 GradLayout grad_layout(int N, int H) {
     GradLayout L;
-    L.groups = N <= kSortOneCta ? (N > 0) : (N + kSortTile - 1) / kSortTile;
-    L.tile = L.groups <= 1 ? N : kSortTile;
-    // short windows spread a frequent row over more threads; long ones keep the pieces of many tokens small
-    L.window = 32;
-    while (L.window < 256 && N / L.window > 8192) L.window *= 2;
+    L.clustered = N > 0 && N <= kSortOneCluster;
+    L.groups = L.clustered ? kSortCluster : (N + kSortTile - 1) / kSortTile;
+    L.tile = L.clustered ? ((N + kSortCluster - 1) / kSortCluster + 31) & ~31 : kSortTile;
+    // short windows spread few tokens over more threads, long ones keep the pieces of many tokens few
+    L.window = 8;
+    while (L.window < kMaxWindow && N / L.window > 512) L.window *= 2;
     L.nwin = (N + L.window - 1) / L.window;
     size_t off = 0;
     L.key0 = off; off = align_up(off + sizeof(int) * N, 256);
@@ -423,7 +481,7 @@ GradLayout grad_layout(int N, int H) {
     L.key1 = off; off = align_up(off + sizeof(int) * N, 256);
     L.pos1 = off; off = align_up(off + sizeof(int) * N, 256);
     L.n_valid = off; off += 256;
-    L.count = off; off = align_up(off + (L.groups > 1 ? sizeof(int) * kDigits * L.groups : 0), 256);
+    L.count = off; off = align_up(off + sizeof(int) * kDigits * L.groups, 256);
     L.piece = off; off = align_up(off + sizeof(float) * 2 * L.nwin * static_cast<size_t>(H), 256);
     L.total = off;
     return L;
@@ -447,7 +505,7 @@ void pdl_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, cudaStream_t
     cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = stream;
 }
 
-template <int GT, int OT, bool VEC> int launch_grad_sums(const GradParams &P, cudaStream_t stream) {
+template <int GT, int OT, bool VEC> int launch_grad_sums(const GradParams &P, int device, cudaStream_t stream) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     pdl_config(cfg, attr, stream);
@@ -455,8 +513,13 @@ template <int GT, int OT, bool VEC> int launch_grad_sums(const GradParams &P, cu
     const int per_block = P.tx * kN;
     cfg.gridDim = dim3((P.nwin + kSumThreads / P.tx - 1) / (kSumThreads / P.tx), (P.H + per_block - 1) / per_block);
     cfg.blockDim = dim3(kSumThreads);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, tli_grad_sum_kernel<GT, OT, VEC>, P);
+    cfg.dynamicSmemBytes = sizeof(int) * (2 * P.window + 2) * (kSumThreads / P.tx);
+    static SmemAllowed allowed;
+    cudaError_t e = allowed.set(reinterpret_cast<const void *>(tli_grad_sum_kernel<GT, OT, VEC>), sizeof(int) * (2 * kMaxWindow + 2) * kSumThreads / kSumMinTx, device);
+    if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
+    e = cudaLaunchKernelEx(&cfg, tli_grad_sum_kernel<GT, OT, VEC>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_sum_kernel");
+    cfg.dynamicSmemBytes = 0;
     e = cudaLaunchKernelEx(&cfg, tli_grad_join_kernel<GT, OT, VEC>, P);
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_join_kernel");
     return TLI_OK;
@@ -466,17 +529,40 @@ template <int OT> int launch_grad(GradParams &P, int gdtype, int device, int num
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     pdl_config(cfg, attr, stream);
-    const size_t smem = sizeof(int) * kSortWarps * kDigits;
+    const size_t smem = kSortSmem;
     static SmemAllowed allowed_sort, allowed_scatter;
     cudaError_t e = allowed_sort.set(reinterpret_cast<const void *>(tli_grad_sort_kernel<OT>), smem, device);
     if (e == cudaSuccess) e = allowed_scatter.set(reinterpret_cast<const void *>(tli_grad_scatter_kernel), smem, device);
     if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
     cfg.blockDim = dim3(kSortThreads);
-    cfg.gridDim = dim3(num_sms); cfg.dynamicSmemBytes = smem;
-    e = cudaLaunchKernelEx(&cfg, tli_grad_sort_kernel<OT>, P);
+    {
+        cudaLaunchAttribute both[2];
+        both[0] = attr[0];
+        both[1].id = cudaLaunchAttributeClusterDimension;
+        both[1].val.clusterDim.x = kSortCluster; both[1].val.clusterDim.y = 1; both[1].val.clusterDim.z = 1;
+        cfg.attrs = both; cfg.numAttrs = P.clustered ? 2 : 1;
+        cfg.gridDim = dim3(num_sms); cfg.dynamicSmemBytes = 0;
+        if (P.clustered) {
+            // as many clusters as are resident together: the fill's shares are fixed, so a second wave would double its time
+            static std::atomic<int> resident{0};
+            int clusters = resident.load(std::memory_order_relaxed);
+            cfg.gridDim = dim3(2 * kSortCluster); cfg.dynamicSmemBytes = smem;
+            if (clusters == 0) {
+                cudaLaunchConfig_t ask = cfg;
+                ask.attrs = both + 1; ask.numAttrs = 1;
+                e = cudaOccupancyMaxActiveClusters(&clusters, tli_grad_sort_kernel<OT>, &ask);
+                if (e != cudaSuccess) return cuda_fail(e, "cudaOccupancyMaxActiveClusters");
+                clusters = std::max(2, clusters);
+                resident.store(clusters, std::memory_order_relaxed);
+            }
+            cfg.gridDim = dim3(clusters * kSortCluster);
+        }
+        e = cudaLaunchKernelEx(&cfg, tli_grad_sort_kernel<OT>, P);
+        cfg.attrs = attr; cfg.numAttrs = 1;
+    }
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_grad_sort_kernel");
     if (P.N == 0) return TLI_OK;
-    if (P.groups > 1) {
+    if (!P.clustered) {
         for (int pass = 0; pass < 2; ++pass) {
             cfg.gridDim = dim3(P.groups); cfg.dynamicSmemBytes = 0;
             e = cudaLaunchKernelEx(&cfg, tli_grad_count_kernel, P, pass);
@@ -489,10 +575,10 @@ template <int OT> int launch_grad(GradParams &P, int gdtype, int device, int num
     const size_t ge = gdtype == TLI_F32 ? 4 : 2;
     const bool vec = on_vectors(P.g, P.gs, ge) && on_vectors(P.out, P.os, Elt<OT>::kBytes) && P.H % 8 == 0;
     const int across = vec ? P.H / (gdtype == TLI_F32 ? 4 : 8) : (P.H + 3) / 4;
-    P.tx = 1;
+    P.tx = kSumMinTx;
     while (P.tx < kSumThreads && P.tx < across) P.tx *= 2;
-    if (gdtype == TLI_F32) return vec ? launch_grad_sums<TLI_F32, OT, true>(P, stream) : launch_grad_sums<TLI_F32, OT, false>(P, stream);
-    return vec ? launch_grad_sums<TLI_BF16, OT, true>(P, stream) : launch_grad_sums<TLI_BF16, OT, false>(P, stream);
+    if (gdtype == TLI_F32) return vec ? launch_grad_sums<TLI_F32, OT, true>(P, device, stream) : launch_grad_sums<TLI_F32, OT, false>(P, device, stream);
+    return vec ? launch_grad_sums<TLI_BF16, OT, true>(P, device, stream) : launch_grad_sums<TLI_BF16, OT, false>(P, device, stream);
 }
 
 }  // namespace
@@ -553,7 +639,7 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *a, void *cuda_stream
     if (a->grad_stride < 0 || (P.V > 1 && a->out_stride < a->H)) return TLI_ERR_ARG;
     const GradLayout L = grad_layout(a->N, a->H);
     if (!a->workspace || reinterpret_cast<uintptr_t>(a->workspace) % 256 || a->workspace_bytes < L.total) return TLI_ERR_WORKSPACE;
-    P.N = a->N; P.H = a->H; P.groups = L.groups; P.tile = L.tile; P.window = L.window; P.nwin = L.nwin;
+    P.N = a->N; P.H = a->H; P.groups = L.groups; P.tile = L.tile; P.clustered = L.clustered; P.window = L.window; P.nwin = L.nwin;
     P.ids = a->ids;
     P.g = a->grad; P.gs = a->grad_stride;
     P.out = a->out; P.os = a->out_stride;

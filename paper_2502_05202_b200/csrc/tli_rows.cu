@@ -35,8 +35,8 @@ constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kPickThreads = 256;                    // pick and spread kernels
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMaxGroups = 8192;                     // group maxima a pick CTA holds (coarser groups beyond)
-constexpr int kListCap = 4096;                       // elements a block searches in shared memory
-constexpr int kSample = 16384;                       // elements of a row that stand for it where the border is guessed
+constexpr int kListCap = 8192;                       // elements a block searches in shared memory
+constexpr int kSample = 8192;                        // elements of a row that stand for it where the border is guessed
 constexpr int kBins = 1024;
 
 struct __align__(16) StripSum { double S; float m; int pad; };       // sum of 2^((z - m) s) over a strip, m its largest
@@ -145,14 +145,33 @@ template <int DT> __device__ __noinline__ uint4 ragged_vector(const void *row, i
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Vector v of a row; ids outside the row or outside the mask read as -inf.
-template <int DT>
-__device__ __forceinline__ uint4 row_vector(const RowView<DT> &rv, const uint32_t *mask, int v, int nvec) {
+// B vectors of a row, v[] >= nvec for none; ids outside the row or outside the mask read as -inf.  The loads first, then what is rare and what
+// needs their results: a vector finished before the next one is asked for costs a trip to memory each.
+template <int DT, int B> __device__ __forceinline__ void row_vectors(const uint4 *vec0, const void *row, int head, int V, int nvec, const uint32_t *mask,
+                                                                     const int (&v)[B], uint4 (&raw)[B]) {
     constexpr uint32_t NI = Elt<DT>::kNegInfWord;
-    if (v >= nvec) return make_uint4(NI, NI, NI, NI);
-    const int e0 = rv.first_elem(v);
-    const uint4 raw = e0 >= 0 && e0 + Elt<DT>::kPerVec <= rv.V ? __ldg(rv.vec0 + v) : ragged_vector<DT>(rv.row, e0, rv.V);
-    return mask ? mask_vector<DT>(raw, mask, e0) : raw;
+    constexpr int EPV = Elt<DT>::kPerVec;
+    bool ragged = false;
+#pragma unroll
+    for (int k = 0; k < B; ++k) {
+        raw[k] = make_uint4(NI, NI, NI, NI);
+        const int e0 = v[k] * EPV - head;
+        const bool whole = v[k] < nvec && e0 >= 0 && e0 + EPV <= V;
+        if (whole) raw[k] = __ldg(vec0 + v[k]);
+        ragged |= v[k] < nvec && !whole;
+    }
+    if (ragged) {
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            const int e0 = v[k] * EPV - head;
+            if (v[k] < nvec && !(e0 >= 0 && e0 + EPV <= V)) raw[k] = ragged_vector<DT>(row, e0, V);
+        }
+    }
+    if (mask) {
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+            if (v[k] < nvec) raw[k] = mask_vector<DT>(raw[k], mask, v[k] * EPV - head);
+    }
 }
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
@@ -234,8 +253,10 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const __grid
     uint4 raw[U];
     const bool live = strip < P.nstrip;
     if (live) {
+        int v[U];
 #pragma unroll
-        for (int q = 0; q < U; ++q) raw[q] = row_vector<DT>(rv, P.mask, v0 + q * 32, nvec);
+        for (int q = 0; q < U; ++q) v[q] = v0 + q * 32;
+        row_vectors<DT, U>(rv.vec0, rv.row, rv.head, P.V, nvec, P.mask, v, raw);
     }
     const RowAsk ask(P, b);
     const bool sums = ask.whole_mass(P.sample);                    // the same for the whole CTA
@@ -316,42 +337,36 @@ struct PickState {
     const uint4 *vec0; const void *row; const uint32_t *mask;
     int head, V, nvec, nstrip, ulog, coarse, ngroups;
     int ng;                  // groups listed; -1: the whole row is
-    int room;                // 8-byte words between the list's start and the strip sums
     float m;
 };
 __shared__ PickState S;
 // Dynamic shared memory: three words per bin of a histogram (zero between uses), the strip sums, the elements that may lie at
-// the border; in the pick kernel also the row's group maxima, the numbers of the groups to read again, and room behind the list for
-// a sample of the row.
+// the border (or a sample of the row); in the pick kernel also the row's group maxima and the numbers of the groups to read again.
 extern __shared__ __align__(16) unsigned char pick_smem[];
 constexpr size_t settle_smem_bytes(int nstrip) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8; }
-constexpr size_t pick_smem_bytes(int nstrip, int ngroups) { return kBins * 12 + kSample * 4 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6; }
+constexpr size_t pick_smem_bytes(int nstrip, int ngroups) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6; }
 constexpr int kMaxRowStrips = (TLI_MAX_V + 6) / (4 * 32 * 8) + 1;
 constexpr size_t kPickSmemMax = pick_smem_bytes(kMaxRowStrips, kMaxGroups), kSettleSmemMax = settle_smem_bytes(kMaxRowStrips);
-static_assert(kSample * 4 >= kListCap * 8, "the sample's room holds the list");
+static_assert(kSample * 4 <= kListCap * 8, "the sample takes the place of the list");
 __device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem); }
 __device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem + kBins * 12); }
 __device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem + kBins * 12); }
 __device__ __forceinline__ u64 *masses() { return list() + kPickThreads; }                // of a short list
-__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12) + S.room; }
+__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12 + kListCap * 8); }
 __device__ __forceinline__ float *group_max() { return reinterpret_cast<float *>(strips() + S.nstrip); }
 __device__ __forceinline__ unsigned short *group_list() { return reinterpret_cast<unsigned short *>(group_max() + S.ngroups); }
 
-template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b, int room) {      // (visible after the next barrier)
+template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b) {      // (visible after the next barrier)
     for (int i = threadIdx.x; i < 3 * kBins / 4; i += kPickThreads) reinterpret_cast<uint4 *>(bins())[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) {
         const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
         S.vec0 = rv.vec0; S.row = rv.row; S.head = rv.head; S.V = P.V; S.nvec = rv.nvec(); S.mask = P.mask;
-        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse; S.room = room; S.ng = -1;
+        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse; S.ng = -1;
         S.ngroups = (P.nstrip + P.coarse - 1) / P.coarse * 32;
     }
 }
-template <int DT> __device__ __forceinline__ uint4 state_vector(int v) {      // vector v of the block's row
-    constexpr uint32_t NI = Elt<DT>::kNegInfWord;
-    if (v >= S.nvec) return make_uint4(NI, NI, NI, NI);
-    const int e0 = v * Elt<DT>::kPerVec - S.head;
-    const uint4 raw = e0 >= 0 && e0 + Elt<DT>::kPerVec <= S.V ? __ldg(S.vec0 + v) : ragged_vector<DT>(S.row, e0, S.V);
-    return S.mask ? mask_vector<DT>(raw, S.mask, e0) : raw;
+template <int DT, int B> __device__ __forceinline__ void state_vectors(const int (&v)[B], uint4 (&raw)[B]) {      // of the block's row
+    row_vectors<DT, B>(S.vec0, S.row, S.head, S.V, S.nvec, S.mask, v, raw);
 }
 template <int DT> __device__ __forceinline__ float vector_element(const uint4 &r, int i) {               // i not known in advance
     if (DT == TLI_F32) return __uint_as_float(i < 2 ? (i == 0 ? r.x : r.y) : (i == 2 ? r.z : r.w));
@@ -405,7 +420,7 @@ template <typename T> __device__ __noinline__ Prefix<T> block_prefix(T x) {
 
 // First bin at which the running measure, from `before`, reaches `want` (-1 if none does), the measure in front of it (or of everything)
 // and its own.
-// A bin's measure is w0 + (w1 << shift) + (w2 << 40).  The bins come back zero unless they are to be kept.
+// A bin's measure is w0 + (w1 << shift) + (w2 << 38).  The bins come back zero unless they are to be kept.
 struct BinAt { int bin; u64 before, measure; };
 static_assert(kBins == 4 * kPickThreads, "four bins per thread");
 __device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool keep) {
@@ -413,7 +428,7 @@ __device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool kee
     uint4 *w = reinterpret_cast<uint4 *>(bins()) + threadIdx.x;
     const uint4 a = w[0], b = w[kBins / 4], c = w[kBins / 2];
     if (!keep) { w[0] = make_uint4(0, 0, 0, 0); w[kBins / 4] = w[0]; w[kBins / 2] = w[0]; }
-    auto value = [shift](unsigned lo, unsigned mid, unsigned hi) { return lo + (static_cast<u64>(mid) << shift) + (static_cast<u64>(hi) << 40); };
+    auto value = [shift](unsigned lo, unsigned mid, unsigned hi) { return lo + (static_cast<u64>(mid) << shift) + (static_cast<u64>(hi) << 38); };
     const u64 x0 = value(a.x, b.x, c.x), x1 = value(a.y, b.y, c.y), x2 = value(a.z, b.z, c.z), x3 = value(a.w, b.w, c.w);
     const u64 mine = x0 + x1 + x2 + x3;
     const Prefix<u64> p = block_prefix(mine);
@@ -438,11 +453,11 @@ __device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool kee
 __device__ __forceinline__ int bin_shift(u64 range) { return range < kBins ? 0 : 54 - __clzll(range); }      // (range >> shift) < 1024
 // an element's weight in units of 1/unit; sums of it do not depend on their order
 template <int DT> __device__ __forceinline__ u64 mass_of(u64 e, double unit) { return __double2ull_rn(S.w(element_logit<DT>(e)) * unit); }
-__device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^60, in three words of 20 bits: 4096 cannot overflow 32
+__device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^57, in three words of 19 bits: 8192 cannot overflow 32
     unsigned *w = bins() + k;
-    atomicAdd(w, static_cast<uint32_t>(f) & 0xfffffu);
-    atomicAdd(w + kBins, static_cast<uint32_t>(f >> 20) & 0xfffffu);
-    const uint32_t c = static_cast<uint32_t>(f >> 40);
+    atomicAdd(w, static_cast<uint32_t>(f) & 0x7ffffu);
+    atomicAdd(w + kBins, static_cast<uint32_t>(f >> 19) & 0x7ffffu);
+    const uint32_t c = static_cast<uint32_t>(f >> 38);
     if (c) atomicAdd(w + 2 * kBins, c);
 }
 
@@ -463,7 +478,7 @@ template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 
                 else atomicAdd(bins() + static_cast<int>(p >> shift), 1u);
             }
         }
-        const BinAt at = find_bin(want, before, 20, false);
+        const BinAt at = find_bin(want, before, 19, false);
         if (at.bin < 0) return 0;
         before = at.before;
         low += static_cast<u64>(at.bin) << shift;
@@ -567,8 +582,7 @@ template <int DT> __device__ __noinline__ int gather(float zlow) {
         int v[B];
 #pragma unroll
         for (int k = 0; k < B; ++k) v[k] = t0 + k * kPickThreads < total ? listed_vector(t0 + k * kPickThreads) : S.nvec;
-#pragma unroll
-        for (int k = 0; k < B; ++k) raw[k] = state_vector<DT>(v[k]);
+        state_vectors<DT, B>(v, raw);
         unsigned in = 0;
 #pragma unroll
         for (int k = 0; k < B; ++k) {
@@ -641,7 +655,7 @@ __device__ __noinline__ float floor_from_groups(bool by_mass, unsigned want, flo
             if (add) atomicAdd(bins() + min(static_cast<int>((m - x) * per), kBins - 1), add);
         }
     }
-    const int bin = find_bin(want, 0, 20, false).bin;
+    const int bin = find_bin(want, 0, 19, false).bin;
     if (bin < 0) return -INFINITY;
     int low = INT_MAX;                                             // the smallest of these bins, by the same rounding that put it there
 #pragma unroll 2
@@ -672,8 +686,7 @@ template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, floa
         int v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = t0 + k * kPickThreads < total ? listed_vector(t0 + k * kPickThreads) : S.nvec;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) raw[k] = state_vector<DT>(v[k]);
+        state_vectors<DT, 4>(v, raw);
         unsigned in = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -796,7 +809,7 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
 
 // ---- the border among thousands: a bracket from a sample ----
 
-// Two logits that the k-th largest (or the last one inside top-p) lies between but for bad luck, from up to 16384 elements
+// Two logits that the k-th largest (or the last one inside top-p) lies between but for bad luck, from up to 8192 elements
 // spread over the row: where the sample itself has that place, and four standard errors to both sides (fewer, if as many elements
 // as lie between would not fit `capacity`).  The sample is counted (weighed) in 1024 equal parts of the interval between its extremes.
 struct Bracket { float low, high; };
@@ -806,15 +819,27 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
     const float m = S.m;
     float least = INFINITY;
     __syncthreads();
-#pragma unroll 8
-    for (int j = threadIdx.x; j < total; j += kPickThreads) {
-        const uint4 r = state_vector<DT>(whole ? j : static_cast<int>(static_cast<long long>(j) * S.nvec / total));
-        float z[EPV];
-        unpack<DT>(r, z);
+    constexpr int B = 4;
+    static_assert(total % (B * kPickThreads) == 0, "whole batches");
+#pragma unroll 1
+    for (int j0 = threadIdx.x; j0 < total; j0 += B * kPickThreads) {
+        uint4 raw[B];
+        int v[B];
 #pragma unroll
-        for (int k = 0; k < EPV; ++k) {
-            if (z[k] > -INFINITY) least = fminf(least, z[k]);
-            sample()[k * total + j] = z[k];
+        for (int k = 0; k < B; ++k) {
+            const int j = j0 + k * kPickThreads;
+            v[k] = whole ? j : static_cast<int>(static_cast<long long>(j) * S.nvec / total);
+        }
+        state_vectors<DT, B>(v, raw);
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            float z[EPV];
+            unpack<DT>(raw[k], z);
+#pragma unroll
+            for (int i = 0; i < EPV; ++i) {
+                if (z[i] > -INFINITY) least = fminf(least, z[i]);
+                sample()[i * total + j0 + k * kPickThreads] = z[i];
+            }
         }
     }
     least = order_float(block_min(float_order(least)));
@@ -825,7 +850,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
     const double share = whole ? 1.0 : static_cast<double>(total) / S.nvec, spare = whole ? 0.0 : 4.0 * sqrt(1.0 - share);
     const bool by_mass = !ask.k_on;
     // by mass: (1-p) Z lies below the border, and the many small weights there are what a sample knows well; in units of
-    // 1/2^17 of it, each clipped at 1.9 (16384 of them fit 32 bits), from the smallest logit up
+    // 1/2^17 of it, each clipped at 1.9 (8192 of them fit 32 bits), from the smallest logit up
     const float sf = static_cast<float>(S.w.s), unit = by_mass ? static_cast<float>(131072.0 / ((1.0 - static_cast<double>(ask.p)) * Z * share)) : 0.f;
     auto bin_of = [&](float z) { return min(static_cast<int>((z - least) * per_bin), kBins - 1); };
 #pragma unroll 4
@@ -842,7 +867,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
     double want, off;
     if (by_mass) {
         want = 131072.0;
-        const int place = find_bin(131072, 0, 20, true).bin;
+        const int place = find_bin(131072, 0, 19, true).bin;
         float square = 0.f;
 #pragma unroll 4
         for (int j = threadIdx.x; j < kSample; j += kPickThreads) {
@@ -856,7 +881,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
     }
     // the places in bins, by proportion inside a bin
     auto place = [&](double at, bool keep) {
-        const BinAt f = find_bin(static_cast<u64>(fmax(1.0, at)), 0, 20, keep);
+        const BinAt f = find_bin(static_cast<u64>(fmax(1.0, at)), 0, 19, keep);
         return f.bin < 0 ? -1.f : f.bin + static_cast<float>((at - static_cast<double>(f.before)) / static_cast<double>(f.measure));
     };
 #pragma unroll 1
@@ -892,7 +917,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
 
 // The border among the n listed elements (logits from ztop down to zlow), with `above` elements of mass `above_mass` in front of
 // them, all kept as far as the list reaches; if they number fewer than k, nothing below zlow could be kept either.  Elements >= edge
-// are kept, in the list and out of it (edge 0: the border is not here).  unit: for masses, so that no sum of them reaches 2^60.
+// are kept, in the list and out of it (edge 0: the border is not here).  unit: for masses, so that no sum of them reaches 2^57.
 struct Edge { u64 edge; double unit; };
 template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask, bool draw, float zmin, double Z, int n, float ztop, float zlow, u64 above, double above_mass) {
     const u64 first = element_of<DT>(ztop, 0), range = first - (static_cast<u64>(logit_key<DT>(zlow)) << 20);
@@ -906,7 +931,7 @@ template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask,
     if (ask.p_on || draw) {
         // (without Z: as many weights up to 1 as there are)
         const double most = ask.p_on && !ask.k_on ? Z : above_mass + fmin(static_cast<double>(n), ask.k_on ? static_cast<double>(ask.k) : static_cast<double>(n));
-        r.unit = two_to(59 - exponent(most));
+        r.unit = two_to(56 - exponent(most));
         if (ask.p_on) {
             const u64 before = __double2ull_rn(above_mass * r.unit);
             double mass = Z * r.unit;
@@ -938,8 +963,8 @@ struct Draw { int token; double prob; };
 template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk &ask, bool draw, float u, float zmin, double Z, int n, Border &border) {
     const int tid = threadIdx.x;
     const u64 e = tid < n ? list()[tid] : 0ull;
-    // the masses' unit: every sum formed here stays below 2^60
-    const double unit = two_to(59 - exponent(ask.p_on && !ask.k_on ? Z : static_cast<double>(n)));
+    // the masses' unit: every sum formed here stays below 2^57
+    const double unit = two_to(56 - exponent(ask.p_on && !ask.k_on ? Z : static_cast<double>(n)));
     const bool weigh = ask.p_on || draw;
     const double w = e && weigh ? S.w(element_logit<DT>(e)) : 0.0;
     const u64 f = __double2ull_rn(w * unit);
@@ -1057,7 +1082,10 @@ template <int DT> __device__ __noinline__ Draw draw_by_strips(Border border, flo
 #pragma unroll 1
         for (int q = 0; q < (1 << S.ulog) && id_hit < 0; ++q) {
             const int v = (strip << (5 + S.ulog)) + q * 32 + lane, e0 = v * EPV - S.head;
-            const uint4 r = state_vector<DT>(v);
+            const int one[1] = {v};
+            uint4 r1[1];
+            state_vectors<DT, 1>(one, r1);
+            const uint4 r = r1[0];
             double x[EPV], sum = 0.0, w_mine = 0.0;
             int id_mine = -1;
 #pragma unroll
@@ -1130,7 +1158,7 @@ template <int DT>
 __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
     exp2_table_init(S.tab, tid);
-    enter_row<DT>(P, row, b, kSample / 2);
+    enter_row<DT>(P, row, b);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const RowAsk ask(P, b);
@@ -1183,7 +1211,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     float floor = -INFINITY;
     if (ask.k_on) {
         floor = ask.k <= kPickThreads / 2 ? floor_from_threads(ask.k, tmax) : floor_from_groups(false, ask.k, tmax);
-        if (floor == -INFINITY && P.V > kListCap && ask.k <= kListCap * 3 / 4) {       // too few groups for that many: from a sample
+        if (floor == -INFINITY && ask.p_on && P.V > kListCap && ask.k <= kListCap * 3 / 4) {       // too few groups for that many: from a sample
             floor = bracket<DT>(ask, Z, kListCap - ask.k).low;
             if (floor == -FLT_MAX) floor = -INFINITY;
         }
@@ -1193,8 +1221,12 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     const bool ok = floor > -INFINITY || (!ask.k_on && !ask.p_on);
     const float zlow = ask.p_on ? fmaxf(floor, -FLT_MAX) : fmaxf(floor, zmin);
     list_groups(zlow, tmax);
-    // every listed group has an element; without a floor only short and mostly masked rows are worth a try
-    const int n = S.ng <= (ok || P.V <= kListCap ? kListCap : 256) ? gather<DT>(zlow) : INT_MAX;
+    // Every listed group has an element.  Without a floor only short and mostly masked rows are worth a try; and beyond some 4096
+    // vectors to read again (4 ns each for this one block) all blocks together are faster, except that they do not do
+    // top-k with top-p.
+    const int vectors = S.ng * (P.coarse << P.ulog);
+    const bool worth = P.V <= kListCap || (ok ? vectors <= 4096 || (ask.k_on && ask.p_on && S.ng <= kListCap) : S.ng <= 256);
+    const int n = worth ? gather<DT>(zlow) : INT_MAX;
     // (fewer than k above a sampled floor: there may be more below it)
     const bool whole = !(ask.k_on && n < ask.k && zlow == floor);
     Border border;
@@ -1250,8 +1282,10 @@ template <int DT, int U> __device__ __forceinline__ void spread_strip(const Rows
     };
     if (__any_sync(0xffffffffu, want)) {
         uint4 raw[U];
+        int v[U];
 #pragma unroll
-        for (int q = 0; q < U; ++q) raw[q] = state_vector<DT>(want ? v0 + q * 32 : nvec);
+        for (int q = 0; q < U; ++q) v[q] = want ? v0 + q * 32 : nvec;
+        state_vectors<DT, U>(v, raw);
 #pragma unroll 1
         for (int q = 0; q < U; ++q) {
             const uint4 r = raw[0];
@@ -1372,7 +1406,7 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
 // The rows that the pick kernel left, by all blocks: each takes eight strips at a time (the next ones when it is done: the block
 // that ends last with a row settles it, which takes as long as several strips).
 template <int DT, int U>
-__global__ void __launch_bounds__(kPickThreads, 3) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
+__global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = __ldcg(P.todo);
@@ -1394,7 +1428,7 @@ __global__ void __launch_bounds__(kPickThreads, 3) tli_rows_spread_kernel(const 
             S.m = __ldcg(&plan->m);
             S.w = Weights(S.m, __ldg(P.tau + b), S.tab);
         }
-        enter_row<DT>(P, row, b, kListCap);
+        enter_row<DT>(P, row, b);
         __syncthreads();
         const int strip = task % nchunk * kPickWarps + (tid >> 5);
         if (strip < P.nstrip) spread_strip<DT, U>(P, plan, row, strip, zlo, zhi, bid, P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f));
@@ -1501,8 +1535,9 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.border = off; off = align_up(off + sizeof(RowBorder) * rows, 256);
     L.plan = off; off = align_up(off + sizeof(RowPlan) * rows, 256);
     L.todo = off; off = align_up(off + sizeof(int) * (rows + 2), 256);
-    // bracketed elements of a row: a sample of 16384 puts the border within about V/64 of them
-    L.listcap = V <= kListCap ? 0 : std::min(kListCap, std::max(2048, V / 32));
+    // bracketed elements of a row: a sample of 8192 puts the border within about V/50 of them; in 16 bits the ties at the
+    // bracket's ends come along
+    L.listcap = V <= kListCap ? 0 : std::min(kListCap, std::max(2048, V / 20));
     L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
     L.total = off;
     return L;
@@ -1549,7 +1584,7 @@ template <int DT, int U> int launch_rows(const RowsParams &P, int device, int nu
         e = allowed_spread.set(reinterpret_cast<const void *>(tli_rows_spread_kernel<DT, U>), kSettleSmemMax, device);
         if (e != cudaSuccess) return cuda_fail(e, "cudaFuncSetAttribute");
         const long long blocks = static_cast<long long>(rows) * ((P.nstrip + kPickWarps - 1) / kPickWarps);
-        cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(blocks, 3LL * num_sms))); cfg.blockDim = dim3(kPickThreads);
+        cfg.gridDim = dim3(static_cast<unsigned>(std::min<long long>(blocks, 2LL * num_sms))); cfg.blockDim = dim3(kPickThreads);
         cfg.dynamicSmemBytes = settle_smem_bytes(P.nstrip);
         e = cudaLaunchKernelEx(&cfg, tli_rows_spread_kernel<DT, U>, P);
         if (e != cudaSuccess) return cuda_fail(e, "launch tli_rows_spread_kernel");

@@ -752,6 +752,7 @@ class Verifier:
             tli_set_tiled(self.ctx, True)
         self._ws: Optional[torch.Tensor] = None
         self._index, self._lib, self._plans = int(device), load(), {}
+        self._stream_ws: Dict[int, torch.Tensor] = {}
 
     def close(self) -> None:
         if self.ctx:
@@ -789,8 +790,17 @@ class Verifier:
         tli_draft_sample(self.ctx, args)
         return out
 
-    # The calls below may overlap others on this context, so each has scratch of its own, from torch's allocator on the
-    # current stream (which also serves a capture).  What depends on shapes alone is worked out once per shape.
+    # The calls below may overlap others on this context: each stream has scratch of its own, in whose order the calls on it
+    # use it, and so has every captured call.  What depends on shapes alone is worked out once per shape.
+
+    def _scratch(self, need: int) -> torch.Tensor:
+        if torch._C._cuda_isCurrentStreamCapturing():
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
+        stream = _raw_stream(self._index)
+        ws = self._stream_ws.get(stream)
+        if ws is None or ws.numel() < need:
+            ws = self._stream_ws[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return ws
 
     def _plan(self, kind: str, key, make):
         plan = self._plans.get((kind, key))
@@ -845,10 +855,9 @@ class Verifier:
         if uniforms.dtype is not torch.float32 or uniforms.shape != shape or uniforms.get_device() != self._index or not uniforms.is_contiguous():
             raise ValueError("uniforms must be a contiguous float32 tensor of shape %s on %s" % (shape, self.device))
         dev = self.device
-        tokens = torch.empty(shape, dtype=torch.int32, device=dev)
-        prob = torch.empty(shape, dtype=torch.float32, device=dev)
-        status = torch.empty(shape, dtype=torch.int32, device=dev)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        tokens, prob, status = torch.empty((3, *shape), dtype=torch.int32, device=dev).unbind(0)     # one allocation for three
+        prob = prob.view(torch.float32)
+        ws = self._scratch(need)
         a = tli_sample_args.from_buffer_copy(template)
         a.logits = logits.data_ptr()
         a.temperature = temperature.data_ptr()
@@ -870,7 +879,7 @@ class Verifier:
         elif out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index or (out.shape[2] > 1 and out.stride(2) != 1):
             raise ValueError("out must have the logits' type, shape and device, and a contiguous vocabulary axis")
         status = torch.empty(shape, dtype=torch.int32, device=dev)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = self._scratch(need)
         a = tli_filter_args.from_buffer_copy(template)
         a.logits = logits.data_ptr()
         a.temperature = temperature.data_ptr()
@@ -921,7 +930,7 @@ class Verifier:
         need = self._plan("grad", (N, H), lambda: tli_embed_grad_workspace_bytes(self.ctx, N, H))
         if need == 0:
             raise TLIError(TLI_ERR_UNSUPPORTED, "tli_embed_grad_workspace_bytes")
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = self._scratch(need)
         self._call("tli_embed_grad", tli_embed_grad_args(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
                                                          grad.data_ptr(), stride, scale, out.data_ptr(), H, ws.data_ptr(), need))
         return {"grad": out}
