@@ -35,7 +35,8 @@ constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kPickThreads = 256;                    // pick and spread kernels
 constexpr int kPickWarps = kPickThreads / 32;
 constexpr int kMaxGroups = 8192;                     // group maxima a pick CTA holds (coarser groups beyond)
-constexpr int kListCap = 8192;                       // elements a block searches in shared memory
+constexpr int kListCap = 4096;                       // elements the pick kernel searches in shared memory
+constexpr int kSpreadCap = 8192;                     // ... the spread kernel
 constexpr int kSample = 8192;                        // elements of a row that stand for it where the border is guessed
 constexpr int kBins = 1024;
 
@@ -94,13 +95,16 @@ __device__ __forceinline__ double exp2_neg(double x, const double *tab) {
 }
 __device__ __forceinline__ int exponent(double x) { return ((__double2hiint(x) >> 20) & 0x7ff) - 1023; }     // of a normal number
 __device__ __forceinline__ double two_to(int n) { return __hiloint2double((n + 1023) << 20, 0); }
-// w(z) = exp((z - m)/tau), s = log2(e)/tau; 0 below cut (2^-1020 of the largest; -inf among them)
+// w(z) = exp((z - m)/tau), s = log2(e)/tau; 0 below cut (exp(-707) of the largest; -inf among them)
 struct Weights {
     double m, s; float cut; const double *tab;
     Weights() = default;
     __device__ __forceinline__ Weights(float m_, float tau, const double *tab_) {
-        m = m_; s = 1.4426950408889634074 / tau; tab = tab_;
-        cut = fmaxf(__double2float_ru(m - 1020.0 / s), -FLT_MAX);        // rounded up: z >= cut stays in exp2_neg's range
+        m = m_; s = kLog2e / tau; tab = tab_; cut = cut_of(m_, tau);
+    }
+    static constexpr double kLog2e = 1.4426950408889634074;
+    __device__ __forceinline__ static float cut_of(float m, float tau) {       // rounded up: z >= cut stays in exp2_neg's range
+        return fmaxf(__double2float_ru(static_cast<double>(m) - 707.0 * static_cast<double>(tau)), -FLT_MAX);
     }
     __device__ __forceinline__ double operator()(float z) const {
         const double w = exp2_neg((static_cast<double>(z) - m) * s, tab);
@@ -330,6 +334,7 @@ __device__ __forceinline__ int element_id(u64 e) { return static_cast<int>(kIdMa
 struct PickState {
     double tab[16];
     u64 slot[kPickWarps];
+    u64 few[kPickThreads], few_mass[kPickThreads];     // a short list and its masses
     u64 found, before;
     int bin, listed;
     // the row
@@ -337,13 +342,14 @@ struct PickState {
     const uint4 *vec0; const void *row; const uint32_t *mask;
     int head, V, nvec, nstrip, ulog, coarse, ngroups;
     int ng;                  // groups listed; -1: the whole row is
+    int room;                // elements the list has room for
     float m;
 };
 __shared__ PickState S;
 // Dynamic shared memory: three words per bin of a histogram (zero between uses), the strip sums, the elements that may lie at
 // the border (or a sample of the row); in the pick kernel also the row's group maxima and the numbers of the groups to read again.
 extern __shared__ __align__(16) unsigned char pick_smem[];
-constexpr size_t settle_smem_bytes(int nstrip) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8; }
+constexpr size_t settle_smem_bytes(int nstrip) { return kBins * 12 + kSpreadCap * 8 + static_cast<size_t>(nstrip) * 8; }
 constexpr size_t pick_smem_bytes(int nstrip, int ngroups) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6; }
 constexpr int kMaxRowStrips = (TLI_MAX_V + 6) / (4 * 32 * 8) + 1;
 constexpr size_t kPickSmemMax = pick_smem_bytes(kMaxRowStrips, kMaxGroups), kSettleSmemMax = settle_smem_bytes(kMaxRowStrips);
@@ -351,17 +357,16 @@ static_assert(kSample * 4 <= kListCap * 8, "the sample takes the place of the li
 __device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem); }
 __device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem + kBins * 12); }
 __device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem + kBins * 12); }
-__device__ __forceinline__ u64 *masses() { return list() + kPickThreads; }                // of a short list
-__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12 + kListCap * 8); }
+__device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12) + S.room; }
 __device__ __forceinline__ float *group_max() { return reinterpret_cast<float *>(strips() + S.nstrip); }
 __device__ __forceinline__ unsigned short *group_list() { return reinterpret_cast<unsigned short *>(group_max() + S.ngroups); }
 
-template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b) {      // (visible after the next barrier)
+template <int DT> __device__ __forceinline__ void enter_row(const RowsParams &P, int row, int b, int room) {      // (visible after the next barrier)
     for (int i = threadIdx.x; i < 3 * kBins / 4; i += kPickThreads) reinterpret_cast<uint4 *>(bins())[i] = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) {
         const RowView<DT> rv(P.z, b * P.sb + (row - b * P.R) * P.sr, P.V);
         S.vec0 = rv.vec0; S.row = rv.row; S.head = rv.head; S.V = P.V; S.nvec = rv.nvec(); S.mask = P.mask;
-        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse; S.ng = -1;
+        S.nstrip = P.nstrip; S.ulog = P.ulog; S.coarse = P.coarse; S.ng = -1; S.room = room;
         S.ngroups = (P.nstrip + P.coarse - 1) / P.coarse * 32;
     }
 }
@@ -453,7 +458,7 @@ __device__ __noinline__ BinAt find_bin(u64 want, u64 before, int shift, bool kee
 __device__ __forceinline__ int bin_shift(u64 range) { return range < kBins ? 0 : 54 - __clzll(range); }      // (range >> shift) < 1024
 // an element's weight in units of 1/unit; sums of it do not depend on their order
 template <int DT> __device__ __forceinline__ u64 mass_of(u64 e, double unit) { return __double2ull_rn(S.w(element_logit<DT>(e)) * unit); }
-__device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^57, in three words of 19 bits: 8192 cannot overflow 32
+__device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^57, in three words of 19 bits: kSpreadCap of them cannot overflow 32
     unsigned *w = bins() + k;
     atomicAdd(w, static_cast<uint32_t>(f) & 0x7ffffu);
     atomicAdd(w + kBins, static_cast<uint32_t>(f >> 19) & 0x7ffffu);
@@ -463,12 +468,15 @@ __device__ __forceinline__ void add_mass(int k, u64 f) {          // f < 2^57, i
 
 // Among the n listed elements that are >= edge, in their order (BY_ID: in increasing id): the one at which the running
 // measure (their number; BY_MASS: their fixed-point mass) reaches `want`, coming from `before`; 0 if none does.  A histogram
-// of 1024 bins over the interval that is left, from the element `first` on, until it holds one.
+// of 1024 bins over the interval that is left, from the element `first` on, until few are left (a level costs some 4000 cycles, a
+// few in front of another 10 each); then every thread adds up what is in front of its own.
 enum : int { BY_MASS = 1, BY_ID = 2 };
+constexpr int kFew = 64;
 template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 want, u64 before, u64 first, u64 range, int how, double unit) {
     u64 low = 0;
     auto pos = [&](u64 e) { return (how & BY_ID) ? static_cast<u64>(element_id(e)) : first - e; };
-    for (;;) {
+    int few;
+    do {
         const int shift = bin_shift(range);
 #pragma unroll 1
         for (int i = threadIdx.x; i < n; i += kPickThreads) {
@@ -478,23 +486,35 @@ template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 
                 else atomicAdd(bins() + static_cast<int>(p >> shift), 1u);
             }
         }
+        if (threadIdx.x == 0) S.listed = 0;
         const BinAt at = find_bin(want, before, 19, false);
         if (at.bin < 0) return 0;
         before = at.before;
         low += static_cast<u64>(at.bin) << shift;
         range = min(range - (static_cast<u64>(at.bin) << shift), (1ull << shift) - 1);
-        int inside = 0;
 #pragma unroll 1
         for (int i = threadIdx.x; i < n; i += kPickThreads) {
             const u64 e = list()[i];
-            if (e >= edge && pos(e) - low <= range) { ++inside; S.found = e; }       // (used if it is the only one)
+            if (e >= edge && pos(e) - low <= range) {
+                const int k = atomicAdd(&S.listed, 1);
+                if (k < kFew) S.few[k] = e;
+            }
         }
-        if (block_sum(inside) == 1) {
-            const u64 e = S.found;
-            __syncthreads();
-            return e;
-        }
+        __syncthreads();
+        few = S.listed;
+        __syncthreads();
+    } while (few > kFew);
+    const u64 e = threadIdx.x < few ? S.few[threadIdx.x] : 0ull;
+    const u64 f = !e ? 0ull : (how & BY_MASS) ? mass_of<DT>(e, unit) : 1ull;
+    S.few_mass[threadIdx.x] = f;
+    __syncthreads();
+    if (e) {
+#pragma unroll 4
+        for (int j = 0; j < few; ++j) before += pos(S.few[j]) < pos(e) ? S.few_mass[j] : 0ull;
+        if (before < want && before + f >= want) S.found = e;      // one thread: the bin's running measure passes `want` once
     }
+    __syncthreads();
+    return S.found;
 }
 
 // ---- steps of the pick kernel ----
@@ -968,7 +988,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
     const bool weigh = ask.p_on || draw;
     const double w = e && weigh ? S.w(element_logit<DT>(e)) : 0.0;
     const u64 f = __double2ull_rn(w * unit);
-    masses()[tid] = f;
+    S.few_mass[tid] = f;
     __syncthreads();
     int rank = 0;
     u64 ahead = 0;
@@ -977,7 +997,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
         for (int j = 0; j < n; ++j) {
             const bool before = list()[j] > e;
             rank += before;
-            ahead += before ? masses()[j] : 0ull;
+            ahead += before ? S.few_mass[j] : 0ull;
         }
     }
     const int k = ask.k_on ? min(ask.k, n) : n;
@@ -1001,7 +1021,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
     u64 own = f;
     if (target == 0) {                                             // the lowest id that has any weight
         own = w > 0.0;
-        masses()[tid] = own;
+        S.few_mass[tid] = own;
         __syncthreads();
     }
     if (kept) {
@@ -1010,7 +1030,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const u64 x = list()[j];
-            before += x >= edge && (static_cast<uint32_t>(x) & kIdMask) > id ? masses()[j] : 0ull;
+            before += x >= edge && (static_cast<uint32_t>(x) & kIdMask) > id ? S.few_mass[j] : 0ull;
         }
         if (before <= target && target < before + own) S.found = e;
     }
@@ -1158,7 +1178,7 @@ template <int DT>
 __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
     exp2_table_init(S.tab, tid);
-    enter_row<DT>(P, row, b);
+    enter_row<DT>(P, row, b, kListCap);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const RowAsk ask(P, b);
@@ -1167,6 +1187,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
 
     __syncthreads();
     const float tmax = load_groups<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32);
+    const double scale = Weights::kLog2e / ask.tau;                // (beside the loads)
     const int bad = (ask.bad_tau ? TLI_ROW_BAD_TEMPERATURE : 0) | (ask.bad_filter ? TLI_ROW_BAD_FILTER : 0);
     if (bad) { finish_row(P, row, bad, BORDER_COPY, all, -1, 0.0); return; }
     // NaN lies above +inf, and that above every finite number, in this order
@@ -1175,7 +1196,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     if (!(m > -INFINITY)) { finish_row(P, row, TLI_ROW_FALLBACK, BORDER_APPLY, all, -1, 0.0); return; }      // no id to keep
     if (tid == 0) {
         S.m = m;
-        if (!ask.one) S.w = Weights(m, ask.tau, S.tab);
+        S.w.m = m; S.w.s = scale; S.w.tab = S.tab; S.w.cut = Weights::cut_of(m, ask.tau);
     }
 
     if (ask.one) {                                                 // the lowest id at the largest logit
@@ -1428,7 +1449,7 @@ __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const 
             S.m = __ldcg(&plan->m);
             S.w = Weights(S.m, __ldg(P.tau + b), S.tab);
         }
-        enter_row<DT>(P, row, b);
+        enter_row<DT>(P, row, b, kSpreadCap);
         __syncthreads();
         const int strip = task % nchunk * kPickWarps + (tid >> 5);
         if (strip < P.nstrip) spread_strip<DT, U>(P, plan, row, strip, zlo, zhi, bid, P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f));
@@ -1537,7 +1558,7 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.todo = off; off = align_up(off + sizeof(int) * (rows + 2), 256);
     // bracketed elements of a row: a sample of 8192 puts the border within about V/50 of them; in 16 bits the ties at the
     // bracket's ends come along
-    L.listcap = V <= kListCap ? 0 : std::min(kListCap, std::max(2048, V / 20));
+    L.listcap = V <= kListCap ? 0 : std::min(kSpreadCap, std::max(2048, V / 20));
     L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
     L.total = off;
     return L;
