@@ -347,16 +347,14 @@ struct PickState {
 };
 __shared__ PickState S;
 // Dynamic shared memory: three words per bin of a histogram (zero between uses), the strip sums, the elements that may lie at
-// the border (or a sample of the row); in the pick kernel also the row's group maxima and the numbers of the groups to read again.
+// the border; in the pick kernel also the row's group maxima and the numbers of the groups to read again.
 extern __shared__ __align__(16) unsigned char pick_smem[];
 constexpr size_t settle_smem_bytes(int nstrip) { return kBins * 12 + kSpreadCap * 8 + static_cast<size_t>(nstrip) * 8; }
 constexpr size_t pick_smem_bytes(int nstrip, int ngroups) { return kBins * 12 + kListCap * 8 + static_cast<size_t>(nstrip) * 8 + static_cast<size_t>(ngroups) * 6; }
 constexpr int kMaxRowStrips = (TLI_MAX_V + 6) / (4 * 32 * 8) + 1;
 constexpr size_t kPickSmemMax = pick_smem_bytes(kMaxRowStrips, kMaxGroups), kSettleSmemMax = settle_smem_bytes(kMaxRowStrips);
-static_assert(kSample * 4 <= kListCap * 8, "the sample takes the place of the list");
 __device__ __forceinline__ unsigned *bins() { return reinterpret_cast<unsigned *>(pick_smem); }
 __device__ __forceinline__ u64 *list() { return reinterpret_cast<u64 *>(pick_smem + kBins * 12); }
-__device__ __forceinline__ float *sample() { return reinterpret_cast<float *>(pick_smem + kBins * 12); }
 __device__ __forceinline__ double *strips() { return reinterpret_cast<double *>(pick_smem + kBins * 12) + S.room; }
 __device__ __forceinline__ float *group_max() { return reinterpret_cast<float *>(strips() + S.nstrip); }
 __device__ __forceinline__ unsigned short *group_list() { return reinterpret_cast<unsigned short *>(group_max() + S.ngroups); }
@@ -663,7 +661,7 @@ __device__ __noinline__ float floor_from_threads(int k, float tmax) {
 // the least of the threads' maxima.  -inf if they do not hold that much.
 __device__ __noinline__ float floor_from_groups(bool by_mass, unsigned want, float tmax) {
     const float m = S.m, *sg = group_max();
-    const float least = order_float(block_min(float_order(tmax > -INFINITY ? tmax : m)));
+    const float least = order_float(block_min(float_order(tmax > -1e30f ? tmax : m)));
     const float q = fmaxf(least - (m - least), -FLT_MAX), step = (m - q) * (1.f / kBins);
     if (!(step > 0.f) || !(step < INFINITY)) return -INFINITY;
     const float per = 1.f / step, sf = static_cast<float>(S.w.s);
@@ -831,16 +829,26 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
 
 // Two logits that the k-th largest (or the last one inside top-p) lies between but for bad luck, from up to 8192 elements
 // spread over the row: where the sample itself has that place, and four standard errors to both sides (fewer, if as many elements
-// as lie between would not fit `capacity`).  The sample is counted (weighed) in 1024 equal parts of the interval between its extremes.
+// as lie between would not fit `capacity`).  The sample is counted and weighed in 1024 equal parts of [q, m], what is below q with the first;
+// q: three times as far below m as the least of the threads' maxima.  (A logit of the type's lowest value is a mask to both.)
 struct Bracket { float low, high; };
-template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity) {
-    constexpr int EPV = Elt<DT>::kPerVec, total = kSample / EPV;
-    const bool whole = S.nvec <= total;
-    const float m = S.m;
-    float least = INFINITY;
-    __syncthreads();
-    constexpr int B = 4;
-    static_assert(total % (B * kPickThreads) == 0, "whole batches");
+template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity, float tmax) {
+    constexpr int EPV = Elt<DT>::kPerVec, total = kSample / EPV, B = 4;
+    static_assert(total % (B * kPickThreads) == 0 && kSample <= 8192, "whole batches; 8192 parts of 498 000 fit 32 bits");
+    const bool whole = S.nvec <= total, by_mass = !ask.k_on;
+    const float m = S.m, sf = static_cast<float>(S.w.s);
+    Bracket r;
+    r.low = -FLT_MAX; r.high = m;
+    float q = order_float(block_min(float_order(tmax > -1e30f ? tmax : m)));
+    q = m - 3.f * (m - q);
+    if (by_mass) q = fmaxf(q, m - 70.f * ask.tau);                 // (no weight worth a part is below that)
+    const float width = (m - q) * (1.f / kBins), per_bin = 1.f / width;
+    if (!(width > 0.f) || !(width < INFINITY) || !(per_bin < INFINITY)) return r;
+    const double share = whole ? 1.0 : static_cast<double>(total) / S.nvec, spare = whole ? 0.0 : 4.0 * sqrt(1.0 - share);
+    // by mass: (1-p) Z lies below the border, and the many small weights there are what a sample knows well; in units of
+    // 1/2^18 of it, each clipped at 1.9, from the smallest logit up.  By count: from the largest down.
+    const float unit = by_mass ? static_cast<float>(262144.0 / ((1.0 - static_cast<double>(ask.p)) * Z * share)) : 0.f;
+    unsigned *w = bins();
 #pragma unroll 1
     for (int j0 = threadIdx.x; j0 < total; j0 += B * kPickThreads) {
         uint4 raw[B];
@@ -857,74 +865,84 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
             unpack<DT>(raw[k], z);
 #pragma unroll
             for (int i = 0; i < EPV; ++i) {
-                if (z[i] > -INFINITY) least = fminf(least, z[i]);
-                sample()[i * total + j0 + k * kPickThreads] = z[i];
+                if (!(z[i] > -INFINITY)) continue;
+                const int up = max(min(static_cast<int>((z[i] - q) * per_bin), kBins - 1), 0);
+                if (by_mass) {
+                    const unsigned add = __float2uint_rn(fminf(ex2((z[i] - m) * sf) * unit, 498000.f));
+                    if (add) { atomicAdd(w + up, add); atomicAdd(w + kBins + up, 1u); }
+                } else {
+                    atomicAdd(w + (kBins - 1 - up), 1u);
+                }
             }
         }
     }
-    least = order_float(block_min(float_order(least)));
-    Bracket r;
-    r.low = -FLT_MAX; r.high = m;
-    const float width = (m - least) * (1.f / kBins), per_bin = 1.f / width;
-    if (!(width > 0.f) || !(width < INFINITY)) return r;           // (nothing seen but the largest value, or too wide for a float)
-    const double share = whole ? 1.0 : static_cast<double>(total) / S.nvec, spare = whole ? 0.0 : 4.0 * sqrt(1.0 - share);
-    const bool by_mass = !ask.k_on;
-    // by mass: (1-p) Z lies below the border, and the many small weights there are what a sample knows well; in units of
-    // 1/2^17 of it, each clipped at 1.9 (8192 of them fit 32 bits), from the smallest logit up
-    const float sf = static_cast<float>(S.w.s), unit = by_mass ? static_cast<float>(131072.0 / ((1.0 - static_cast<double>(ask.p)) * Z * share)) : 0.f;
-    auto bin_of = [&](float z) { return min(static_cast<int>((z - least) * per_bin), kBins - 1); };
-#pragma unroll 4
-    for (int j = threadIdx.x; j < kSample; j += kPickThreads) {
-        const float z = sample()[j];
-        if (!(z > -INFINITY)) continue;
-        if (by_mass) {
-            const unsigned add = __float2uint_rn(fminf(ex2((z - m) * sf) * unit, 249000.f));
-            if (add) atomicAdd(bins() + bin_of(z), add);
-        } else {
-            atomicAdd(bins() + (kBins - 1 - bin_of(z)), 1u);
+    __syncthreads();
+    uint4 *own = reinterpret_cast<uint4 *>(w) + threadIdx.x;       // four bins of each thread, out of shared memory for good
+    const uint4 a = own[0], c = by_mass ? own[kBins / 4] : a;
+    own[0] = make_uint4(0, 0, 0, 0);
+    own[kBins / 4] = own[0];
+    const unsigned x[4] = {a.x, a.y, a.z, a.w}, n[4] = {c.x, c.y, c.z, c.w};
+    const unsigned mine = a.x + a.y + a.z + a.w;
+    const unsigned run0 = block_prefix(mine).before;
+    // where the running measure reaches `at`, in bins, by proportion inside one; every thread looks at its own four
+    auto place = [&](double at, float *out) {
+        unsigned run = run0;
+        if (static_cast<double>(run0) < at && static_cast<double>(run0) + mine >= at) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (run < at && static_cast<double>(run) + x[i] >= at) *out = threadIdx.x * 4 + i + static_cast<float>((at - run) / x[i]);
+                run += x[i];
+            }
         }
-    }
-    double want, off;
+    };
+    float *at = reinterpret_cast<float *>(S.few);
+    if (threadIdx.x < 3) at[threadIdx.x] = -1.f;
+    double want = 262144.0, off;
     if (by_mass) {
-        want = 131072.0;
-        const int place = find_bin(131072, 0, 19, true).bin;
-        float square = 0.f;
-#pragma unroll 4
-        for (int j = threadIdx.x; j < kSample; j += kPickThreads) {
-            const float z = sample()[j], a = ex2((z - m) * sf) * unit;
-            if (z > -INFINITY && (bin_of(z) <= place || place < 0)) square += a * a;
-        }
-        off = spare * sqrt(block_prefix(static_cast<double>(square)).total) + 600.0;
+        __syncthreads();
+        place(want, at + 2);
+        __syncthreads();
+        const float here = at[2] < 0.f ? static_cast<float>(kBins) : at[2];
+        float square = 0.f;                                        // sum of the squared weights below the place, bin by bin from their mean
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (static_cast<float>(threadIdx.x * 4 + i) <= here && n[i]) square += static_cast<float>(x[i]) * static_cast<float>(x[i]) / static_cast<float>(n[i]);
+        off = spare * sqrt(block_prefix(static_cast<double>(square)).total) + 1200.0;
     } else {
         want = ask.k * share;
         off = spare * (sqrt(want) + 1.0);
     }
-    // the places in bins, by proportion inside a bin
-    auto place = [&](double at, bool keep) {
-        const BinAt f = find_bin(static_cast<u64>(fmax(1.0, at)), 0, 19, keep);
-        return f.bin < 0 ? -1.f : f.bin + static_cast<float>((at - static_cast<double>(f.before)) / static_cast<double>(f.measure));
-    };
 #pragma unroll 1
     for (int round = 0; round < 2; ++round) {
-        const float near = place(want - off, true), far = place(want + off, true);
+        __syncthreads();
+        if (threadIdx.x < 2) at[threadIdx.x] = -1.f;
+        __syncthreads();
+        place(fmax(1.0, want - off), at);
+        place(want + off, at + 1);
+        __syncthreads();
+        const float near = at[0], far = at[1];
         r.low = -FLT_MAX; r.high = m;
         if (by_mass) {
-            if (near > 0.f) r.low = least + near * width;
-            if (far >= 0.f) r.high = least + far * width;
+            if (near > 1.f) r.low = q + near * width;
+            if (far >= 0.f) r.high = q + far * width;
         } else {
-            if (far >= 0.f) r.low = m - far * width;
+            if (far >= 0.f && far < kBins - 1) r.low = m - far * width;
             if (want - off >= 1.0 && near > 0.f) r.high = m - near * width;
         }
         if (round) break;
         int inside = 0;
-#pragma unroll 4
-        for (int j = threadIdx.x; j < kSample; j += kPickThreads) inside += sample()[j] >= r.low && sample()[j] <= r.high;
+        const float last = far < 0.f ? static_cast<float>(kBins) : far;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float bin = static_cast<float>(threadIdx.x * 4 + i);
+            if (bin + 1.f > near && bin < last)
+                inside += static_cast<int>(static_cast<float>(n[i]) * (fminf(bin + 1.f, last) - fmaxf(bin, near)) + 0.5f);
+        }
         const double expected = block_sum(inside) / share;
         if (expected <= 0.9 * capacity) break;
         off *= fmax(0.4, 0.8 * capacity / expected);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kPickThreads) bins()[i] = 0;
     r.high = fminf(r.high, m);
     if (DT == TLI_BF16) {                                          // values of the row's type, so that keys and logits say the same
         r.low = fmaxf(__bfloat162float(__float2bfloat16_rd(r.low)), -FLT_MAX);
@@ -1233,7 +1251,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     if (ask.k_on) {
         floor = ask.k <= kPickThreads / 2 ? floor_from_threads(ask.k, tmax) : floor_from_groups(false, ask.k, tmax);
         if (floor == -INFINITY && ask.p_on && P.V > kListCap && ask.k <= kListCap * 3 / 4) {       // too few groups for that many: from a sample
-            floor = bracket<DT>(ask, Z, kListCap - ask.k).low;
+            floor = bracket<DT>(ask, Z, kListCap - ask.k, tmax).low;
             if (floor == -FLT_MAX) floor = -INFINITY;
         }
     } else if (ask.p_on && Z < 8192.0) {
@@ -1265,7 +1283,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
         }
     }
     if (ask.k_on || ask.p_on) {
-        const Bracket br = bracket<DT>(ask, Z, P.listcap);
+        const Bracket br = bracket<DT>(ask, Z, P.listcap, tmax);
         plan_row(P, row, PLAN_BRACKET, br.low, br.high, -1, zmin, Z);
         return;
     }
