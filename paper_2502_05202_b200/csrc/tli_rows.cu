@@ -476,7 +476,7 @@ template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 
     int few;
     do {
         const int shift = bin_shift(range);
-#pragma unroll 1
+#pragma unroll 4
         for (int i = threadIdx.x; i < n; i += kPickThreads) {
             const u64 e = list()[i], p = pos(e) - low;
             if (e >= edge && p <= range) {
@@ -490,7 +490,7 @@ template <int DT> __device__ __noinline__ u64 find_element(int n, u64 edge, u64 
         before = at.before;
         low += static_cast<u64>(at.bin) << shift;
         range = min(range - (static_cast<u64>(at.bin) << shift), (1ull << shift) - 1);
-#pragma unroll 1
+#pragma unroll 4
         for (int i = threadIdx.x; i < n; i += kPickThreads) {
             const u64 e = list()[i];
             if (e >= edge && pos(e) - low <= range) {
@@ -975,7 +975,7 @@ template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask,
             double mass = Z * r.unit;
             if (ask.k_on) {                                        // the mass that top-k leaves
                 u64 all = 0;
-#pragma unroll 1
+#pragma unroll 4
                 for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], r.unit);
                 mass = static_cast<double>(before + block_prefix(all).total);
             }
@@ -1062,7 +1062,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
 // The id that owns u * total among the listed elements >= edge.
 template <int DT> __device__ __noinline__ Draw draw_from_list(float u, int n, u64 edge, double unit) {
     u64 mine = 0;
-#pragma unroll 1
+#pragma unroll 4
     for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= edge) mine += mass_of<DT>(list()[i], unit);
     const u64 total = block_prefix(mine).total, target = static_cast<u64>(static_cast<double>(u) * static_cast<double>(total));
     u64 hit;
@@ -1114,56 +1114,42 @@ template <int DT> __device__ __noinline__ Draw draw_by_strips(Border border, flo
     if (strip == hit) *before = run;
     else if (lowest == INT_MAX && first <= last && last < end) *before = run - strips()[last];
     __syncthreads();
-    if (warp == 0) {
-        double base = *before, w_last = 0.0, w_hit = 0.0;
-        int id_last = -1, id_hit = -1;
-#pragma unroll 1
-        for (int q = 0; q < (1 << S.ulog) && id_hit < 0; ++q) {
-            const int v = (strip << (5 + S.ulog)) + q * 32 + lane, e0 = v * EPV - S.head;
-            const int one[1] = {v};
-            uint4 r1[1];
-            state_vectors<DT, 1>(one, r1);
-            const uint4 r = r1[0];
-            double x[EPV], sum = 0.0, w_mine = 0.0;
-            int id_mine = -1;
+    // the strip's vectors of every lane, one per warp (there are at most as many)
+    static_assert(kPickWarps >= 8, "a warp per vector of a strip");
+    const int e0 = ((strip << (5 + S.ulog)) + warp * 32 + lane) * EPV - S.head;
+    double x[EPV], sum = 0.0, w_mine = 0.0;
+    int id_mine = -1;
 #pragma unroll
-            for (int j = 0; j < EPV; ++j) {
-                const float z = vector_element<DT>(r, j);
-                x[j] = z > border.z || (z == border.z && e0 + j <= border.id) ? S.w(z) : 0.0;
-                sum += x[j];
-                if (x[j] > 0.0) { id_mine = e0 + j; w_mine = x[j]; }
-            }
-            double incl = sum;
+    for (int j = 0; j < EPV; ++j) x[j] = 0.0;
+    if (warp < (1 << S.ulog)) {
+        const int v[1] = {(strip << (5 + S.ulog)) + warp * 32 + lane};
+        uint4 r[1];
+        state_vectors<DT, 1>(v, r);
+        float z[EPV];
+        unpack<DT>(r[0], z);
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
-            }
-            const unsigned over = __ballot_sync(0xffffffffu, sum > 0.0 && base + incl > target), some = __ballot_sync(0xffffffffu, sum > 0.0);
-            if (some) {
-                const int src = 31 - __clz(some);
-                id_last = __shfl_sync(0xffffffffu, id_mine, src);
-                w_last = __shfl_sync(0xffffffffu, w_mine, src);
-            }
-            if (over) {
-                double c = base + (incl - sum), wt = w_mine;
-                int id = -1;
-#pragma unroll
-                for (int j = 0; j < EPV; ++j) {                    // the first whose running sum exceeds the target
-                    c += x[j];
-                    if (id < 0 && x[j] > 0.0 && c > target) { id = e0 + j; wt = x[j]; }
-                }
-                if (id < 0) id = id_mine;
-                const int src = __ffs(over) - 1;
-                id_hit = __shfl_sync(0xffffffffu, id, src);
-                w_hit = __shfl_sync(0xffffffffu, wt, src);
-            }
-            base += __shfl_sync(0xffffffffu, incl, 31);
+        for (int j = 0; j < EPV; ++j) {
+            x[j] = z[j] > border.z || (z[j] == border.z && e0 + j <= border.id) ? S.w(z[j]) : 0.0;
+            sum += x[j];
+            if (x[j] > 0.0) { id_mine = e0 + j; w_mine = x[j]; }
         }
-        if (lane == 0) {
-            S.found = static_cast<u64>(id_hit >= 0 ? id_hit : id_last);
-            *before = (id_hit >= 0 ? w_hit : w_last) / p.total;
+    }
+    const double front = *before + block_prefix(sum).before;       // (block_prefix begins with a barrier)
+    // the first lane whose running sum exceeds the target, else the last one that has any weight
+    const int hit_at = block_min(sum > 0.0 && front + sum > target ? static_cast<int>(threadIdx.x) : INT_MAX);
+    const int last_at = block_max(sum > 0.0 ? static_cast<int>(threadIdx.x) : -1);
+    if (static_cast<int>(threadIdx.x) == (hit_at < INT_MAX ? hit_at : last_at)) {
+        if (hit_at < INT_MAX) {
+            double c = front;
+            bool found = false;
+#pragma unroll
+            for (int j = 0; j < EPV; ++j) {                        // the first element whose running sum does (rounding: or the last)
+                c += x[j];
+                if (!found && x[j] > 0.0 && c > target) { found = true; id_mine = e0 + j; w_mine = x[j]; }
+            }
         }
+        S.found = static_cast<u64>(id_mine);
+        *before = w_mine / p.total;
     }
     __syncthreads();
     Draw d;
@@ -1294,21 +1280,19 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
 
 // ---- rows whose kept set has thousands of elements ----
 
-// One strip of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed; what lies from there down to
-// zlo goes to the row's list.  A weight costs 12 fp64 operations whether one lane of a warp wants them or 32, so the kept
-// logits are queued per warp and weighed 32 at a time.
+// Strips [strip, end) of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed, strip by strip; what
+// lies from there down to zlo goes to the row's list.  A weight costs 12 fp64 operations whether one lane of a warp wants it or
+// 32, so the kept logits are queued per warp and weighed 32 at a time.  The next strip is on its way while one is worked on.
 constexpr int kQueue = 32 * 9, kStash = 96;              // 31 and a vector of each lane; 64 and one element of each lane
 static_assert(kPickWarps * (kQueue * 4 + kStash * 8) <= kListCap * 8, "queues and stashes take the place of the list");
-template <int DT, int U> __device__ __forceinline__ void spread_strip(const RowsParams &P, RowPlan *plan, int row, int strip, float zlo, float zhi, int bid, bool weigh) {
+template <int DT, int U> __device__ __forceinline__ void spread_strips(const RowsParams &P, RowPlan *plan, int row, int strip, int end, float zlo, float zhi, int bid, bool weigh) {
     constexpr int EPV = Elt<DT>::kPerVec;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nvec = S.nvec;
     u64 *stash = list() + warp * kStash;
     float *queue = reinterpret_cast<float *>(list() + kPickWarps * kStash) + warp * kQueue;
-    const float gm = load_group<DT>(P.gmax, static_cast<size_t>(row) * P.nstrip * 32 + strip * 32 + lane);
-    const int nvec = S.nvec, v0 = strip * (32 * U) + lane;
-    const bool want = gm >= fminf(zhi, zlo);
-    double acc = 0.0;
-    int queued = 0, stashed = 0, count = 0;
+    const size_t groups = static_cast<size_t>(row) * P.nstrip * 32 + lane;
+    const float least = fminf(zhi, zlo);
+    int stashed = 0;
     auto flush = [&]() {                                           // the stash to the row's list
         __syncwarp();
         int at = 0;
@@ -1319,12 +1303,24 @@ template <int DT, int U> __device__ __forceinline__ void spread_strip(const Rows
         stashed = 0;
         __syncwarp();
     };
-    if (__any_sync(0xffffffffu, want)) {
-        uint4 raw[U];
+    uint4 next[U];
+    auto fetch = [&](int st, float gm) {
         int v[U];
 #pragma unroll
-        for (int q = 0; q < U; ++q) v[q] = want ? v0 + q * 32 : nvec;
-        state_vectors<DT, U>(v, raw);
+        for (int q = 0; q < U; ++q) v[q] = gm >= least ? st * (32 * U) + q * 32 + lane : nvec;
+        state_vectors<DT, U>(v, next);
+    };
+    float gm_after = strip + 1 < end ? load_group<DT>(P.gmax, groups + (strip + 1) * 32) : -INFINITY;
+    fetch(strip, load_group<DT>(P.gmax, groups + strip * 32));
+#pragma unroll 1
+    for (; strip < end; ++strip) {
+        uint4 raw[U];
+#pragma unroll
+        for (int q = 0; q < U; ++q) raw[q] = next[q];
+        if (strip + 1 < end) fetch(strip + 1, gm_after);
+        if (strip + 2 < end) gm_after = load_group<DT>(P.gmax, groups + (strip + 2) * 32);
+        double acc = 0.0;
+        int queued = 0, count = 0;
 #pragma unroll 1
         for (int q = 0; q < U; ++q) {
             const uint4 r = raw[0];
@@ -1332,7 +1328,7 @@ template <int DT, int U> __device__ __forceinline__ void spread_strip(const Rows
             for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
             float z[EPV];
             unpack<DT>(r, z);
-            const int e0 = (v0 + q * 32) * EPV - S.head;
+            const int e0 = (strip * (32 * U) + q * 32 + lane) * EPV - S.head;
             unsigned near = 0;
 #pragma unroll
             for (int i = 0; i < EPV; ++i) {
@@ -1360,15 +1356,17 @@ template <int DT, int U> __device__ __forceinline__ void spread_strip(const Rows
             __syncwarp();
         }
         count += queued;
-        if (weigh && lane < queued) acc += S.w(queue[lane]);
-        if (stashed) flush();
+        if (weigh) {
+            if (lane < queued) acc += S.w(queue[lane]);
+            acc = warp_sum(acc);
+        }
         __syncwarp();
+        if (lane == 0) {
+            StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
+            __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
+        }
     }
-    acc = warp_sum(acc);
-    if (lane == 0) {
-        StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
-        __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
-    }
+    if (stashed) flush();
 }
 
 // Such a row's border in its list, and the draw.
@@ -1395,7 +1393,7 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
         const int n = static_cast<int>(__ldcg(&plan->listed));
         Edge at = {0, 1.0};
         if (n <= P.listcap) {
-#pragma unroll 1
+#pragma unroll 8
             for (int i = tid; i < n; i += kPickThreads) list()[i] = __ldcg(P.lists + static_cast<size_t>(row) * P.listcap + i);
             __syncthreads();
             // (fewer than k in all is not something the bracket can say)
@@ -1409,7 +1407,7 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
 #pragma unroll 1
                 for (int i = tid; i < P.nstrip; i += kPickThreads) extra[i] = 0;
                 __syncthreads();
-#pragma unroll 1
+#pragma unroll 4
                 for (int i = tid; i < n; i += kPickThreads)
                     if (list()[i] >= at.edge) atomicAdd(extra + ((element_id(list()[i]) + S.head) / EPV >> (5 + S.ulog)), mass_of<DT>(list()[i], at.unit));
                 __syncthreads();
@@ -1442,7 +1440,7 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
     finish_row(P, row, 0, BORDER_APPLY, border, d.token, d.prob);
 }
 
-// The rows that the pick kernel left, by all blocks: each takes eight strips at a time (the next ones when it is done: the block
+// The rows that the pick kernel left, by all blocks: each takes some strips at a time (the next ones when it is done: the block
 // that ends last with a row settles it, which takes as long as several strips).
 template <int DT, int U>
 __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
@@ -1450,7 +1448,10 @@ __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = __ldcg(P.todo);
     if (rows == 0) return;
-    const int nchunk = (P.nstrip + kPickWarps - 1) / kPickWarps;
+    // strips of a warp at a time: some three turns for every block
+    const long long all = static_cast<long long>(rows) * P.nstrip;
+    const int each = static_cast<int>(min(8ll, max(1ll, all / (3ll * gridDim.x * kPickWarps))));
+    const int nchunk = (P.nstrip + kPickWarps * each - 1) / (kPickWarps * each);
     exp2_table_init(S.tab, tid);
     int *next = P.todo + 1 + P.B * P.R;
     for (;;) {
@@ -1469,8 +1470,9 @@ __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const 
         }
         enter_row<DT>(P, row, b, kSpreadCap);
         __syncthreads();
-        const int strip = task % nchunk * kPickWarps + (tid >> 5);
-        if (strip < P.nstrip) spread_strip<DT, U>(P, plan, row, strip, zlo, zhi, bid, P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f));
+        const int strip = (task % nchunk * kPickWarps + (tid >> 5)) * each;
+        if (strip < P.nstrip)
+            spread_strips<DT, U>(P, plan, row, strip, min(strip + each, P.nstrip), zlo, zhi, bid, P.sample || (P.top_p && __ldg(P.top_p + b) < 1.f));
         __threadfence();
         __syncthreads();
         if (tid == 0) S.listed = atomicAdd(&plan->done, 1);
