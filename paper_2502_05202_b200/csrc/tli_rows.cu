@@ -331,9 +331,9 @@ __device__ __forceinline__ int element_id(u64 e) { return static_cast<int>(kIdMa
 // with every step inlined and unrolled they were 300 to 540 KB and took two to ten times as long.  The steps are
 // functions that are called, their loops are not unrolled, and the block's state is in shared memory instead of registers.
 
-struct PickState {
+struct __align__(16) PickState {
     double tab[16];
-    u64 slot[kPickWarps];
+    alignas(16) u64 slot[kPickWarps];                  // (read as int4)
     u64 few[kPickThreads], few_mass[kPickThreads];     // a short list and its masses
     u64 found, before;
     int bin, listed;
