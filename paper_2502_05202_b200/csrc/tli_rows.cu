@@ -1376,9 +1376,15 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
     const RowAsk ask(P, b);
     const float zmin = __ldcg(&plan->zmin), zlo = __ldcg(&plan->zlo), zhi = __ldcg(&plan->zhi);
     const double Z = __ldcg(&plan->Z);
+    const bool bracketed = __ldcg(&plan->kind) == PLAN_BRACKET;
+    const int n = static_cast<int>(__ldcg(&plan->listed));
+    if (bracketed && n <= P.listcap) {
+#pragma unroll 8
+        for (int i = tid; i < n; i += kPickThreads) list()[i] = __ldcg(P.lists + static_cast<size_t>(row) * P.listcap + i);
+    }
     u64 above = 0;
     double mass = 0.0;
-#pragma unroll 1
+#pragma unroll 2
     for (int i = tid; i < P.nstrip; i += kPickThreads) {
         const double2 raw = __ldcg(reinterpret_cast<const double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + i));
         const StripSum ss = *reinterpret_cast<const StripSum *>(&raw);
@@ -1389,13 +1395,9 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
     above = block_prefix(above).total;
     mass = block_prefix(mass).total;
     Border border = {zhi, __ldcg(&plan->bid)};
-    if (__ldcg(&plan->kind) == PLAN_BRACKET) {
-        const int n = static_cast<int>(__ldcg(&plan->listed));
+    if (bracketed) {
         Edge at = {0, 1.0};
         if (n <= P.listcap) {
-#pragma unroll 8
-            for (int i = tid; i < n; i += kPickThreads) list()[i] = __ldcg(P.lists + static_cast<size_t>(row) * P.listcap + i);
-            __syncthreads();
             // (fewer than k in all is not something the bracket can say)
             if (!ask.k_on || above + n >= static_cast<u64>(ask.k)) at = border_in_list<DT>(ask, P.sample, zmin, Z, n, zhi, zlo, above, mass);
         }
@@ -1403,16 +1405,26 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
         if (at.edge && border.z <= zhi) {
             if (P.sample) {
                 // the kept elements of the list join their strips, in fixed point so that their order does not matter
-                u64 *extra = reinterpret_cast<u64 *>(bins());      // (1040 words at most)
-#pragma unroll 1
-                for (int i = tid; i < P.nstrip; i += kPickThreads) extra[i] = 0;
+                // (the bins hold a strip each; a row of the largest vocabulary can have one more)
+                static_assert(kMaxRowStrips <= kBins + 1, "one strip beyond the bins");
+                if (tid == 0) S.before = 0;
                 __syncthreads();
 #pragma unroll 4
-                for (int i = tid; i < n; i += kPickThreads)
-                    if (list()[i] >= at.edge) atomicAdd(extra + ((element_id(list()[i]) + S.head) / EPV >> (5 + S.ulog)), mass_of<DT>(list()[i], at.unit));
+                for (int i = tid; i < n; i += kPickThreads) {
+                    const u64 e = list()[i];
+                    if (e < at.edge) continue;
+                    const int strip = (element_id(e) + S.head) / EPV >> (5 + S.ulog);
+                    if (strip < kBins) add_mass(strip, mass_of<DT>(e, at.unit));
+                    else atomicAdd(&S.before, mass_of<DT>(e, at.unit));
+                }
                 __syncthreads();
+                const double part = 1.0 / at.unit;                 // (a power of two)
 #pragma unroll 1
-                for (int i = tid; i < P.nstrip; i += kPickThreads) strips()[i] += static_cast<double>(extra[i]) / at.unit;
+                for (int i = tid; i < P.nstrip; i += kPickThreads) {
+                    const unsigned *w = bins() + i;
+                    const u64 more = i < kBins ? w[0] + (static_cast<u64>(w[kBins]) << 19) + (static_cast<u64>(w[2 * kBins]) << 38) : S.before;
+                    strips()[i] += static_cast<double>(more) * part;
+                }
             }
         } else {                                                   // bad luck, or min-p above the bracket: the long way
             const Hint hint = {zlo, zhi, above, mass};

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, Optional
 
 import numpy as np
@@ -732,6 +733,24 @@ def tli_selftest_bounded_wait(ctx: int, polls: int = 2000, stream: Optional[int]
     return out.value == 1
 
 
+# The argument structs of the calls below as bytes: packing them is a third of the cost of filling a ctypes.Structure, which counts where
+# a call takes ten microseconds.  Native alignment ("@") lays them out as C does; "0P" pads the end.
+_PACK_SAMPLE = struct.Struct("@iiiiPqqPPPPPPPPPN").pack
+_PACK_FILTER = struct.Struct("@iiiiPqqPPPPPqqPPN").pack
+_PACK_EMBED = struct.Struct("@iiiiiPPqfPqP").pack
+_PACK_EMBED_GRAD = struct.Struct("@iiiiiiPPqfPqPN").pack
+
+
+def _packed_entries():
+    """The four entry points as functions of (ctx, packed struct, stream)."""
+    load()
+    lib = ctypes.CDLL(LIB_PATH)                                    # function objects of its own, the library is loaded once
+    entries = [lib.tli_sample, lib.tli_filter, lib.tli_embed, lib.tli_embed_grad]
+    for fn in entries:
+        fn.argtypes, fn.restype = [ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p], ctypes.c_int
+    return entries
+
+
 def _current_device() -> int:
     return torch._C._cuda_getDevice()
 
@@ -751,7 +770,8 @@ class Verifier:
         if tiled:
             tli_set_tiled(self.ctx, True)
         self._ws: Optional[torch.Tensor] = None
-        self._index, self._lib, self._plans = int(device), load(), {}
+        self._index, self._plans = int(device), {}
+        self._fn_sample, self._fn_filter, self._fn_embed, self._fn_embed_grad = _packed_entries()
         self._stream_ws: Dict[int, torch.Tensor] = {}
 
     def close(self) -> None:
@@ -802,26 +822,24 @@ class Verifier:
             ws = self._stream_ws[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
         return ws
 
-    def _plan(self, kind: str, key, make):
-        plan = self._plans.get((kind, key))
-        if plan is None:
-            if len(self._plans) > 1000:
-                self._plans.clear()
-            plan = self._plans[(kind, key)] = make()
+    def _plan(self, key, plan):
+        if len(self._plans) > 1000:
+            self._plans.clear()
+        self._plans[key] = plan
         return plan
 
-    def _call(self, name: str, args) -> None:
-        fn = getattr(self._lib, name)
+    def _call(self, fn, args: bytes) -> None:
+        """One of the entry points below on the current stream; ``args``: its argument struct, packed."""
         if _current_device() == self._index:
-            rc = fn(self.ctx, ctypes.byref(args), _raw_stream(self._index))
+            rc = fn(self.ctx, args, _raw_stream(self._index))
         else:
             with torch.cuda.device(self._index):
-                rc = fn(self.ctx, ctypes.byref(args), _raw_stream(self._index))
+                rc = fn(self.ctx, args, _raw_stream(self._index))
         if rc != TLI_OK:
-            raise TLIError(rc, name)
+            raise TLIError(rc, fn.__name__)
 
     def _row_plan(self, logits, side):
-        """(B, R, shape of a per-sequence tensor, shape of a per-row one, scratch bytes, filled argument structs)."""
+        """(shape of a per-sequence tensor, shape of a per-row one, scratch bytes, dtype, strides)."""
         B, R, _ = logits.shape
         dt = _logit_dtype(logits)
         _check_rows(self.ctx, logits, side, ())
@@ -829,18 +847,18 @@ class Verifier:
         if need == 0 or tli_filter_workspace_bytes(self.ctx, B, R, dt, side) != need:
             raise TLIError(TLI_ERR_UNSUPPORTED, "tli_sample_workspace_bytes")
         sb, sr, _ = logits.stride()
-        sample = tli_sample_args(B=B, R=R, dtype=dt, side=side, stride_b=sb, stride_r=sr, workspace_bytes=need)
-        filt = tli_filter_args(B=B, R=R, dtype=dt, side=side, stride_b=sb, stride_r=sr, workspace_bytes=need)
-        return B, R, (B,), (B, R), need, bytes(sample), bytes(filt)
+        return (B,), (B, R), need, (B, R, dt, side), sb, sr
 
     def _rows(self, logits, side, temperature, top_k, top_p, min_p):
         if logits.dim() != 3:
             raise ValueError("logits must be [B, R, V]")
-        plan = self._plan("rows", (logits.shape, logits.stride(), logits.dtype, side), lambda: self._row_plan(logits, side))
-        on = self._index
+        key = (logits.shape, logits.stride(), logits.dtype, side)
+        plan = self._plans.get(key)
+        if plan is None:
+            plan = self._plan(key, self._row_plan(logits, side))
+        on, shape = self._index, plan[0]
         if logits.get_device() != on:
             raise ValueError("logits must be on %s" % self.device)
-        shape = plan[2]
         for t, dtype in ((temperature, torch.float32), (top_k, torch.int32), (top_p, torch.float32), (min_p, torch.float32)):
             if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != on or not t.is_contiguous()):
                 raise ValueError("temperature, top_k, top_p and min_p must be contiguous float32, int32, float32 and float32 "
@@ -851,28 +869,22 @@ class Verifier:
                min_p=None) -> Dict[str, torch.Tensor]:
         """Draw one id per row of ``logits`` [B,R,V] under temperature, top-k, top-p and min-p (per sequence,
         ``None`` = off); on the drafter side from the ids inside the intersection.  Returns device tensors."""
-        _, _, _, shape, need, template, _ = self._rows(logits, side, temperature, top_k, top_p, min_p)
+        _, shape, need, head, sb, sr = self._rows(logits, side, temperature, top_k, top_p, min_p)
         if uniforms.dtype is not torch.float32 or uniforms.shape != shape or uniforms.get_device() != self._index or not uniforms.is_contiguous():
             raise ValueError("uniforms must be a contiguous float32 tensor of shape %s on %s" % (shape, self.device))
-        dev = self.device
-        tokens, prob, status = torch.empty((3, *shape), dtype=torch.int32, device=dev).unbind(0)     # one allocation for three
+        tokens, prob, status = torch.empty((3, *shape), dtype=torch.int32, device=self.device).unbind(0)     # one allocation for three
         prob = prob.view(torch.float32)
         ws = self._scratch(need)
-        a = tli_sample_args.from_buffer_copy(template)
-        a.logits = logits.data_ptr()
-        a.temperature = temperature.data_ptr()
-        a.top_k = None if top_k is None else top_k.data_ptr()
-        a.top_p = None if top_p is None else top_p.data_ptr()
-        a.min_p = None if min_p is None else min_p.data_ptr()
-        a.uniforms = uniforms.data_ptr()
-        a.tokens, a.prob, a.status, a.workspace = tokens.data_ptr(), prob.data_ptr(), status.data_ptr(), ws.data_ptr()
-        self._call("tli_sample", a)
+        self._call(self._fn_sample, _PACK_SAMPLE(
+            *head, logits.data_ptr(), sb, sr, temperature.data_ptr(), 0 if top_k is None else top_k.data_ptr(),
+            0 if top_p is None else top_p.data_ptr(), 0 if min_p is None else min_p.data_ptr(), uniforms.data_ptr(),
+            tokens.data_ptr(), prob.data_ptr(), status.data_ptr(), ws.data_ptr(), need))
         return {"tokens": tokens, "prob": prob, "status": status}
 
     def filter(self, logits, temperature, side: int = TLI_SIDE_TARGET, top_k=None, top_p=None, min_p=None,
                out=None) -> Dict[str, torch.Tensor]:
         """The rows of ``logits`` [B,R,V] with -inf outside the kept set (``out=logits``: in place)."""
-        _, _, _, shape, need, _, template = self._rows(logits, side, temperature, top_k, top_p, min_p)
+        _, shape, need, head, sb, sr = self._rows(logits, side, temperature, top_k, top_p, min_p)
         dev = self.device
         if out is None:
             out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
@@ -880,15 +892,11 @@ class Verifier:
             raise ValueError("out must have the logits' type, shape and device, and a contiguous vocabulary axis")
         status = torch.empty(shape, dtype=torch.int32, device=dev)
         ws = self._scratch(need)
-        a = tli_filter_args.from_buffer_copy(template)
-        a.logits = logits.data_ptr()
-        a.temperature = temperature.data_ptr()
-        a.top_k = None if top_k is None else top_k.data_ptr()
-        a.top_p = None if top_p is None else top_p.data_ptr()
-        a.min_p = None if min_p is None else min_p.data_ptr()
-        a.out, a.status, a.workspace = out.data_ptr(), status.data_ptr(), ws.data_ptr()
-        a.out_stride_b, a.out_stride_r, _ = out.stride()
-        self._call("tli_filter", a)
+        ob, orr, _ = out.stride()
+        self._call(self._fn_filter, _PACK_FILTER(
+            *head, logits.data_ptr(), sb, sr, temperature.data_ptr(), 0 if top_k is None else top_k.data_ptr(),
+            0 if top_p is None else top_p.data_ptr(), 0 if min_p is None else min_p.data_ptr(),
+            out.data_ptr(), ob, orr, status.data_ptr(), ws.data_ptr(), need))
         return {"logits": out, "status": status}
 
     def _table_rows(self, side: int) -> int:
@@ -911,8 +919,8 @@ class Verifier:
         stride, H = _matrix("table", table), table.shape[1]
         rows = torch.empty((*ids.shape, H), dtype=table.dtype, device=dev)
         table_ids = torch.empty(ids.shape, dtype=torch.int32, device=dev)
-        self._call("tli_embed", tli_embed_args(ids.numel(), H, _logit_dtype(table), ids_side, table_side, ids.data_ptr(), table.data_ptr(),
-                                               stride, scale, rows.data_ptr(), H, table_ids.data_ptr()))
+        self._call(self._fn_embed, _PACK_EMBED(ids.numel(), H, _logit_dtype(table), ids_side, table_side, ids.data_ptr(), table.data_ptr(), stride,
+                                               scale, rows.data_ptr(), H, table_ids.data_ptr()))
         return {"rows": rows, "table_ids": table_ids}
 
     def embed_grad(self, ids, grad, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET,
@@ -927,11 +935,13 @@ class Verifier:
             grad = grad.reshape(N, H)
         stride = _matrix("grad", grad)
         out = torch.empty((V, H), dtype=dtype or grad.dtype, device=dev)
-        need = self._plan("grad", (N, H), lambda: tli_embed_grad_workspace_bytes(self.ctx, N, H))
+        need = self._plans.get((N, H))
+        if need is None:
+            need = self._plan((N, H), tli_embed_grad_workspace_bytes(self.ctx, N, H))
         if need == 0:
             raise TLIError(TLI_ERR_UNSUPPORTED, "tli_embed_grad_workspace_bytes")
         ws = self._scratch(need)
-        self._call("tli_embed_grad", tli_embed_grad_args(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
+        self._call(self._fn_embed_grad, _PACK_EMBED_GRAD(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
                                                          grad.data_ptr(), stride, scale, out.data_ptr(), H, ws.data_ptr(), need))
         return {"grad": out}
 

@@ -58,3 +58,13 @@ def test_ids_carried_between_vocabularies():
     assert list(ro.table_ids([0, 1, 2, 3, -1], m, 5, 1, 0)) == [3, -1, 0, -1, -1]
     assert list(ro.table_ids([0, 1, 3, 4, 5, -2], m, 5, 0, 1)) == [2, -1, 0, -1, -1, -1]
     assert list(ro.table_ids([0, 4, 5], m, 5, 0, 0)) == [0, 4, -1]
+
+
+def test_packed_arguments_are_laid_out_as_the_structs():
+    for pack, cls in ((tli._PACK_SAMPLE, tli.tli_sample_args), (tli._PACK_FILTER, tli.tli_filter_args), (tli._PACK_EMBED, tli.tli_embed_args),
+                      (tli._PACK_EMBED_GRAD, tli.tli_embed_grad_args)):
+        values = [1.5 if t is ctypes.c_float else 3 + 7 * i for i, (_, t) in enumerate(cls._fields_)]
+        filled = cls.from_buffer_copy(bytes(ctypes.sizeof(cls)))
+        for (name, _), x in zip(cls._fields_, values):
+            setattr(filled, name, x)
+        assert pack(*values) == bytes(filled)
