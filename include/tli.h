@@ -461,8 +461,8 @@ int tli_shard_select(tli_ctx *ctx, const tli_verify_args *args, const void *rows
  * depend on timing.  Both calls are asynchronous on the stream, allocate
  * nothing, only launch kernels (they can be captured) and use of the context
  * only its maps: calls on one context may overlap if their workspaces and outputs
- * are distinct.  Errors as for tli_verify(); a context of tli_shard_create() is
- * refused.  The context's device must be current.
+ * are distinct.  Errors as for tli_verify(); a context of tli_shard_create(), and a
+ * call while another device than the context's is current, get TLI_ERR_ARG.
  */
 typedef struct {
     int32_t B;      /* sequences, >= 1 */
@@ -508,8 +508,8 @@ typedef struct {
     const float *top_p, *min_p;
 
     /* [device] out [B, R, V] in the rows' type: the logit where it is kept, -inf elsewhere.  May be
-     * `logits` itself with the same strides (in place); any other overlap with it, or of
-     * its rows with one another, is an error.  A flagged row is copied unchanged (so that a later
+     * `logits` itself with the same strides (in place); rows that overlap others of
+     * its own or of the logits are refused (TLI_ERR_ARG).  A flagged row is copied unchanged (so that a later
      * call flags it too), except that a row without ids (FALLBACK) becomes -inf. */
     void *out;
     int64_t out_stride_b, out_stride_r;

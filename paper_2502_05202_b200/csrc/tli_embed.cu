@@ -595,7 +595,7 @@ int tli_embed(tli_ctx *ctx, const tli_embed_args *a, void *cuda_stream) {
     const int rc = embed_side(ctx, a->ids_side, a->table_side, P.n_ids, V, P.map);
     if (rc != TLI_OK) return rc;
     if (a->N == 0) return TLI_OK;
-    if (!a->ids || !a->table || !a->out) return TLI_ERR_ARG;
+    if (!a->ids || !a->table || !a->out || !aligned4({a->ids, a->table_ids}) || !on_device(ctx)) return TLI_ERR_ARG;
     const size_t elt = a->dtype == TLI_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(a->table) % elt || reinterpret_cast<uintptr_t>(a->out) % elt) return TLI_ERR_ARG;
     if (a->table_stride < 0 || (a->N > 1 && a->out_stride < a->H)) return TLI_ERR_ARG;
@@ -633,7 +633,7 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *a, void *cuda_stream
     memset(&P, 0, sizeof P);
     const int rc = embed_side(ctx, a->ids_side, a->table_side, P.n_ids, P.V, P.map);
     if (rc != TLI_OK) return rc;
-    if (!a->out || (a->N > 0 && (!a->ids || !a->grad))) return TLI_ERR_ARG;
+    if (!a->out || (a->N > 0 && (!a->ids || !a->grad)) || !aligned4({a->ids}) || !on_device(ctx)) return TLI_ERR_ARG;
     const size_t ge = a->grad_dtype == TLI_F32 ? 4 : 2, oe = a->out_dtype == TLI_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(a->grad) % ge || reinterpret_cast<uintptr_t>(a->out) % oe) return TLI_ERR_ARG;
     if (a->grad_stride < 0 || (P.V > 1 && a->out_stride < a->H)) return TLI_ERR_ARG;

@@ -27,6 +27,7 @@
 #include <cuda_bf16.h>
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 
 namespace {
 
@@ -1669,6 +1670,31 @@ int run_rows(RowsParams &P, const tli_ctx *ctx, int32_t dtype, int32_t side, voi
 #undef TLI_ROWS
 }
 
+// The context's device is the current one (a launch elsewhere would read this device's pointers there).
+bool on_device(const tli_ctx *ctx) {
+    int current = -1;
+    return cudaGetDevice(&current) == cudaSuccess && current == ctx->device;
+}
+bool aligned4(std::initializer_list<const void *> pointers) {
+    uintptr_t bits = 0;
+    for (const void *p : pointers) bits |= reinterpret_cast<uintptr_t>(p);
+    return bits % 4 == 0;
+}
+// Whether rows of V elements written at `out` meet any read at `in` other than themselves.
+bool rows_collide(const char *in, int64_t sb, int64_t sr, const char *out, int64_t ob, int64_t orr, int64_t B, int64_t R, int64_t V, int64_t elt) {
+    if (B == 1) sb = ob = 0;
+    if (R == 1) sr = orr = 0;
+    if (in == out && sb == ob && sr == orr) return false;          // in place
+    const int64_t in_span = ((B - 1) * sb + (R - 1) * sr + V) * elt, out_span = ((B - 1) * ob + (R - 1) * orr + V) * elt;
+    if (out + out_span <= in || in + in_span <= out) return false;
+    // rows of one pitch can lie in one another's gaps
+    if (sb != ob || sr != orr) return true;
+    const int64_t pitch = sr == 0 ? sb : sb == 0 ? sr : std::min(sb, sr), apart = (out > in ? out - in : in - out);
+    if (pitch == 0 || sb % pitch || sr % pitch || apart % elt) return true;
+    const int64_t gap = apart / elt % pitch;
+    return gap < V || gap > pitch - V;
+}
+
 // What tli_sample() and tli_filter() check alike.
 int check_rows(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, int32_t side, const void *logits, int64_t sb, int64_t sr,
                const float *tau, const void *workspace, size_t workspace_bytes) {
@@ -1676,7 +1702,7 @@ int check_rows(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, int32_t 
     if (static_cast<long long>(B) * R > TLI_MAX_B) return TLI_ERR_UNSUPPORTED;
     if (dtype != TLI_F32 && dtype != TLI_BF16) return TLI_ERR_ARG;
     if (side != TLI_SIDE_TARGET && side != TLI_SIDE_DRAFTER) return TLI_ERR_ARG;
-    if (!logits || !tau) return TLI_ERR_ARG;
+    if (!logits || !tau || !on_device(ctx)) return TLI_ERR_ARG;
     const size_t elt = dtype == TLI_F32 ? 4 : 2;
     if (reinterpret_cast<uintptr_t>(logits) % elt || sb < 0 || sr < 0) return TLI_ERR_ARG;
     const size_t need = rows_workspace(ctx, B, R, dtype, side);
@@ -1701,6 +1727,7 @@ int tli_sample(tli_ctx *ctx, const tli_sample_args *a, void *cuda_stream) {
                               a->workspace, a->workspace_bytes);
     if (rc != TLI_OK) return rc;
     if (!a->uniforms || !a->tokens) return TLI_ERR_ARG;
+    if (!aligned4({a->temperature, a->top_k, a->top_p, a->min_p, a->uniforms, a->tokens, a->prob, a->status})) return TLI_ERR_ARG;
     RowsParams P;
     memset(&P, 0, sizeof P);
     P.B = a->B; P.R = a->R; P.sample = 1;
@@ -1724,6 +1751,9 @@ int tli_filter(tli_ctx *ctx, const tli_filter_args *a, void *cuda_stream) {
     if (a->R > 1 && orr < V) return TLI_ERR_ARG;
     if (a->B > 1 && ob < V) return TLI_ERR_ARG;
     if (a->B > 1 && a->R > 1 && !(ob >= (a->R - 1) * orr + V || orr >= (a->B - 1) * ob + V)) return TLI_ERR_ARG;
+    if (!aligned4({a->temperature, a->top_k, a->top_p, a->min_p, a->status})) return TLI_ERR_ARG;
+    if (rows_collide(reinterpret_cast<const char *>(a->logits), a->stride_b, a->stride_r, reinterpret_cast<const char *>(a->out), ob, orr, a->B, a->R, V,
+                     static_cast<int64_t>(elt))) return TLI_ERR_ARG;
     RowsParams P;
     memset(&P, 0, sizeof P);
     P.B = a->B; P.R = a->R; P.sample = 0;

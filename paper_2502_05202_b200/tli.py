@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+import threading
 from typing import Dict, Optional
 
 import numpy as np
@@ -772,7 +773,7 @@ class Verifier:
         self._ws: Optional[torch.Tensor] = None
         self._index, self._plans = int(device), {}
         self._fn_sample, self._fn_filter, self._fn_embed, self._fn_embed_grad = _packed_entries()
-        self._stream_ws: Dict[int, torch.Tensor] = {}
+        self._kept = threading.local()
 
     def close(self) -> None:
         if self.ctx:
@@ -810,16 +811,18 @@ class Verifier:
         tli_draft_sample(self.ctx, args)
         return out
 
-    # The calls below may overlap others on this context: each stream has scratch of its own, in whose order the calls on it
-    # use it, and so has every captured call.  What depends on shapes alone is worked out once per shape.
+    # The calls below may overlap others on this context.  Scratch is kept per thread and stream (on one stream calls use it one
+    # after the other; two threads could interleave the kernels of theirs), a captured call has its own.  What depends on
+    # shapes alone is worked out once per shape.
 
     def _scratch(self, need: int) -> torch.Tensor:
-        if torch._C._cuda_isCurrentStreamCapturing():
+        if torch._C._cuda_isCurrentStreamCapturing() or _current_device() != self._index:
             return torch.empty(need, dtype=torch.uint8, device=self.device)
+        kept = self._kept.__dict__
         stream = _raw_stream(self._index)
-        ws = self._stream_ws.get(stream)
+        ws = kept.get(stream)
         if ws is None or ws.numel() < need:
-            ws = self._stream_ws[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
+            ws = kept[stream] = torch.empty(need, dtype=torch.uint8, device=self.device)
         return ws
 
     def _plan(self, key, plan):
@@ -872,8 +875,9 @@ class Verifier:
         _, shape, need, head, sb, sr = self._rows(logits, side, temperature, top_k, top_p, min_p)
         if uniforms.dtype is not torch.float32 or uniforms.shape != shape or uniforms.get_device() != self._index or not uniforms.is_contiguous():
             raise ValueError("uniforms must be a contiguous float32 tensor of shape %s on %s" % (shape, self.device))
-        tokens, prob, status = torch.empty((3, *shape), dtype=torch.int32, device=self.device).unbind(0)     # one allocation for three
-        prob = prob.view(torch.float32)
+        prob = torch.empty_like(uniforms)                          # (cheaper than torch.empty with a shape and a device)
+        tokens = torch.empty_like(uniforms, dtype=torch.int32)
+        status = torch.empty_like(tokens)
         ws = self._scratch(need)
         self._call(self._fn_sample, _PACK_SAMPLE(
             *head, logits.data_ptr(), sb, sr, temperature.data_ptr(), 0 if top_k is None else top_k.data_ptr(),
@@ -885,12 +889,11 @@ class Verifier:
                out=None) -> Dict[str, torch.Tensor]:
         """The rows of ``logits`` [B,R,V] with -inf outside the kept set (``out=logits``: in place)."""
         _, shape, need, head, sb, sr = self._rows(logits, side, temperature, top_k, top_p, min_p)
-        dev = self.device
         if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+            out = torch.empty_like(logits)
         elif out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index or (out.shape[2] > 1 and out.stride(2) != 1):
             raise ValueError("out must have the logits' type, shape and device, and a contiguous vocabulary axis")
-        status = torch.empty(shape, dtype=torch.int32, device=dev)
+        status = torch.empty(shape, dtype=torch.int32, device=self.device)
         ws = self._scratch(need)
         ob, orr, _ = out.stride()
         self._call(self._fn_filter, _PACK_FILTER(
@@ -916,9 +919,9 @@ class Verifier:
         V, dev = self._table_rows(table_side), self.device
         if table.dim() != 2 or table.shape[0] != V or table.get_device() != self._index:
             raise ValueError("table must be [%d, H] on %s" % (V, dev))
-        stride, H = _matrix("table", table), table.shape[1]
-        rows = torch.empty((*ids.shape, H), dtype=table.dtype, device=dev)
-        table_ids = torch.empty(ids.shape, dtype=torch.int32, device=dev)
+        stride, H = _matrix("table", table), table.shape[1]        # (H 1: any stride will do)
+        rows = table.new_empty((*ids.shape, H))
+        table_ids = torch.empty_like(ids)
         self._call(self._fn_embed, _PACK_EMBED(ids.numel(), H, _logit_dtype(table), ids_side, table_side, ids.data_ptr(), table.data_ptr(), stride,
                                                scale, rows.data_ptr(), H, table_ids.data_ptr()))
         return {"rows": rows, "table_ids": table_ids}

@@ -145,9 +145,9 @@ def test_gradient_of_long_and_short_runs(kind):
             check_grad(v, m, ids, torch.randn(N, H, device="cuda").to(gdtype), 1.0, T, T, torch.float32)
 
 
-@pytest.mark.parametrize("N", [65535, 65536, 65537, 150001])
+@pytest.mark.parametrize("N", [65535, 65536, 65537, 131072, 131073, 150001])
 def test_gradient_of_many_tokens(N):
-    """The sort of one CTA and of several; a vocabulary that needs both digits."""
+    """The sort of one cluster and of many CTAs; a vocabulary that needs both digits."""
     rng = np.random.default_rng(N)
     V_t, V_d = 70001, 5
     m = np.array([4, -1, 70000, 0, 1], np.int32)

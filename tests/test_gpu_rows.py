@@ -278,6 +278,64 @@ def test_captured_replayed_and_overlapping_calls():
         assert all(torch.equal(g, want[i]) for g in got[i])
 
 
+def test_masks_of_the_lowest_value_beside_a_large_kept_set():
+    """Flat rows with most ids masked by the type's lowest value or -inf: the sample that brackets the border sees the masks too."""
+    rng = np.random.default_rng(19)
+    V = 70001
+    v, part = verifier(rng, V, T)
+    table = [(1.0, 0, 0.9, 0.0), (1.0, 0, 0.99, 0.0), (1.3, 9000, 1.0, 0.0), (1.0, 3000, 0.9, 0.0), (1.0, 12000, 0.95, 0.0), (1.0, 0, 0.97, 1e-3)]
+    for dtype in (wl.F32, wl.BF16):
+        lowest = torch.finfo(torch.bfloat16 if dtype == wl.BF16 else torch.float32).min
+        z = rng.normal(-9, 1.5, (len(table), 3, V))
+        z[:, 1][:, rng.random(V) < 0.6] = lowest
+        z[:, 2][:, rng.random(V) < 0.6] = -INF
+        check(v, T, part, to_dtype(z, dtype), asks(len(table), table), numbers(rng, (len(table), 3)))
+
+
+def test_calls_from_several_threads():
+    """Threads that share a Verifier and a stream: their kernels may interleave, their scratch may not."""
+    import threading
+    rng = np.random.default_rng(20)
+    V, B, R = 30000, 18, 2
+    v, part = verifier(rng, V, T)
+    tau, k, p, mp = (torch.from_numpy(x).cuda() for x in asks(B))
+    z = [to_dtype(rng.normal(0, 1 + i, (B, R, V)), wl.BF16).cuda() for i in range(4)]
+    u = [torch.from_numpy(numbers(rng, (B, R))).cuda() for _ in range(4)]
+    want = [v.sample(z[i], tau, u[i], top_k=k, top_p=p, min_p=mp)["tokens"] for i in range(4)]
+    torch.cuda.synchronize()
+    got = [[] for _ in range(4)]
+
+    def work(i):
+        for _ in range(30):
+            got[i].append(v.sample(z[i], tau, u[i], top_k=k, top_p=p, min_p=mp)["tokens"])
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(4):
+        assert len(got[i]) == 30 and all(torch.equal(g, want[i]) for g in got[i])
+
+
+def test_output_rows_between_input_rows():
+    """An output that lies in the gaps of the input's rows is fine, one that meets them is refused."""
+    rng = np.random.default_rng(21)
+    V, B, R = 1000, 3, 2
+    v, _ = verifier(rng, V, T)
+    buf = torch.from_numpy(rng.normal(0, 2, (B, R, 2, V)).astype(np.float32)).cuda()
+    tau, k = torch.ones(B, device="cuda"), torch.full((B,), 7, dtype=torch.int32, device="cuda")
+    want = v.filter(buf[:, :, 0].contiguous(), tau, top_k=k)["logits"]
+    v.filter(buf[:, :, 0], tau, top_k=k, out=buf[:, :, 1])
+    assert torch.equal(buf[:, :, 1], want)
+    flat = torch.randn(B * R * V + 8, device="cuda")
+    with pytest.raises(tli.TLIError):
+        v.filter(flat[:B * R * V].view(B, R, V), tau, top_k=k, out=flat[8:].view(B, R, V))
+    with pytest.raises(tli.TLIError):
+        v.filter(flat[:R * V].view(1, R, V), tau[:1], top_k=k[:1], out=flat[V:V + R * V].view(1, R, V))
+
+
 def test_refusals():
     rng = np.random.default_rng(18)
     V = 100
@@ -308,6 +366,8 @@ def test_refusals():
         assert call(B=65536) == tli.TLI_ERR_UNSUPPORTED
         for bad in (dict(workspace=None), dict(workspace=ws.data_ptr() + 16), dict(workspace_bytes=ws.numel() - 1)):
             assert call(**bad) == tli.TLI_ERR_WORKSPACE, bad
+    for bad in (dict(uniforms=u.data_ptr() + 2), dict(tokens=tok.data_ptr() + 1), dict(top_k=tok.data_ptr() + 2)):
+        assert sample(**bad) == tli.TLI_ERR_ARG, bad
     assert sample(uniforms=None) == tli.TLI_ERR_ARG and sample(tokens=None) == tli.TLI_ERR_ARG
     for bad in (dict(out=None), dict(out=z.data_ptr() + 1), dict(out_stride_r=V - 1), dict(out_stride_b=3 * V - 1), dict(out_stride_b=-1)):
         assert filt(**bad) == tli.TLI_ERR_ARG, bad
