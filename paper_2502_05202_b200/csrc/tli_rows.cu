@@ -1237,8 +1237,8 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     float floor = -INFINITY;
     if (ask.k_on) {
         floor = ask.k <= kPickThreads / 2 ? floor_from_threads(ask.k, tmax) : floor_from_groups(false, ask.k, tmax);
-        if (floor == -INFINITY && ask.p_on && P.V > kListCap && ask.k <= kListCap * 3 / 4) {       // too few groups for that many: from a sample
-            floor = bracket<DT>(ask, Z, kListCap - ask.k, tmax).low;
+        if (floor == -INFINITY && ask.p_on && P.V > kListCap && ask.k <= P.listcap * 3 / 4) {      // too few groups for that many: from a sample
+            floor = bracket<DT>(ask, Z, P.listcap - ask.k, tmax).low;
             if (floor == -FLT_MAX) floor = -INFINITY;
         }
     } else if (ask.p_on && Z < 8192.0) {
@@ -1248,10 +1248,9 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     const float zlow = ask.p_on ? fmaxf(floor, -FLT_MAX) : fmaxf(floor, zmin);
     list_groups(zlow, tmax);
     // Every listed group has an element.  Without a floor only short and mostly masked rows are worth a try; and beyond some 4096
-    // vectors to read again (4 ns each for this one block) all blocks together are faster, except that they do not do
-    // top-k with top-p.
+    // vectors to read again (4 ns each for this one block) all blocks together are faster.
     const int vectors = S.ng * (P.coarse << P.ulog);
-    const bool worth = P.V <= kListCap || (ok ? vectors <= 4096 || (ask.k_on && ask.p_on && S.ng <= kListCap) : S.ng <= 256);
+    const bool worth = P.V <= kListCap || (ok ? vectors <= 4096 : S.ng <= 256);
     const int n = worth ? gather<DT>(zlow) : INT_MAX;
     // (fewer than k above a sampled floor: there may be more below it)
     const bool whole = !(ask.k_on && n < ask.k && zlow == floor);
@@ -1268,6 +1267,10 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
             finish_row(P, row, 0, BORDER_APPLY, border_of<DT>(at.edge), d.token, d.prob);
             return;
         }
+    }
+    if (ask.k_on && ok && ask.k <= P.listcap * 3 / 4) {            // all that top-k can keep goes to the list
+        plan_row(P, row, PLAN_BRACKET, floor, m, -1, zmin, Z);
+        return;
     }
     if (ask.k_on || ask.p_on) {
         const Bracket br = bracket<DT>(ask, Z, P.listcap, tmax);
