@@ -1284,18 +1284,52 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
 
 // ---- rows whose kept set has thousands of elements ----
 
+// Which of a vector's elements are at least `least`, a bit each, and their order: fp32 element i is bit i; bf16 element 2k + h (half
+// h of word k) is bit 16h + k, so that one packed comparison and one and-or find two.
+template <int DT> struct Least {
+    float f;
+    __nv_bfloat162 b;
+    __device__ __forceinline__ explicit Least(float least) : f(least), b(__bfloat162bfloat162(__float2bfloat16_ru(least))) {}
+    __device__ __forceinline__ unsigned bits(const uint4 &r) const {
+        if constexpr (DT == TLI_F32) {
+            return static_cast<unsigned>(__uint_as_float(r.x) >= f) | static_cast<unsigned>(__uint_as_float(r.y) >= f) << 1 |
+                   static_cast<unsigned>(__uint_as_float(r.z) >= f) << 2 | static_cast<unsigned>(__uint_as_float(r.w) >= f) << 3;
+        } else {
+            auto two = [this](uint32_t x) { return __hge2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&x), b); };
+            return (two(r.x) & 0x10001u) | (two(r.y) & 0x20002u) | (two(r.z) & 0x40004u) | (two(r.w) & 0x80008u);
+        }
+    }
+    // the same order for a bit per element in increasing order
+    __device__ __forceinline__ static unsigned arranged(unsigned x) {
+        if (DT == TLI_F32) return x & 0xfu;
+        x = (x & 0x55u) | (x & 0xaau) << 15;
+        x = (x | x >> 1) & 0x330033u;
+        return (x | x >> 2) & 0xf000fu;
+    }
+    static constexpr int kVectors = DT == TLI_F32 ? 8 : 4;         // of one word of bits, four places apart
+    __device__ __forceinline__ static int vector(int bit) { return (DT == TLI_F32 ? bit : bit & 15) >> 2; }
+    __device__ __forceinline__ static int element(int bit) { return DT == TLI_F32 ? bit & 3 : (bit & 3) * 2 + (bit >> 4); }
+};
+
 // Strips [strip, end) of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed, strip by strip; what
-// lies from there down to zlo goes to the row's list.  A weight costs 12 fp64 operations whether one lane of a warp wants it or
-// 32, so the kept logits are queued per warp and weighed 32 at a time.  The next strip is on its way while one is worked on.
-constexpr int kQueue = 32 * 9, kStash = 96;              // 31 and a vector of each lane; 64 and one element of each lane
-static_assert(kPickWarps * (kQueue * 4 + kStash * 8) <= kListCap * 8, "queues and stashes take the place of the list");
+// lies from there down to zlo goes to the row's list.  Every lane finds its candidates as bits first, then takes them one by one
+// from a copy of its vectors in shared memory (they cannot be indexed in registers): what an element costs that is neither kept nor
+// near the border is one comparison.  The next strip is on its way while one is worked on.
+constexpr int kStash = 96;                               // 64 and one element of each lane
+constexpr int kStage = 8 * 32;                           // vectors of a strip at most
+static_assert(kPickWarps * (kStage * 16 + kStash * 8) <= kSpreadCap * 8, "strips and stashes take the place of the list");
 template <int DT, int U> __device__ __forceinline__ void spread_strips(const RowsParams &P, RowPlan *plan, int row, int strip, int end, float zlo, float zhi, int bid, bool weigh) {
-    constexpr int EPV = Elt<DT>::kPerVec;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nvec = S.nvec;
-    u64 *stash = list() + warp * kStash;
-    float *queue = reinterpret_cast<float *>(list() + kPickWarps * kStash) + warp * kQueue;
+    using L = Least<DT>;
+    constexpr int EPV = Elt<DT>::kPerVec, NW = (U + L::kVectors - 1) / L::kVectors;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nvec = S.nvec, head = S.head;
+    const uint4 *vec0 = S.vec0;
+    const uint32_t *mask = S.mask;
+    const Weights w = S.w;
+    uint4 *stage = reinterpret_cast<uint4 *>(list()) + warp * kStage + lane;
+    u64 *stash = list() + kPickWarps * kStage * 2 + warp * kStash;
     const size_t groups = static_cast<size_t>(row) * P.nstrip * 32 + lane;
-    const float least = fminf(zhi, zlo);
+    const L least(fminf(zhi, zlo));
+    const bool ties = bid >= 0;                                    // (then all of them: min-p's border)
     int stashed = 0;
     auto flush = [&]() {                                           // the stash to the row's list
         __syncwarp();
@@ -1308,63 +1342,76 @@ template <int DT, int U> __device__ __forceinline__ void spread_strips(const Row
         __syncwarp();
     };
     uint4 next[U];
+    unsigned in[U];                                                // the mask's bits of the vectors
+#pragma unroll
+    for (int q = 0; q < U; ++q) in[q] = ~0u;
     auto fetch = [&](int st, float gm) {
         int v[U];
 #pragma unroll
-        for (int q = 0; q < U; ++q) v[q] = gm >= least ? st * (32 * U) + q * 32 + lane : nvec;
-        state_vectors<DT, U>(v, next);
+        for (int q = 0; q < U; ++q) v[q] = gm >= least.f ? st * (32 * U) + q * 32 + lane : nvec;
+        row_vectors<DT, U>(vec0, S.row, head, P.V, nvec, nullptr, v, next);
+        if (mask) {
+#pragma unroll
+            for (int q = 0; q < U; ++q)
+                if (v[q] < nvec) in[q] = mask_bits(mask, v[q] * EPV - head);
+        }
     };
     float gm_after = strip + 1 < end ? load_group<DT>(P.gmax, groups + (strip + 1) * 32) : -INFINITY;
     fetch(strip, load_group<DT>(P.gmax, groups + strip * 32));
 #pragma unroll 1
     for (; strip < end; ++strip) {
-        uint4 raw[U];
+        unsigned bits[NW];
 #pragma unroll
-        for (int q = 0; q < U; ++q) raw[q] = next[q];
+        for (int i = 0; i < NW; ++i) bits[i] = 0;
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+            stage[q * 32] = next[q];                               // (read by this lane only)
+            unsigned x = least.bits(next[q]);
+            if (mask) x &= L::arranged(in[q]);
+            bits[q / L::kVectors] |= x << q % L::kVectors * 4;
+        }
         if (strip + 1 < end) fetch(strip + 1, gm_after);
         if (strip + 2 < end) gm_after = load_group<DT>(P.gmax, groups + (strip + 2) * 32);
+        const int id0 = (strip * (32 * U) + lane) * EPV - head;
         double acc = 0.0;
-        int queued = 0, count = 0;
-#pragma unroll 1
-        for (int q = 0; q < U; ++q) {
-            const uint4 r = raw[0];
+        int count = 0, base = 0;
+        unsigned now = bits[0];
+        if (NW > 1 && now == 0) { now = bits[NW - 1]; base = L::kVectors; bits[NW - 1] = 0; }
+        while (__any_sync(0xffffffffu, now != 0)) {                // two of each lane at a time
+            float z[2];
+            int id[2];
+            bool kept[2];
 #pragma unroll
-            for (int k = 0; k + 1 < U; ++k) raw[k] = raw[k + 1];
-            float z[EPV];
-            unpack<DT>(r, z);
-            const int e0 = (strip * (32 * U) + q * 32 + lane) * EPV - S.head;
-            unsigned near = 0;
-#pragma unroll
-            for (int i = 0; i < EPV; ++i) {
-                const bool kept = z[i] > zhi || (z[i] == zhi && e0 + i <= bid);
-                const unsigned who = __ballot_sync(0xffffffffu, kept);
-                if (kept) queue[queued + __popc(who & ((1u << lane) - 1u))] = z[i];
-                queued += __popc(who);
-                near |= static_cast<unsigned>(!kept && z[i] >= zlo) << i;
-            }
-            while (__any_sync(0xffffffffu, near != 0)) {           // one of each lane at a time
-                if (stashed > kStash - 32) flush();
-                const unsigned who = __ballot_sync(0xffffffffu, near != 0);
-                if (near) {
-                    const int i = __ffs(near) - 1;
-                    stash[stashed + __popc(who & ((1u << lane) - 1u))] = element_of<DT>(vector_element<DT>(r, i), e0 + i);
-                    near &= near - 1;
+            for (int r = 0; r < 2; ++r) {
+                z[r] = -INFINITY; id[r] = 0;
+                if (now) {
+                    const int bit = __ffs(now) - 1, v = (base + L::vector(bit)) * 32, i = L::element(bit);
+                    now &= now - 1;
+                    if constexpr (DT == TLI_F32) z[r] = reinterpret_cast<const float *>(stage + v)[i];
+                    else z[r] = __uint_as_float(static_cast<uint32_t>(reinterpret_cast<const unsigned short *>(stage + v)[i]) << 16);
+                    id[r] = id0 + v * EPV + i;
+                    if (NW > 1 && now == 0) { now = bits[NW - 1]; base = L::kVectors; bits[NW - 1] = 0; }
                 }
+                kept[r] = z[r] > zhi || (ties && z[r] == zhi);
+                count += kept[r];
+            }
+            if (weigh && __any_sync(0xffffffffu, kept[0] || kept[1])) {
+                const double w0 = w(z[0]), w1 = w(z[1]);
+                acc += kept[0] ? w0 : 0.0;
+                acc += kept[1] ? w1 : 0.0;
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const bool near = !kept[r] && z[r] >= zlo;
+                const unsigned who = __ballot_sync(0xffffffffu, near);
+                if (who == 0) continue;
+                if (stashed > kStash - 32) flush();
+                if (near) stash[stashed + __popc(who & ((1u << lane) - 1u))] = element_of<DT>(z[r], id[r]);
                 stashed += __popc(who);
             }
-            __syncwarp();
-            while (queued >= 32) {
-                queued -= 32; count += 32;
-                if (weigh) acc += S.w(queue[queued + lane]);
-            }
-            __syncwarp();
         }
-        count += queued;
-        if (weigh) {
-            if (lane < queued) acc += S.w(queue[lane]);
-            acc = warp_sum(acc);
-        }
-        __syncwarp();
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (weigh) acc = warp_sum(acc);
         if (lane == 0) {
             StripSum ss; ss.S = acc; ss.m = 0.f; ss.pad = count;
             __stcg(reinterpret_cast<double2 *>(P.ssum + static_cast<size_t>(row) * P.nstrip + strip), *reinterpret_cast<const double2 *>(&ss));
