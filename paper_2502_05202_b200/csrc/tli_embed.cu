@@ -68,7 +68,9 @@ template <int DT> __device__ __forceinline__ void set_element(void *p, long long
 
 constexpr int kEmbUnroll = 4;
 
-// VEC: rows of both sides lie on 16-byte boundaries and H is a whole number of vectors; otherwise element by element
+// VEC: rows of both sides lie on 16-byte boundaries and H is a whole number of vectors; otherwise element by element.
+// 16 384 bf16 rows of 4096: 134 MB written and 58 MB of distinct rows read in 32 us (29.4 at the measured copy bandwidth).  48 rows of
+// 2048: 2.1 us, the chain id -> map -> row.
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kEmbThreads) tli_embed_kernel(const __grid_constant__ EmbedParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -251,7 +253,8 @@ __device__ void fill_zero(const GradParams &P, unsigned cta, unsigned n) {
 }
 
 // The first cluster sorts, the others fill dW with zeros.  (Two passes of one cluster of eight and two barriers each against
-// eight more launches; the fill hides it up to some 10^5 tokens.)
+// eight more launches; the fill hides it up to some 10^5 tokens.)  49 152 fp32 rows of 2048 (403 MB) in 71 us, 5.7 TB/s: the fill has the SMs of
+// the clusters that fit together, 112 of 148.
 template <int OT>
 __global__ void __launch_bounds__(kSortThreads) tli_grad_sort_kernel(const __grid_constant__ GradParams P) {
     extern __shared__ __align__(16) int sort_smem[];
@@ -367,6 +370,7 @@ template <int GT, bool VEC> struct Columns {
 constexpr int kSumBatch = 8;               // rows of the gradient a thread has in flight
 constexpr int kMaxWindow = 256;
 
+// Bound by the latency of a window's gathered rows, eight of them on their way: 16 384 bf16 rows of 2048 (67 MB) in 10 us, 32 768 of 1024 in 24.
 // The windows of a block: their tokens' keys, with the one in front and the one behind (-1 where there is none), and positions.
 template <int GT, int OT, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const __grid_constant__ GradParams P) {
@@ -418,7 +422,8 @@ __global__ void __launch_bounds__(kSumThreads) tli_grad_sum_kernel(const __grid_
     flush(key[1 + count] == cur);
 }
 
-// The row that begins in a window and goes on in the next ones: their pieces in order, eight on their way at a time.
+// The row that begins in a window and goes on in the next ones: their pieces in order, eight on their way at a time (2 to 8 us after the
+// sums, most of it the launch).
 template <int GT, int OT, bool VEC>
 __global__ void __launch_bounds__(kSumThreads) tli_grad_join_kernel(const __grid_constant__ GradParams P) {
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -6,18 +6,25 @@
 // the ids with w >= min_p: three prefixes of one order, so what is kept is a prefix too, and one border
 // (logit, id) says all of it.  The rest of the work is to find that border without sorting the row.
 //
-//   tli_rows_scan_kernel   reads every row once (HBM-bound): each lane leaves the largest of its U 16-byte vectors
-//                          (a "group", 16*U bytes of the row) in the workspace, 1/(8U) or less of what it read;
-//                          rows that need the whole mass (top-p without top-k, no filter at all) also leave a sum
-//                          per strip of 32 groups.
-//   tli_rows_pick_kernel   one CTA per row.  k groups have a largest element at or above the k-th largest group
-//                          maximum, so at least k elements do: that maximum (taken from a histogram) is a
-//                          floor under the border.  Only the groups that reach the floor are read again, their few
-//                          elements sorted in shared memory, the border read off, the id drawn.  The same with
-//                          mass instead of count for top-p.  Sets that do not fit the sort (flat rows, k in the
-//                          thousands) go through a histogram over key digits instead: same border, more passes.
+//   tli_rows_scan_kernel   reads every row once: each lane leaves the largest of its U 16-byte vectors (a "group") in the
+//                          workspace, 1/(8U) or less of what it read; rows that need the whole mass (top-p without
+//                          top-k, no filter at all) also leave a sum per strip of 32 groups.
+//   tli_rows_pick_kernel   one CTA per row.  k groups have a largest element at or above the k-th largest group maximum, so at
+//                          least k elements do: a histogram of the maxima gives a floor under the border (the same with mass
+//                          instead of count for top-p).  Only the groups that reach the floor are read again; their elements
+//                          are a list in shared memory in which the border and the draw are found by counting (up to 256) or
+//                          by histograms over what is left of the interval (up to 4096).
+//   tli_rows_spread_kernel the rows whose list would not fit, by all CTAs: a sample of 8192 elements brackets the border between two
+//                          logits, one more pass over the row counts and weighs what lies above the bracket and lists what
+//                          lies in it; the CTA that ends a row's last strips finds border and draw as above.  If the bracket
+//                          was wrong (or a run of equal logits is longer than the list, or top-k of many thousands meets
+//                          top-p) the border is found by key digits over the whole row: the same border, more passes.
 //   tli_rows_mask_kernel   (filter only) writes the row: -inf without reading it wherever the group maximum is
 //                          below the border, the compared elements elsewhere.
+//
+// Bytes: a row once (sample), once and written once (filter).  At the measured copy bandwidth that is 50 us for 320 fp32 rows of
+// 256 000; the call takes 79 us at top-k 50, 134 at top-p .5, 285 to 305 at top-p .9 to .95 (two thirds of that is the fp64 work of
+// the scan and of the spread pass).  One fp32 row of 32 000: 17 us, three launches and 13 us of dependent steps.
 //
 // Weights and sums are fp64: the ids that come out are exact decisions (which id owns v * total, which one is
 // the last inside top-p), and with 10^5 candidates an fp32 sum (2^-24 relative) would decide some of them by
@@ -244,6 +251,8 @@ struct RowAsk {
     }
 };
 
+// Bound by DRAM where no mass is asked for: 320 fp32 rows of 256 000 (328 MB) in 48 us, 6.8 TB/s; by the issue slots of the fp64
+// weights where every row wants its mass: 95 us.  Small blocks (128 threads) because a row of 32 000 has only 16 to 32 strips.
 template <int DT, int U>
 __global__ void __launch_bounds__(kRowThreads) tli_rows_scan_kernel(const __grid_constant__ RowsParams P) {
     __shared__ double tab[16];
@@ -997,6 +1006,8 @@ template <int DT> __device__ __forceinline__ Border border_of(u64 edge) {
 }
 
 struct Draw { int token; double prob; };
+// (a number outside [0, 1) is the caller's mistake, but still draws a kept id)
+__device__ __forceinline__ float uniform_of(const RowsParams &P, int row) { return fminf(fmaxf(__ldg(P.u + row), 0.f), 1.f); }
 // Border and draw from a list of at most one element per thread: every thread counts, and weighs, what is in front of its own
 // element, in the order of the logits and then in that of the ids.  Two trips through the list against ten block-wide steps.
 template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk &ask, bool draw, float u, float zmin, double Z, int n, Border &border) {
@@ -1179,6 +1190,9 @@ __device__ __noinline__ void plan_row(const RowsParams &P, int row, int kind, fl
     P.todo[1 + atomicAdd(P.todo, 1)] = row;
 }
 
+// Bound by latency: some ten block-wide steps and three or four trips to L2 in a row, 10 to 12 us at top-k 50 for one row or 64, 17 us
+// for rows of 256 000 (their 8000 group maxima); 20 to 45 us where a list of thousands or a bracket is needed.  Two or three CTAs
+// share an SM (group maxima and list: 50 to 94 KB), so some 300 to 440 rows are one wave.
 template <int DT>
 __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
@@ -1187,7 +1201,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const RowAsk ask(P, b);
-    const float u = P.sample ? __ldg(P.u + row) : 0.f;
+    const float u = P.sample ? uniform_of(P, row) : 0.f;
     const Border all = {-INFINITY, -1};
 
     __syncthreads();
@@ -1248,7 +1262,9 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     const float zlow = ask.p_on ? fmaxf(floor, -FLT_MAX) : fmaxf(floor, zmin);
     list_groups(zlow, tmax);
     // Every listed group has an element.  Without a floor only short and mostly masked rows are worth a try; and beyond some 4096
-    // vectors to read again (4 ns each for this one block) all blocks together are faster.
+    // vectors to read again (4 ns each for this one block) all blocks together are faster: with a limit of 8192 a call for 80 fp32 rows
+    // of 256 000 at top-p .9 takes 137 us against 113 (48 bf16 rows of 128 256 at .95: 38 against 51), with one of 1024 the latter
+    // at .9 takes 41 us against 29 (64 bf16 rows of 32 000, mixed filters: 55 against 63).
     const int vectors = S.ng * (P.coarse << P.ulog);
     const bool worth = P.V <= kListCap || (ok ? vectors <= 4096 : S.ng <= 256);
     const int n = worth ? gather<DT>(zlow) : INT_MAX;
@@ -1314,7 +1330,8 @@ template <int DT> struct Least {
 // Strips [strip, end) of such a row by one warp: what (zhi, bid) keeps is counted and, if asked for, weighed, strip by strip; what
 // lies from there down to zlo goes to the row's list.  Every lane finds its candidates as bits first, then takes them one by one
 // from a copy of its vectors in shared memory (they cannot be indexed in registers): what an element costs that is neither kept nor
-// near the border is one comparison.  The next strip is on its way while one is worked on.
+// near the border is one comparison.  The next strip is on its way while one is worked on.  (Ballots per element instead of bits per
+// lane: 304 fp32 rows of 256 000 at top-p .95 in 215 us against 149.  Weighing the kept ones of a warp 32 at a time from a queue: 152.)
 constexpr int kStash = 96;                               // 64 and one element of each lane
 constexpr int kStage = 8 * 32;                           // vectors of a strip at most
 static_assert(kPickWarps * (kStage * 16 + kStash * 8) <= kSpreadCap * 8, "strips and stashes take the place of the list");
@@ -1499,12 +1516,14 @@ template <int DT> __device__ __noinline__ void settle_row(const RowsParams &P, R
         }
     }
     Draw d = {-1, 0.0};
-    if (P.sample) d = draw_by_strips<DT>(border, __ldg(P.u + row));
+    if (P.sample) d = draw_by_strips<DT>(border, uniform_of(P, row));
     finish_row(P, row, 0, BORDER_APPLY, border, d.token, d.prob);
 }
 
 // The rows that the pick kernel left, by all blocks: each takes some strips at a time (the next ones when it is done: the block
-// that ends last with a row settles it, which takes as long as several strips).
+// that ends last with a row settles it, which takes 13 to 25 us, as long as several strips).  Two blocks of 128 registers per SM hold
+// 16 warps with a strip of 4 KB on its way each.  304 fp32 rows of 256 000 at top-p .95 in 149 us (2.1 TB/s read again; the issue slots are
+// 43% busy, the rest waits for the loads, for fp64 results and for the slowest warp of a task); ends 20 us after its last strip.
 template <int DT, int U>
 __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x;
@@ -1546,6 +1565,7 @@ __global__ void __launch_bounds__(kPickThreads, 2) tli_rows_spread_kernel(const 
     }
 }
 
+// Bound by DRAM: 576 bf16 rows of 152 064 (175 MB written, up to as much read) in 42 us.
 template <int DT, int U>
 __global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const __grid_constant__ RowsParams P) {
     constexpr uint32_t NI = Elt<DT>::kNegInfWord;
@@ -1624,8 +1644,8 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const __grid
 
 struct RowsLayout { int U, nstrip, coarse, listcap; size_t gmax, ssum, border, plan, todo, lists, total; };
 
-// Groups of 8 vectors; of 4 where a row has at most 8192 vectors, so that a short row still has enough groups for
-// a top-k of a few hundred.
+// Groups of 8 vectors; of 4 and 2 where a row has at most 8192 and 4096 vectors, so that a short row still has enough groups for a
+// top-k of a few hundred and enough strips for the SMs (64 bf16 rows of 32 000 at top-k 50: 12 us of pick kernel with groups of 2, 19 with groups of 8).
 RowsLayout rows_layout(long long rows, int V, int dtype) {
     RowsLayout L;
     const int nvec = chunks_per_row(V, dtype, 1);

@@ -180,6 +180,22 @@ def test_the_ends_of_the_uniform(u):
     check(v, D, part, z, asks(B), np.full((B, 2), u, np.float32))
 
 
+@pytest.mark.parametrize("V", [600, 9000, 40000])
+def test_uniforms_outside_their_range_still_draw_a_kept_id(V):
+    rng = np.random.default_rng(13)
+    v, part = verifier(rng, V, T)
+    us = np.array([1.0, 2.0, 1e30, INF, -INF, -1.0, np.nan], np.float32)
+    B = len(ASKS)
+    z = rng.normal(0, 1, (B, us.size, V)).astype(np.float32)
+    tau, k, p, mp = asks(B)
+    dt, dk, dp, dm = (torch.from_numpy(x).cuda() for x in (tau, k, p, mp))
+    _, _, status, kept = ro.rows(z.astype(np.float64), part, tau, k, p, mp, np.zeros((B, us.size), np.float32))
+    out = v.sample(torch.from_numpy(z).cuda(), dt, torch.from_numpy(np.tile(us, (B, 1))).cuda(), side=T, top_k=dk, top_p=dp, min_p=dm)
+    tokens = out["tokens"].cpu().numpy()
+    assert (status == 0).all() and (out["status"].cpu().numpy() == 0).all()
+    assert np.take_along_axis(kept, tokens[..., None].astype(np.int64), 2).all()
+
+
 @pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
 @pytest.mark.parametrize("offset", [0, 1, 3])
 def test_strides_alignment_and_padding(offset, dtype):
