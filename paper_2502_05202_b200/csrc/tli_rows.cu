@@ -1331,7 +1331,7 @@ template <int DT> struct Least {
 // lies from there down to zlo goes to the row's list.  Every lane finds its candidates as bits first, then takes them one by one
 // from a copy of its vectors in shared memory (they cannot be indexed in registers): what an element costs that is neither kept nor
 // near the border is one comparison.  The next strip is on its way while one is worked on.  (Ballots per element instead of bits per
-// lane: 304 fp32 rows of 256 000 at top-p .95 in 215 us against 149.  Weighing the kept ones of a warp 32 at a time from a queue: 152.)
+// lane: 304 fp32 rows of 256 000 at top-p .95 in 215 us against 149.  Weighing the kept ones of a warp 32 at a time from a queue costs as much as it saves.)
 constexpr int kStash = 96;                               // 64 and one element of each lane
 constexpr int kStage = 8 * 32;                           // vectors of a strip at most
 static_assert(kPickWarps * (kStage * 16 + kStash * 8) <= kSpreadCap * 8, "strips and stashes take the place of the list");
@@ -1645,7 +1645,8 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const __grid
 struct RowsLayout { int U, nstrip, coarse, listcap; size_t gmax, ssum, border, plan, todo, lists, total; };
 
 // Groups of 8 vectors; of 4 and 2 where a row has at most 8192 and 4096 vectors, so that a short row still has enough groups for a
-// top-k of a few hundred and enough strips for the SMs (64 bf16 rows of 32 000 at top-k 50: 12 us of pick kernel with groups of 2, 19 with groups of 8).
+// top-k of a few hundred (or thousand: 64 bf16 rows of 32 000, top-k 1000 with top-p .99: 48 us against 59 with groups of 8 and, before
+// lists were as long, 319 of 4) and the scan enough strips for the SMs (4.8 us against 6.1 with groups of 8).
 RowsLayout rows_layout(long long rows, int V, int dtype) {
     RowsLayout L;
     const int nvec = chunks_per_row(V, dtype, 1);
@@ -1659,9 +1660,10 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.border = off; off = align_up(off + sizeof(RowBorder) * rows, 256);
     L.plan = off; off = align_up(off + sizeof(RowPlan) * rows, 256);
     L.todo = off; off = align_up(off + sizeof(int) * (rows + 2), 256);
-    // bracketed elements of a row: a sample of 8192 puts the border within about V/50 of them; in 16 bits the ties at the
-    // bracket's ends come along
-    L.listcap = V <= kListCap ? 0 : std::min(kSpreadCap, std::max(2048, V / 20));
+    // Bracketed elements of a row: a sample of 8192 puts the border within about V/50 of them, in 16 bits the ties at the bracket's
+    // ends come along, and a top-k of thousands with top-p wants them all.  (V/20: 64 bf16 rows of 32 000, top-k 2500 to 5000 with
+    // top-p, went through digits in 257 to 290 us against 81 to 112; where the list was long enough both are alike.)
+    L.listcap = V <= kListCap ? 0 : std::min(kSpreadCap, std::max(2048, V / 4));
     L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
     L.total = off;
     return L;

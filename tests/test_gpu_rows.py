@@ -125,6 +125,19 @@ def test_kept_sets_of_thousands(scale, dtype):
 
 @pytest.mark.parametrize("side", [T, D])
 @pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+def test_top_k_of_thousands_with_top_p(dtype, side):
+    """Around the lengths of the lists: as many elements as fit, one more, and far more."""
+    rng = np.random.default_rng(31)
+    V = 32003
+    v, part = verifier(rng, V, side, f=0.9)
+    table = [(1.0, k, p, m) for k in (1024, 1537, 2048, 3000, 4096, 4097, 6143, 6144, 6145, 8192, 8193) for p, m in ((0.99, 0.0), (0.6, 1e-3))]
+    B = len(table)
+    z = np.stack([rng.normal(0, 1, (B, V)), rng.normal(0, 0.05, (B, V))], axis=1)
+    check(v, side, part, to_dtype(z, dtype), asks(B, table), numbers(rng, (B, 2)))
+
+
+@pytest.mark.parametrize("side", [T, D])
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
 def test_masked_infinite_and_nan_logits(dtype, side):
     rng = np.random.default_rng(5 + dtype)
     V = 5003
