@@ -841,14 +841,14 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
 // spread over the row: where the sample itself has that place, and four standard errors to both sides (fewer, if as many elements
 // as lie between would not fit `capacity`).  The sample is counted and weighed in 1024 equal parts of [q, m], what is below q with the first;
 // q: three times as far below m as the least of the threads' maxima.  (A logit of the type's lowest value is a mask to both.)
-struct Bracket { float low, high; };
+struct Bracket { float low, high; bool wide; };            // wide: with four standard errors it would not have fit
 template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity, float tmax) {
     constexpr int EPV = Elt<DT>::kPerVec, total = kSample / EPV, B = 4;
     static_assert(total % (B * kPickThreads) == 0 && kSample <= 8192, "whole batches; 8192 parts of 498 000 fit 32 bits");
     const bool whole = S.nvec <= total, by_mass = !ask.k_on;
     const float m = S.m, sf = static_cast<float>(S.w.s);
     Bracket r;
-    r.low = -FLT_MAX; r.high = m;
+    r.low = -FLT_MAX; r.high = m; r.wide = false;
     float q = order_float(block_min(float_order(tmax > -1e30f ? tmax : m)));
     q = m - 3.f * (m - q);
     if (by_mass) q = fmaxf(q, m - 70.f * ask.tau);                 // (no weight worth a part is below that)
@@ -923,7 +923,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
         off = spare * (sqrt(want) + 1.0);
     }
 #pragma unroll 1
-    for (int round = 0; round < 2; ++round) {
+    for (int round = 0; round < 4; ++round) {
         __syncthreads();
         if (threadIdx.x < 2) at[threadIdx.x] = -1.f;
         __syncthreads();
@@ -939,7 +939,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
             if (far >= 0.f && far < kBins - 1) r.low = m - far * width;
             if (want - off >= 1.0 && near > 0.f) r.high = m - near * width;
         }
-        if (round) break;
+        if (round == 3) break;
         int inside = 0;
         const float last = far < 0.f ? static_cast<float>(kBins) : far;
 #pragma unroll
@@ -950,6 +950,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
         }
         const double expected = block_sum(inside) / share;
         if (expected <= 0.9 * capacity) break;
+        r.wide = true;
         off *= fmax(0.4, 0.8 * capacity / expected);
     }
     __syncthreads();
@@ -1289,7 +1290,26 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
         return;
     }
     if (ask.k_on || ask.p_on) {
-        const Bracket br = bracket<DT>(ask, Z, P.listcap, tmax);
+        Bracket br = bracket<DT>(ask, Z, P.listcap, tmax);
+        if (!ask.k_on) br.low = fminf(fmaxf(br.low, floor), br.high);
+        // A bracket too wide for the list is that of a row whose mass lies in a few large elements, with many small ones below them.  It comes here
+        // when two of them share a group (the maxima do not hold the mass, or only far down): the list above the largest groups'
+        // maxima is complete as far as it goes, and as a rule far enough.  (One such row of 48 bf16 rows of 128 256 ended in the digits: 359 us a
+        // call against 35.)
+        const int per = P.coarse << P.ulog;
+        const float top = br.wide && !ask.k_on ? floor_from_groups(false, 2048 / per, tmax) : -INFINITY;
+        if (top > -INFINITY) {
+            list_groups(top, tmax);
+            const int few = S.ng * per <= 8192 ? gather<DT>(top) : INT_MAX;
+            if (few <= kListCap) {
+                const Edge at = border_in_list<DT>(ask, P.sample, zmin, Z, few, m, top, 0, 0.0);
+                if (at.edge) {
+                    if (P.sample) d = draw_from_list<DT>(u, few, at.edge, at.unit);
+                    finish_row(P, row, 0, BORDER_APPLY, border_of<DT>(at.edge), d.token, d.prob);
+                    return;
+                }
+            }
+        }
         plan_row(P, row, PLAN_BRACKET, br.low, br.high, -1, zmin, Z);
         return;
     }
