@@ -838,11 +838,11 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
 // ---- the border among thousands: a bracket from a sample ----
 
 // Two logits that the k-th largest (or the last one inside top-p) lies between but for bad luck, from up to 8192 elements
-// spread over the row: where the sample itself has that place, and four standard errors to both sides (fewer, if as many elements
-// as lie between would not fit `capacity`).  The sample is counted and weighed in 1024 equal parts of [q, m], what is below q with the first;
+// spread over the row: where the sample itself has that place, and four standard errors to both sides (up to eight, if few elements
+// lie between; fewer, if as many would not fit `capacity`), not below `floor`.  The sample is counted and weighed in 1024 equal parts of [q, m], what is below q with the first;
 // q: three times as far below m as the least of the threads' maxima.  (A logit of the type's lowest value is a mask to both.)
 struct Bracket { float low, high; bool wide; };            // wide: with four standard errors it would not have fit
-template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity, float tmax) {
+template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, double Z, int capacity, float floor, float tmax) {
     constexpr int EPV = Elt<DT>::kPerVec, total = kSample / EPV, B = 4;
     static_assert(total % (B * kPickThreads) == 0 && kSample <= 8192, "whole batches; 8192 parts of 498 000 fit 32 bits");
     const bool whole = S.nvec <= total, by_mass = !ask.k_on;
@@ -930,7 +930,7 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
         place(fmax(1.0, want - off), at);
         place(want + off, at + 1);
         __syncthreads();
-        const float near = at[0], far = at[1];
+        const float near = by_mass ? fmaxf(at[0], (floor - q) * per_bin) : at[0], far = at[1];
         r.low = -FLT_MAX; r.high = m;
         if (by_mass) {
             if (near > 1.f) r.low = q + near * width;
@@ -949,12 +949,17 @@ template <int DT> __device__ __noinline__ Bracket bracket(const RowAsk &ask, dou
                 inside += static_cast<int>(static_cast<float>(n[i]) * (fminf(bin + 1.f, last) - fmaxf(bin, near)) + 0.5f);
         }
         const double expected = block_sum(inside) / share;
+        if (round == 0 && expected < 0.0625 * capacity) {          // up to twice as wide: nearly free, and a miss is not
+            off *= fmin(2.0, 0.0625 * capacity / fmax(expected, 1.0));
+            continue;
+        }
         if (expected <= 0.9 * capacity) break;
         r.wide = true;
         off *= fmax(0.4, 0.8 * capacity / expected);
     }
     __syncthreads();
-    r.high = fminf(r.high, m);
+    r.low = fmaxf(r.low, floor);
+    r.high = fmaxf(fminf(r.high, m), r.low);
     if (DT == TLI_BF16) {                                          // values of the row's type, so that keys and logits say the same
         r.low = fmaxf(__bfloat162float(__float2bfloat16_rd(r.low)), -FLT_MAX);
         r.high = __bfloat162float(__float2bfloat16_ru(r.high));
@@ -1195,7 +1200,7 @@ __device__ __noinline__ void plan_row(const RowsParams &P, int row, int kind, fl
 // for rows of 256 000 (their 8000 group maxima); 20 to 45 us where a list of thousands or a bracket is needed.  Two or three CTAs
 // share an SM (group maxima and list: 50 to 94 KB), so some 300 to 440 rows are one wave.
 template <int DT>
-__global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
+__global__ void __launch_bounds__(kPickThreads, 3) tli_rows_pick_kernel(const __grid_constant__ RowsParams P) {
     const int tid = threadIdx.x, row = blockIdx.x, b = row / P.R;
     exp2_table_init(S.tab, tid);
     enter_row<DT>(P, row, b, kListCap);
@@ -1253,7 +1258,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
     if (ask.k_on) {
         floor = ask.k <= kPickThreads / 2 ? floor_from_threads(ask.k, tmax) : floor_from_groups(false, ask.k, tmax);
         if (floor == -INFINITY && ask.p_on && P.V > kListCap && ask.k <= P.listcap * 3 / 4) {      // too few groups for that many: from a sample
-            floor = bracket<DT>(ask, Z, P.listcap - ask.k, tmax).low;
+            floor = bracket<DT>(ask, Z, P.listcap - ask.k, -FLT_MAX, tmax).low;
             if (floor == -FLT_MAX) floor = -INFINITY;
         }
     } else if (ask.p_on && Z < 8192.0) {
@@ -1290,8 +1295,7 @@ __global__ void __launch_bounds__(kPickThreads) tli_rows_pick_kernel(const __gri
         return;
     }
     if (ask.k_on || ask.p_on) {
-        Bracket br = bracket<DT>(ask, Z, P.listcap, tmax);
-        if (!ask.k_on) br.low = fminf(fmaxf(br.low, floor), br.high);
+        const Bracket br = bracket<DT>(ask, Z, P.listcap, ask.k_on ? -FLT_MAX : fmaxf(floor, -FLT_MAX), tmax);
         // A bracket too wide for the list is that of a row whose mass lies in a few large elements, with many small ones below them.  It comes here
         // when two of them share a group (the maxima do not hold the mass, or only far down): the list above the largest groups'
         // maxima is complete as far as it goes, and as a rule far enough.  (One such row of 48 bf16 rows of 128 256 ended in the digits: 359 us a
