@@ -136,6 +136,23 @@ def test_top_k_of_thousands_with_top_p(dtype, side):
     check(v, side, part, to_dtype(z, dtype), asks(B, table), numbers(rng, (B, 2)))
 
 
+@pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
+@pytest.mark.parametrize("V", [40001, 128256, 300007])
+def test_a_few_large_elements_over_a_heavy_tail(V, dtype):
+    """Most of the mass in two or three elements, side by side or apart; the border among them, just behind them, or far down the tail."""
+    rng = np.random.default_rng(V + dtype)
+    v, part = verifier(rng, V, T)
+    table = [(1.0, 0, p, m) for p in (0.5, 0.9, 0.915, 0.925, 0.95, 0.99) for m in (0.0, 1e-4)]
+    B = len(table)
+    z = rng.normal(0, 1.5, (B, 4, V))
+    tail = np.log(np.exp(z).sum(-1))
+    for r, (many, apart) in enumerate(((2, 1), (3, 1), (2, 5000), (3, 3))):
+        for j in range(many):
+            z[:, r, 9000 + j * apart] = tail[:, r] + np.log(0.92 / 0.08 / many)
+    kept = check(v, T, part, to_dtype(z, dtype), asks(B, table), numbers(rng, (B, 4)))
+    assert kept.sum(-1).min() <= 2 and kept.sum(-1).max() > 1000
+
+
 @pytest.mark.parametrize("side", [T, D])
 @pytest.mark.parametrize("dtype", [wl.F32, wl.BF16])
 def test_masked_infinite_and_nan_logits(dtype, side):
