@@ -638,7 +638,9 @@ template <int DT> __device__ __noinline__ int gather(float zlow) {
         }
     }
     __syncthreads();
-    return S.listed;
+    const int n = S.listed;
+    __syncthreads();                                               // (the next step may count in the same word)
+    return n;
 }
 
 // A floor under the border for a top-k of at most half as many as there are threads, from the threads' maxima (nearly as tight

@@ -1,0 +1,41 @@
+"""The row kernels with their threads in orders that a GPU need not show (rows_on_cpu.py): the same tokens, probabilities, kept sets and
+status bits as the fp64 definition, and blocks that end, whatever runs first between two barriers."""
+import numpy as np
+import pytest
+
+import row_oracle as ro
+import rows_on_cpu as rc
+
+ORDERS = range(6)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return rc.build()
+
+
+def check(lib, z, asks, dtype=0, part=None, order=0, seed=0, left=None):
+    """Sampled and filtered against the definition; ``left``: how many rows the pick kernel is to leave to the spread kernel."""
+    z = np.ascontiguousarray(z, np.float32)
+    if dtype:
+        z = (z.view(np.uint32) & 0xffff0000).view(np.float32)
+    B, R, V = z.shape
+    f = lambda i, t: np.array([asks[b % len(asks)][i] for b in range(B)], t)
+    ask = f(0, np.float32), f(1, np.int32), f(2, np.float32), f(3, np.float32)
+    u = np.random.default_rng(seed).integers(0, 1 << 24, (B, R)).astype(np.float32) / np.float32(1 << 24)
+    tokens, prob, status, kept = ro.rows(z.astype(np.float64), np.ones(V, bool) if part is None else part, *ask, u)
+    got = rc.run(lib, z, dtype, ask, u, part, order, seed)
+    np.testing.assert_array_equal(got["status"], status)
+    np.testing.assert_array_equal(got["tokens"], tokens)
+    np.testing.assert_allclose(got["prob"], prob, rtol=2.0 ** -24 + 1e-12, atol=2.0 ** -149)
+    assert left is None or got["left"] == left
+    got = rc.run(lib, z, dtype, ask, None, part, order, seed)
+    np.testing.assert_array_equal(got["status"], status)
+    np.testing.assert_array_equal(got["kept"][status == 0], kept[status == 0])
+
+
+@pytest.mark.parametrize("order", ORDERS)
+def test_lists_of_hundreds(lib, order):
+    """257 to 4096 listed elements: the search begins to count in the word that the list's length was read from."""
+    z = np.random.default_rng(1).normal(0, 3, (4, 1, 3000))
+    check(lib, z, [(1.0, 500, 1.0, 0.0), (1.0, 0, 0.95, 0.0), (1.0, 400, 0.9, 0.0), (1.0, 2999, 1.0, 0.0)], order=order, left=0)
