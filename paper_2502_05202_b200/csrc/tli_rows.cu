@@ -1050,6 +1050,7 @@ template <int DT> __device__ __noinline__ Draw pick_from_short_list(const RowAsk
     if (e && rank == count - 1) { S.found = e; S.before = ahead + f; }
     __syncthreads();
     const u64 edge = S.found, total = S.before;
+    __syncthreads();                                               // (the draw leaves its element where the border was)
     border.z = element_logit<DT>(edge);
     border.id = element_id(edge);
     // fewer kept than asked for: only min-p or the end of the row can be the reason, and both hold below the list too

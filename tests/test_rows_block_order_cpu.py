@@ -39,3 +39,12 @@ def test_lists_of_hundreds(lib, order):
     """257 to 4096 listed elements: the search begins to count in the word that the list's length was read from."""
     z = np.random.default_rng(1).normal(0, 3, (4, 1, 3000))
     check(lib, z, [(1.0, 500, 1.0, 0.0), (1.0, 0, 0.95, 0.0), (1.0, 400, 0.9, 0.0), (1.0, 2999, 1.0, 0.0)], order=order, left=0)
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("scale", [1, 3])
+def test_lists_of_several_warps(lib, scale, order):
+    """33 to 256 listed elements: the drawn one is left in the word that the border was read from."""
+    z = np.random.default_rng(scale).normal(0, scale, (12, 1, 4096))
+    for seed in range(4):
+        check(lib, z, [(1.0, 100, 1.0, 0.0), (1.0, 60, 1.0, 0.0), (1.0, 128, 0.9, 0.0)], order=order, seed=seed, left=0)
