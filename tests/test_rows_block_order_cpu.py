@@ -14,15 +14,16 @@ def lib():
     return rc.build()
 
 
-def check(lib, z, asks, dtype=0, part=None, order=0, seed=0, left=None):
-    """Sampled and filtered against the definition; ``left``: how many rows the pick kernel is to leave to the spread kernel."""
+def check(lib, z, asks, dtype=0, part=None, order=0, seed=0, left=None, u=None):
+    """Sampled (``u``: with this number for every row) and filtered against the definition; ``left``: how many rows the pick kernel is to leave to the
+    spread kernel."""
     z = np.ascontiguousarray(z, np.float32)
     if dtype:
         z = (z.view(np.uint32) & 0xffff0000).view(np.float32)
     B, R, V = z.shape
     f = lambda i, t: np.array([asks[b % len(asks)][i] for b in range(B)], t)
     ask = f(0, np.float32), f(1, np.int32), f(2, np.float32), f(3, np.float32)
-    u = np.random.default_rng(seed).integers(0, 1 << 24, (B, R)).astype(np.float32) / np.float32(1 << 24)
+    u = np.full((B, R), u, np.float32) if u is not None else np.random.default_rng(seed).integers(0, 1 << 24, (B, R)).astype(np.float32) / np.float32(1 << 24)
     tokens, prob, status, kept = ro.rows(z.astype(np.float64), np.ones(V, bool) if part is None else part, *ask, u)
     got = rc.run(lib, z, dtype, ask, u, part, order, seed)
     np.testing.assert_array_equal(got["status"], status)
@@ -48,3 +49,43 @@ def test_lists_of_several_warps(lib, scale, order):
     z = np.random.default_rng(scale).normal(0, scale, (12, 1, 4096))
     for seed in range(4):
         check(lib, z, [(1.0, 100, 1.0, 0.0), (1.0, 60, 1.0, 0.0), (1.0, 128, 0.9, 0.0)], order=order, seed=seed, left=0)
+
+
+def tail(rng, shape, scale):
+    return rng.normal(0, scale, shape) - 1.1 * np.log1p(rng.permutation(shape[-1]))
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_every_way_through_the_kernels(lib, dtype, order):
+    """Rows without filters, of one id, of short and long lists, left to the spread kernel, settled there from the list and by digits."""
+    rng = np.random.default_rng(7 + dtype)
+    asks = [(1.0, 0, 1.0, 0.0), (0.0, 0, 0.9, 0.0), (1.0, 1, 1.0, 0.0), (0.8, 50, 0.9, 0.0), (1.0, 0, 1.0, 0.05), (1.3, 0, 0.9, 0.0),
+            (1.0, 3000, 1.0, 0.0), (1.0, 3000, 0.9, 0.01), (1.0, 7000, 0.8, 0.0), (1.0, 0, 0.99, 1e-4), (-1.0, 0, 1.0, 0.0), (1.0, 0, np.nan, 0.0)]
+    z = np.concatenate([tail(rng, (len(asks), 1, 9001), 3), rng.normal(0, 0.05, (len(asks), 1, 9001))], axis=1)
+    check(lib, z, asks, dtype=dtype, order=order, seed=order)
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_ties_masks_and_nothing(lib, dtype, order):
+    rng = np.random.default_rng(9 + dtype)
+    asks = [(1.0, 0, 0.5, 0.0), (1.0, 70, 1.0, 0.0), (0.7, 2000, 0.9, 0.0), (1.0, 0, 1.0, 0.5), (1.0, 0, 1.0, 0.0), (0.0, 0, 1.0, 0.0)]
+    V = 5003
+    z = rng.integers(0, 3, (len(asks), 6, V)) * 0.5
+    part = rng.random(V) < 0.6
+    z[:, 1] = -np.inf
+    z[:, 2][:, rng.random(V) < 0.9] = -np.inf
+    z[:, 3, np.flatnonzero(part)[5]] = np.nan
+    z[:, 4] = rng.normal(0, 1, (len(asks), V))
+    z[:, 4, np.flatnonzero(~part)[::3]] = np.nan
+    z[:, 5] = 1.0
+    check(lib, z, asks, dtype=dtype, part=part, order=order, seed=order)
+
+
+@pytest.mark.parametrize("order", ORDERS)
+@pytest.mark.parametrize("u", [0.0, 1.0 - 2.0 ** -24])
+def test_the_ends_of_the_uniform(lib, u, order):
+    rng = np.random.default_rng(11)
+    asks = [(1.0, 100, 1.0, 0.0), (1.0, 1000, 1.0, 0.0), (1.0, 3000, 0.9, 0.0), (1.0, 0, 1.0, 0.0), (0.02, 0, 0.99, 0.0), (1.0, 5000, 0.99, 0.0)]
+    check(lib, rng.normal(0, 1, (len(asks), 1, 32003)), asks, order=order, u=u)
