@@ -703,13 +703,14 @@ __device__ __noinline__ float floor_from_groups(bool by_mass, unsigned want, flo
 // fixed-point numbers (two 32-bit shared atomics with a carry).
 
 enum : int { PASS_COUNT_KEYS, PASS_WEIGH_KEYS, PASS_WEIGH, PASS_COUNT, PASS_COUNT_IDS, PASS_LOWEST_ID };
-// One pass over the row (or its listed groups) for the elements whose logit is in [low, high]: their number, mass or lowest id, or a histogram
-// of their keys down from `high`, or of their ids up from `base`.
+// One pass over the row (or its listed groups) for the elements whose logit is in [low, high]: their number, mass (the bits of a double: small
+// weights count, however many there are) or lowest id, or a histogram of their keys down from `high`, or of their ids up from `base`.
 template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, float high, int shift, int base, double unit) {
     constexpr int EPV = Elt<DT>::kPerVec;
     const int total = listed_vectors();
     const uint32_t top = logit_key<DT>(high);
     u64 mine = what == PASS_LOWEST_ID ? INT_MAX : 0;
+    double mass = 0.0;
 #pragma unroll 1
     for (int t0 = threadIdx.x; t0 < total; t0 += 4 * kPickThreads) {
         uint4 raw[4];
@@ -736,15 +737,16 @@ template <int DT> __device__ __noinline__ u64 row_pass(int what, float low, floa
                 if (id >= base && (id - base) >> shift < kBins) atomicAdd(bins() + ((id - base) >> shift), 1u);
                 continue;
             }
+            if (what == PASS_WEIGH) { mass += S.w(x); continue; }
             const u64 f = what == PASS_COUNT_KEYS ? 1ull : __double2ull_rn(S.w(x) * unit);
-            if (what == PASS_WEIGH) { mine += f; continue; }
             const uint32_t j = (top - logit_key<DT>(x)) >> shift, lo = static_cast<uint32_t>(f);
             const uint32_t old = atomicAdd(bins() + j, lo);
             const uint32_t hi = static_cast<uint32_t>(f >> 32) + (old + lo < old ? 1u : 0u);
             if (hi) atomicAdd(bins() + kBins + j, hi);
         }
     }
-    if (what == PASS_WEIGH || what == PASS_COUNT) return block_prefix(mine).total;
+    if (what == PASS_WEIGH) return static_cast<u64>(__double_as_longlong(block_prefix(mass).total));
+    if (what == PASS_COUNT) return block_prefix(mine).total;
     if (what == PASS_LOWEST_ID) return static_cast<u64>(block_min(static_cast<int>(mine)));
     return 0;
 }
@@ -786,12 +788,10 @@ template <int DT> __device__ __noinline__ Border border_by_digits(const RowAsk &
         take = ask.k - before;
     }
     if (ask.p_on) {
-        if (ask.k_on) {                                            // the mass that top-k leaves: at most 2^20 weights up to 1
-            const double unit = 4398046511104.0;                   // 2^42
+        if (ask.k_on) {                                            // the mass that top-k leaves
             const uint32_t lo = cut ? key + 1 : bottom;
-            u64 above = 0;
-            if (lo <= top) above = row_pass<DT>(PASS_WEIGH, key_logit<DT>(lo), S.m, 0, 0, unit);
-            Z = static_cast<double>(above) / unit + (cut ? static_cast<double>(take) * S.w(key_logit<DT>(key)) : 0.0);
+            Z = cut ? static_cast<double>(take) * S.w(key_logit<DT>(key)) : 0.0;
+            if (lo <= top) Z += __longlong_as_double(static_cast<long long>(row_pass<DT>(PASS_WEIGH, key_logit<DT>(lo), S.m, 0, 0, 0.0)));
         }
         const double unit = two_to(61 - exponent(Z));              // Z unit < 2^62
         const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * Z * unit)));

@@ -214,6 +214,8 @@ static inline float __int_as_float(int x) { return __uint_as_float(static_cast<u
 static inline int __double2hiint(double x) { return static_cast<int>(emu::as_bits(x) >> 32); }
 static inline int __double2loint(double x) { return static_cast<int>(emu::as_bits(x)); }
 static inline double __hiloint2double(int hi, int lo) { return emu::from_bits<double>(static_cast<unsigned long long>(static_cast<unsigned>(hi)) << 32 | static_cast<unsigned>(lo)); }
+static inline long long __double_as_longlong(double x) { return static_cast<long long>(emu::as_bits(x)); }
+static inline double __longlong_as_double(long long x) { return emu::from_bits<double>(static_cast<unsigned long long>(x)); }
 static inline unsigned long long __double2ull_rn(double x) { return x > 0 ? static_cast<unsigned long long>(nearbyint(x)) : 0ull; }
 static inline unsigned __float2uint_rn(float x) { return x > 0 ? static_cast<unsigned>(nearbyintf(x)) : 0u; }
 static inline float __double2float_ru(double x) {

@@ -89,3 +89,16 @@ def test_the_ends_of_the_uniform(lib, u, order):
     rng = np.random.default_rng(11)
     asks = [(1.0, 100, 1.0, 0.0), (1.0, 1000, 1.0, 0.0), (1.0, 3000, 0.9, 0.0), (1.0, 0, 1.0, 0.0), (0.02, 0, 0.99, 0.0), (1.0, 5000, 0.99, 0.0)]
     check(lib, rng.normal(0, 1, (len(asks), 1, 32003)), asks, order=order, u=u)
+
+
+@pytest.mark.parametrize("bits", [43.1, 44.1, 45.1])
+@pytest.mark.parametrize("k,V", [(8000, 9001), (8999, 9001), (30000, 40001)])
+def test_top_k_by_digits_counts_small_weights(lib, k, V, bits):
+    """An id of weight 1, one of 1 - d and k - 2 of 2^-bits or a little less, of 2 d in all or a little more: half of their mass is more than the first id has, so
+    top-p 1/2 keeps two.  Without the small ones it keeps one.  The border lies d / 2 from the first id's mass, more than 1e-11 of the mass."""
+    z = (-bits - 0.3 * np.random.default_rng(k).random((1, 1, V))) * np.log(2.0)
+    d = (k - 2) * 2.0 ** (-bits - 0.3) / 2
+    assert d / 4 > 1e-11
+    z[0, 0, 17] = 0.0
+    z[0, 0, 4001] = -d
+    check(lib, z, [(1.0, k, 0.5, 0.0)], left=1)
