@@ -985,18 +985,24 @@ template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask,
         r.edge = find_element<DT>(n, 1, ask.k, above, first, range, 0, 0.0);
     }
     if (ask.p_on || draw) {
-        // (without Z: as many weights up to 1 as there are)
-        const double most = ask.p_on && !ask.k_on ? Z : above_mass + fmin(static_cast<double>(n), ask.k_on ? static_cast<double>(ask.k) : static_cast<double>(n));
+        // The unit by the mass itself: by the number of elements (a weight is at most 1) thousands of small weights beside a large one would round
+        // to nothing.  Fixed point says the mass well enough for its exponent, and, unlike fp64, the same in whatever order the list is.
+        const bool by_z = ask.p_on && !ask.k_on;
+        double most = Z;
+        auto listed_mass = [&](double unit) {                      // of what top-k leaves
+            u64 all = 0;
+#pragma unroll 4
+            for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], unit);
+            return block_prefix(all).total;
+        };
+        if (!by_z) {
+            const double coarse = two_to(43);                      // (up to 2^13 weights)
+            most = above_mass + static_cast<double>(listed_mass(coarse) + n) / coarse;
+        }
         r.unit = two_to(56 - exponent(most));
         if (ask.p_on) {
             const u64 before = __double2ull_rn(above_mass * r.unit);
-            double mass = Z * r.unit;
-            if (ask.k_on) {                                        // the mass that top-k leaves
-                u64 all = 0;
-#pragma unroll 4
-                for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], r.unit);
-                mass = static_cast<double>(before + block_prefix(all).total);
-            }
+            const double mass = by_z ? Z * r.unit : static_cast<double>(before + listed_mass(r.unit));
             const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * mass)));
             const u64 edge = above > 0 && before >= want ? 0ull : find_element<DT>(n, r.edge, want, before, first, range, BY_MASS, r.unit);
             r.edge = edge;

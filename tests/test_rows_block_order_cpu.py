@@ -102,3 +102,33 @@ def test_top_k_by_digits_counts_small_weights(lib, k, V, bits):
     z[0, 0, 17] = 0.0
     z[0, 0, 4001] = -d
     check(lib, z, [(1.0, k, 0.5, 0.0)], left=1)
+
+
+LISTS = [(4096, 4000, 46.1, 0.3, 0), (4096, 4096, 46.1, 0.3, 0), (40001, 6000, 45.1, 3.0, 1), (40001, 5000, 45.1, 2.5, 1)]
+
+
+@pytest.mark.parametrize("V,k,bits,width,left", LISTS)
+def test_lists_count_small_weights(lib, V, k, bits, width, left):
+    """The same among lists of thousands, in the pick kernel and settled by the spread kernel."""
+    z = (-bits - width * np.random.default_rng(k).random((1, 1, V))) * np.log(2.0)
+    d = (k - 2) * 2.0 ** (-bits - 0.5) / 2
+    assert d / 4 > 4e-12
+    z[0, 0, 17] = 0.0
+    z[0, 0, 3001] = -d
+    check(lib, z, [(1.0, k, 0.5, 0.0)], left=left)
+
+
+@pytest.mark.parametrize("V,k,bits,width,left", LISTS)
+def test_draws_among_small_weights(lib, V, k, bits, width, left):
+    """All ids but the last have small weights, and the number falls among them: the drawn id owns it, up to 2e-12 of the mass."""
+    z = (-bits - width * np.random.default_rng(k).random((1, 1, V))) * np.log(2.0)
+    z[0, 0, V - 1] = 0.0
+    z = z.astype(np.float32)
+    ids, w, _ = ro.kept_ids(z[0, 0].astype(np.float64), np.ones(V, bool), 1.0, k, 1.0, 0.0)
+    c = np.cumsum(w)
+    u = np.float32(c[len(c) // 2] / c[-1])                                   # half of the small ones lie in front
+    assert 5e-12 < u < 1e-9
+    got = rc.run(lib, z, 0, (np.ones(1, np.float32), np.full(1, k, np.int32), np.ones(1, np.float32), np.zeros(1, np.float32)), np.full((1, 1), u, np.float32))
+    assert got["left"] == left and got["status"][0, 0] == 0
+    at = np.flatnonzero(ids == got["tokens"][0, 0])[0]
+    assert c[at] - w[at] - 2e-12 * c[-1] <= float(u) * c[-1] <= c[at] + 2e-12 * c[-1]
