@@ -1713,8 +1713,8 @@ size_t rows_workspace(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, i
 struct SmemAllowed {
     std::atomic<unsigned long long> devices{0};
     cudaError_t set(const void *fn, size_t bytes, int device) {
-        const unsigned long long bit = 1ull << (device & 63);
-        if (device < 64 && (devices.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+        const unsigned long long bit = device < 64 ? 1ull << device : 0ull;        // (beyond: every time)
+        if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
         const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
         if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
         return e;
