@@ -503,6 +503,19 @@ int embed_side(const tli_ctx *ctx, int32_t ids_side, int32_t table_side, int &n_
 bool on_vectors(const void *p, int64_t stride, size_t elt) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride * static_cast<int64_t>(elt) % 16 == 0;
 }
+// As many clusters of a kernel as are resident together (two at least), asked once per device.
+struct ClustersResident {
+    std::atomic<int> known[64] = {};
+    cudaError_t get(const void *fn, const cudaLaunchConfig_t *cfg, int device, int &n) {
+        n = device < 64 ? known[device].load(std::memory_order_relaxed) : 0;
+        if (n > 0) return cudaSuccess;
+        const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, fn, cfg);
+        if (e != cudaSuccess) return e;
+        n = std::max(2, n);
+        if (device < 64) known[device].store(n, std::memory_order_relaxed);
+        return cudaSuccess;
+    }
+};
 void pdl_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute *attr, cudaStream_t stream) {
     memset(&cfg, 0, sizeof cfg);
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -549,17 +562,13 @@ template <int OT> int launch_grad(GradParams &P, int gdtype, int device, int num
         cfg.gridDim = dim3(num_sms); cfg.dynamicSmemBytes = 0;
         if (P.clustered) {
             // as many clusters as are resident together: the fill's shares are fixed, so a second wave would double its time
-            static std::atomic<int> resident{0};
-            int clusters = resident.load(std::memory_order_relaxed);
+            static ClustersResident resident;
+            int clusters = 0;
             cfg.gridDim = dim3(2 * kSortCluster); cfg.dynamicSmemBytes = smem;
-            if (clusters == 0) {
-                cudaLaunchConfig_t ask = cfg;
-                ask.attrs = both + 1; ask.numAttrs = 1;
-                e = cudaOccupancyMaxActiveClusters(&clusters, tli_grad_sort_kernel<OT>, &ask);
-                if (e != cudaSuccess) return cuda_fail(e, "cudaOccupancyMaxActiveClusters");
-                clusters = std::max(2, clusters);
-                resident.store(clusters, std::memory_order_relaxed);
-            }
+            cudaLaunchConfig_t ask = cfg;
+            ask.attrs = both + 1; ask.numAttrs = 1;
+            e = resident.get(reinterpret_cast<const void *>(tli_grad_sort_kernel<OT>), &ask, device, clusters);
+            if (e != cudaSuccess) return cuda_fail(e, "cudaOccupancyMaxActiveClusters");
             cfg.gridDim = dim3(clusters * kSortCluster);
         }
         e = cudaLaunchKernelEx(&cfg, tli_grad_sort_kernel<OT>, P);

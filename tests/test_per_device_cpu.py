@@ -36,3 +36,17 @@ extern "C" int ask(int device, int fail) {                                   // 
 }""")
     assert [lib.ask(d, 0) for d in (64, 0, 0, 63, 63, 64, 1)] == [1, 1, 0, 1, 0, 1, 1]
     assert [lib.ask(2, f) for f in (1, 0, 0)] == [-1, 1, 0]
+
+
+def test_resident_clusters_are_those_of_the_device(tmp_path):
+    embed = open(os.path.join(CSRC, "tli_embed.cu")).read()
+    lib = compiled(tmp_path, _definition(embed, "struct ClustersResident") + """
+extern "C" int ask(int device, int clusters, int fail) {                     // (calls that reached CUDA, -1 for an error) * 1000 + clusters
+    static ClustersResident resident;
+    cudaLaunchConfig_t cfg;
+    calls = 0; answer = clusters; fails = fail;
+    int n = 0;
+    return resident.get(nullptr, &cfg, device, n) == cudaSuccess ? calls * 1000 + n : -1;
+}""")
+    assert [lib.ask(d, c, 0) for d, c in ((0, 14), (1, 8), (0, 9), (1, 9), (64, 5), (0, 9), (63, 1))] == [1014, 1008, 14, 8, 1005, 14, 1002]
+    assert [lib.ask(2, 7, f) for f in (1, 0, 0)] == [-1, 1007, 7]
