@@ -779,6 +779,7 @@ class Verifier:
         if self.ctx:
             tli_destroy(self.ctx)
             self.ctx = 0
+        self._ws, self._kept = None, threading.local()             # scratch of every thread and stream
 
     def __del__(self):
         try:
