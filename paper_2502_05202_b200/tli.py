@@ -11,6 +11,7 @@ import ctypes
 import os
 import struct
 import threading
+import warnings
 from typing import Dict, Optional
 
 import numpy as np
@@ -915,7 +916,10 @@ class Verifier:
     def embed(self, ids, table, scale: float = 1.0, ids_side: int = TLI_SIDE_TARGET,
               table_side: int = TLI_SIDE_TARGET) -> Dict[str, torch.Tensor]:
         """Rows of ``table`` [V,H] for ``ids`` (any shape) of either vocabulary, times ``scale``, and the ids in
-        the table's vocabulary (-1, with a zero row, where there is none)."""
+        the table's vocabulary (-1, with a zero row, where there is none).  The rows are no part of an autograd graph:
+        the table's gradient is :meth:`embed_grad`'s (a table that waits for one by other means gets a warning)."""
+        if table.requires_grad and torch.is_grad_enabled():
+            warnings.warn("embed() records no autograd graph: the table gets its gradient from embed_grad(), or detach it", stacklevel=2)
         self._ids(ids)
         V, dev = self._table_rows(table_side), self.device
         if table.dim() != 2 or table.shape[0] != V or table.get_device() != self._index:
