@@ -986,24 +986,21 @@ template <int DT> __device__ __noinline__ Edge border_in_list(const RowAsk &ask,
     }
     if (ask.p_on || draw) {
         // The unit by the mass itself: by the number of elements (a weight is at most 1) thousands of small weights beside a large one would round
-        // to nothing.  Fixed point says the mass well enough for its exponent, and, unlike fp64, the same in whatever order the list is.
-        const bool by_z = ask.p_on && !ask.k_on;
-        double most = Z;
-        auto listed_mass = [&](double unit) {                      // of what top-k leaves
+        // to nothing.  The mass that top-k leaves is summed in units of 2^-50 (8192 weights fit 64 bits, and are off by 2^-38 at most) and not in
+        // fp64, which would depend on the list's order.
+        double mass = Z;
+        if (!ask.p_on || ask.k_on) {
+            constexpr double fine = 1125899906842624.0;            // 2^50
+            static_assert(kSpreadCap <= 1 << 13 && kListCap <= kSpreadCap, "sums below 2^64");
             u64 all = 0;
 #pragma unroll 4
-            for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], unit);
-            return block_prefix(all).total;
-        };
-        if (!by_z) {
-            const double coarse = two_to(43);                      // (up to 2^13 weights)
-            most = above_mass + static_cast<double>(listed_mass(coarse) + n) / coarse;
+            for (int i = threadIdx.x; i < n; i += kPickThreads) if (list()[i] >= r.edge) all += mass_of<DT>(list()[i], fine);
+            mass = above_mass + static_cast<double>(block_prefix(all).total) / fine;
         }
-        r.unit = two_to(56 - exponent(most));
+        r.unit = two_to(56 - exponent(mass + 1e-11));
         if (ask.p_on) {
             const u64 before = __double2ull_rn(above_mass * r.unit);
-            const double mass = by_z ? Z * r.unit : static_cast<double>(before + listed_mass(r.unit));
-            const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * mass)));
+            const u64 want = max(1ull, static_cast<u64>(ceil(static_cast<double>(ask.p) * mass * r.unit)));
             const u64 edge = above > 0 && before >= want ? 0ull : find_element<DT>(n, r.edge, want, before, first, range, BY_MASS, r.unit);
             r.edge = edge;
             if (edge == 0) return r;
