@@ -456,9 +456,10 @@ int tli_shard_select(tli_ctx *ctx, const tli_verify_args *args, const void *rows
  *                 the first; <= 0: off
  * The first id is always kept.  tau == 0 keeps it alone, whatever the filters say.
  *
- * Weights and sums are fp64: the kept set and the id drawn equal those of the
- * definition unless a mass lies within fp64 rounding of its border, and do not
- * depend on timing.  Both calls are asynchronous on the stream, allocate
+ * Weights are fp64 (3e-13 relative; an id more than 707 tau below the first has
+ * none) and sums fp64 or fixed point: the kept set and the id drawn equal those
+ * of the definition unless a mass lies within 5e-12 of the mass it is a share of from
+ * its border, and do not depend on timing.  Both calls are asynchronous on the stream, allocate
  * nothing, only launch kernels (they can be captured) and use of the context
  * only its maps: calls on one context may overlap if their workspaces and outputs
  * are distinct.  Errors as for tli_verify(); a context of tli_shard_create(), and a
@@ -495,7 +496,10 @@ typedef struct {
     size_t workspace_bytes;
 } tli_sample_args;
 
-/* Bytes of device scratch tli_sample() needs for (B, R, dtype, side); 0 on bad arguments. */
+/* Bytes of device scratch tli_sample() needs for (B, R, dtype, side); 0 on bad arguments.  Most of it is a list of
+ * min(8192, max(2048, V / 4)) ids of 8 bytes for every row of more than 4096 ids, whether its filters come to need one or not: as
+ * many bytes as the logits themselves for bf16 rows of 32 000, a quarter for fp32 rows of 64 000, 4.3 GB for 65 535 rows of 32 768
+ * or more. */
 size_t tli_sample_workspace_bytes(const tli_ctx *ctx, int32_t B, int32_t R, int32_t dtype, int32_t side);
 int tli_sample(tli_ctx *ctx, const tli_sample_args *args, void *cuda_stream);
 
@@ -528,7 +532,7 @@ int tli_filter(tli_ctx *ctx, const tli_filter_args *args, void *cuda_stream);
  * embeddings; its next_token is a target id and enters the drafter's.  This call
  * carries ids to the table's vocabulary (the id map, its inverse, or
  * neither) and looks the rows up:
- *     out[i] = scale * table[t(ids[i])]        one rounding to the type of the rows
+ *     out[i] = scale * table[t(ids[i])]        the product in fp32, then rounded to the type of the rows
  * An id outside its vocabulary or without a counterpart in the table's
  * gives a row of zeros and table_ids[i] = -1.  Asynchronous on the stream,
  * allocates nothing, launches one kernel, uses of the context only its maps.
@@ -555,7 +559,8 @@ int tli_embed(tli_ctx *ctx, const tli_embed_args *args, void *cuda_stream);
  *     out[v] = scale * sum over i with t(ids[i]) == v of grad[i]
  * Every row of out is written (zeros where no token refers to it).  Sums are
  * fp32 over the tokens sorted by (row, position): the result does not depend on
- * timing, and is rounded once.  Asynchronous, allocates nothing, only launches
+ * timing.  The sum times scale is an fp32 product, then rounded to the type of
+ * out.  Asynchronous, allocates nothing, only launches
  * kernels, uses of the context only its maps.
  */
 typedef struct {

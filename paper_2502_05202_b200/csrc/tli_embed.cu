@@ -12,7 +12,7 @@
 //       tli_grad_sum_kernel      a window of sorted tokens per group of threads: rows whose tokens all lie in the
 //                                window are written, the pieces of a row that crosses a window go to the workspace.
 //       tli_grad_join_kernel     adds the pieces of such a row in window order.
-// Sums are fp32 (a row is rounded once, after the scale).
+// Sums are fp32; the scaled sum, an fp32 product, is rounded to the type of dW.
 
 namespace {
 
@@ -47,7 +47,7 @@ template <int DT> __device__ __forceinline__ uint4 scale_vector(const uint4 &r, 
     } else {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)                                // one rounding, to nearest even
+        for (int i = 0; i < 4; ++i)                                // to nearest even
             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(z[2 * i + 1] * c), "f"(z[2 * i] * c));
         return make_uint4(w[0], w[1], w[2], w[3]);
     }

@@ -18,17 +18,23 @@
 //                          logits, one more pass over the row counts and weighs what lies above the bracket and lists what
 //                          lies in it; the CTA that ends a row's last strips finds border and draw as above.  If the bracket
 //                          was wrong (or a run of equal logits is longer than the list, or top-k of many thousands meets
-//                          top-p) the border is found by key digits over the whole row: the same border, more passes.
+//                          top-p, or min-p cuts above the bracket of a top-p without top-k: the bracket knows nothing of min-p)
+//                          the border is found by key digits over the whole row by one CTA: the same border, more passes.  For the
+//                          last of these that is the rule, not bad luck: 48 bf16 rows of 128 256 at top-p .95 with min-p .05
+//                          take 366 us (filter 181) against 63 at top-p .95 alone and 25 at min-p .05 alone; 320 fp32 rows of 256 000
+//                          1.9 ms (filter 1.0) against 311 and 79 us.
 //   tli_rows_mask_kernel   (filter only) writes the row: -inf without reading it wherever the group maximum is
 //                          below the border, the compared elements elsewhere.
 //
 // Bytes: a row once (sample), once and written once (filter).  At the measured copy bandwidth that is 50 us for 320 fp32 rows of
-// 256 000; the call takes 79 us at top-k 50, 134 at top-p .5, 285 to 305 at top-p .9 to .95 (two thirds of that is the fp64 work of
-// the scan and of the spread pass).  One fp32 row of 32 000: 17 us, three launches and 13 us of dependent steps.
+// 256 000; the call takes 84 us at top-k 50, 135 at top-p .5, 288 to 311 at top-p .9 to .95 (two thirds of that is the fp64 work of
+// the scan and of the spread pass).  One fp32 row of 32 000: 18 us, three launches and 13 us of dependent steps.
 //
 // Weights and sums are fp64: the ids that come out are exact decisions (which id owns v * total, which one is
 // the last inside top-p), and with 10^5 candidates an fp32 sum (2^-24 relative) would decide some of them by
-// rounding.  An fp64 weight costs 12 fp64 operations; one pass over a row is then bound by the fp64 pipe only
+// rounding.  A weight is off by 1.5e-13 of itself at most (3e-13 where it is a product of two, a strip's sum at its own largest logit and
+// that logit's weight), a list's fixed-point mass by 4e-12, a sum of a whole row by less than 1e-12: an id is decided by these only where
+// its border lies within 5e-12 of the mass.  An fp64 weight costs 12 fp64 operations; one pass over a row is then bound by the fp64 pipe only
 // for 16-bit rows that need the whole mass.
 
 #include <cuda_bf16.h>
@@ -81,7 +87,7 @@ __device__ __forceinline__ void exp2_table_init(double *tab, int tid) {
     }
 }
 // 2^x for x in [-1021, 0] as a product q * t: x = n/16 + r, |r| <= 1/32; q = 2^r by its Taylor series in r ln 2 to the fifth power
-// (next term (ln2/32)^6/6! = 1.4e-13), t = 2^(n/16) = tab[n mod 16] with n/16 added to the exponent field (the table's entry lacks
+// (next term (ln2/32)^6/6! = 1.4e-13, the whole error 1.46e-13), t = 2^(n/16) = tab[n mod 16] with n/16 added to the exponent field (the table's entry lacks
 // what the low four bits of n would add).  On this part an fp64 instruction holds the issue port for two cycles: the 12 of a
 // weight and five others are what bounds a pass that weighs a whole row.
 __device__ __forceinline__ void exp2_parts(double x, const double *tab, double &q, double &t) {
@@ -1675,7 +1681,7 @@ __global__ void __launch_bounds__(kRowThreads) tli_rows_mask_kernel(const __grid
 struct RowsLayout { int U, nstrip, coarse, listcap; size_t gmax, ssum, border, plan, todo, lists, total; };
 
 // Groups of 8 vectors; of 4 and 2 where a row has at most 8192 and 4096 vectors, so that a short row still has enough groups for a
-// top-k of a few hundred (or thousand: 64 bf16 rows of 32 000, top-k 1000 with top-p .99: 48 us against 59 with groups of 8 and, before
+// top-k of a few hundred (or thousand: 64 bf16 rows of 32 000, top-k 1000 with top-p .99: 45 us against 59 with groups of 8 and, before
 // lists were as long, 319 of 4) and the scan enough strips for the SMs (4.8 us against 6.1 with groups of 8).
 RowsLayout rows_layout(long long rows, int V, int dtype) {
     RowsLayout L;
@@ -1692,7 +1698,7 @@ RowsLayout rows_layout(long long rows, int V, int dtype) {
     L.todo = off; off = align_up(off + sizeof(int) * (rows + 2), 256);
     // Bracketed elements of a row: a sample of 8192 puts the border within about V/50 of them, in 16 bits the ties at the bracket's
     // ends come along, and a top-k of thousands with top-p wants them all.  (V/20: 64 bf16 rows of 32 000, top-k 2500 to 5000 with
-    // top-p, went through digits in 257 to 290 us against 81 to 112; where the list was long enough both are alike.)
+    // top-p, went through digits in 257 to 290 us against 79 to 119; where the list was long enough both are alike.)
     L.listcap = V <= kListCap ? 0 : std::min(kSpreadCap, std::max(2048, V / 4));
     L.lists = off; off = align_up(off + sizeof(unsigned long long) * rows * L.listcap, 256);
     L.total = off;

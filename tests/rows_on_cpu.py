@@ -84,6 +84,11 @@ extern "C" int rows_on_cpu(int sample, int B, int R, int V, int dtype, const voi
     free(ws);
     return ok ? 0 : 1;
 }
+extern "C" void exp2_on_cpu(const double *x, double *out, int n) {            // (the weights' powers of two, without threads)
+    double tab[16];
+    for (int i = 0; i < 16; ++i) exp2_table_init(tab, i);
+    for (int i = 0; i < n; ++i) out[i] = exp2_neg(x[i], tab);
+}
 extern "C" const char *emulator_message() { return emu::message; }
 """
 

@@ -132,3 +132,15 @@ def test_draws_among_small_weights(lib, V, k, bits, width, left):
     assert got["left"] == left and got["status"][0, 0] == 0
     at = np.flatnonzero(ids == got["tokens"][0, 0])[0]
     assert c[at] - w[at] - 2e-12 * c[-1] <= float(u) * c[-1] <= c[at] + 2e-12 * c[-1]
+
+
+def test_powers_of_two_to_the_stated_error(lib):
+    """exp2_neg() against 2^x in 64-bit mantissas: 1.5e-13 of the value, from 0 to where the weights are cut off."""
+    import ctypes
+    rng = np.random.default_rng(3)
+    x = np.concatenate([-1020.0 * rng.random(200000), -40.0 * rng.random(200000), -np.arange(0, 1020.0, 1 / 32), -np.geomspace(1e-300, 1.0, 5000), [0.0]])
+    out = np.empty_like(x)
+    lib.exp2_on_cpu(ctypes.c_void_p(x.ctypes.data), ctypes.c_void_p(out.ctypes.data), ctypes.c_int(x.size))
+    assert np.finfo(np.longdouble).nmant >= 63
+    error = np.abs(out.astype(np.longdouble) / np.exp2(x.astype(np.longdouble)) - 1)
+    assert 1e-13 < error.max() <= 1.5e-13 and out[-1] == 1.0
