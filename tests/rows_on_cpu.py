@@ -125,13 +125,13 @@ def source(edit=lambda text: text):
 
 def build(edit=lambda text: text):
     """The compiled kernels as a ctypes library."""
-    folder = tempfile.mkdtemp(prefix="rows_on_cpu_")
-    cpp, lib = os.path.join(folder, "rows.cpp"), os.path.join(folder, "rows.so")
-    with open(cpp, "w") as f:
-        f.write(source(edit))
-    subprocess.run(["g++", "-std=c++17", "-O1", "-w", "-ffp-contract=off", "-fno-strict-aliasing", "-fPIC", "-shared", "-I", os.path.join(ROOT, "tests"),
-                    "-I", os.path.join(ROOT, "include"), "-o", lib, cpp], check=True)
-    handle = ctypes.CDLL(lib)
+    with tempfile.TemporaryDirectory(prefix="rows_on_cpu_") as folder:
+        cpp, lib = os.path.join(folder, "rows.cpp"), os.path.join(folder, "rows.so")
+        with open(cpp, "w") as f:
+            f.write(source(edit))
+        subprocess.run(["g++", "-std=c++17", "-O1", "-w", "-ffp-contract=off", "-fno-strict-aliasing", "-fPIC", "-shared", "-I", os.path.join(ROOT, "tests"),
+                        "-I", os.path.join(ROOT, "include"), "-o", lib, cpp], check=True)
+        handle = ctypes.CDLL(lib)                                    # (stays loaded without its file)
     handle.emulator_message.restype = ctypes.c_char_p
     return handle
 
