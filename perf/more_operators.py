@@ -209,7 +209,9 @@ def run(s):
         if op == "loss":
             return v.loss(s["logits"], s["ids"], **how)
         if op == "loss_grad":
-            return v.loss_grad(s["logits"], s["ids"], s["stats"], grad_loss=s["grad_loss"], **how)
+            # 32-bit rows over the whole vocabulary: the plain form works in the logits' own memory, and so does this call
+            place = s["logits"] if case["type"] == _F32 and not case["shared"] else None
+            return v.loss_grad(s["logits"], s["ids"], s["stats"], grad_loss=s["grad_loss"], out=place, **how)
         if op == "head_loss":
             return v.head_loss(s["hidden"], s["weight"], s["ids"], **how)
         out = v.head_loss_grad(s["hidden"], s["weight"], s["ids"], s["stats"], s["target_logits"],
