@@ -58,7 +58,8 @@ enum {
     TLI_ROW_TIMEOUT = 16,         /* a bounded wait inside a kernel ran out: results not to be trusted.  Sticky: every
                                    * later call on the context reports it too, until tli_reset() */
     TLI_ROW_BAD_TEMPERATURE = 32, /* temperature negative or not finite: accepted = 0, next_token = 0 */
-    TLI_ROW_BAD_FILTER = 64       /* top_p or min_p is NaN (tli_sample(), tli_filter()) */
+    TLI_ROW_BAD_FILTER = 64,      /* top_p or min_p is NaN (tli_sample(), tli_filter()) */
+    TLI_ROW_LEFT_OUT = 128        /* no target id of the row takes part (tli_loss()): loss and gradient 0 */
 };
 
 /* which of the context's two vocabularies ids, rows of logits or an embedding table belong to */
@@ -70,6 +71,7 @@ enum { TLI_SIDE_TARGET = 0, TLI_SIDE_DRAFTER = 1 };
 #define TLI_MAX_SHARDS 64   /* vocabulary shards (tli_shard_create) */
 #define TLI_MAX_TOKENS 4194304 /* tokens per call of tli_embed() and tli_embed_grad() */
 #define TLI_MAX_H 65536     /* width of an embedding row */
+#define TLI_MAX_TARGETS 256 /* target ids per row of tli_loss() */
 #define TLI_STATIC_SCRATCH_BYTES 4194304 /* 4 MiB: scratch built into the library for tli_verify_static() */
 
 /*
@@ -580,6 +582,72 @@ typedef struct {
 
 size_t tli_embed_grad_workspace_bytes(const tli_ctx *ctx, int32_t N, int32_t H);
 int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *args, void *cuda_stream);
+
+/*
+ * Losses for fine-tuning a drafter (or a target) on tokens of either vocabulary:
+ * cross entropy against a label, or the divergence from a teacher's k largest
+ * logits, say the target's for a drafter.
+ *
+ * Row n has k target ids of vocabulary ids_side, carried to the rows' vocabulary
+ * as tli_embed() carries its ids.  With support TLI_SUPPORT_ALL every id of
+ * the row takes part; with TLI_SUPPORT_SHARED (drafter rows only) those inside the
+ * intersection, so that the softmax is q', what drafts are drawn from.  A target
+ * takes part if its id has a counterpart that does, and its teacher logit is not
+ * below -1e30 (or -inf).  With tau = temperature[n]:
+ *     p = softmax(teacher / tau) over the targets that take part (one label: p = 1)
+ *     q = softmax(z / tau) over the ids that take part
+ *     loss = sum over targets j of p_j (ln p_j - ln q[id_j])
+ *     d loss / d z[v] = (q[v] - sum over j with id_j == v of p_j) / tau
+ * The same id twice in a row counts twice.  A logit below -1e30 counts as -inf in the
+ * sum.  Rows without a target that takes part (TLI_ROW_LEFT_OUT), without a logit above
+ * -inf (TLI_ROW_FALLBACK) or with a temperature that is not positive and finite, or whose
+ * reciprocal is not (TLI_ROW_BAD_TEMPERATURE) have loss 0, stats 0 and gradient 0; NaN or
+ * +inf among the logits or teacher logits that take part gives a loss and a gradient row
+ * of NaN (TLI_ROW_NONFINITE).
+ *
+ * Sums are fp32, in an order that does not depend on timing.  The calls are
+ * asynchronous on the stream, allocate nothing, only launch kernels (they can be
+ * captured) and use of the context only its maps: calls on one context may
+ * overlap if their outputs (and workspaces) are distinct.  Errors as for tli_sample().
+ */
+enum { TLI_SUPPORT_ALL = 0, TLI_SUPPORT_SHARED = 1 };
+
+typedef struct {
+    int32_t N;                  /* rows, 0 .. TLI_MAX_TOKENS */
+    int32_t k;                  /* target ids per row, 1 .. TLI_MAX_TARGETS (1 without teacher logits) */
+    int32_t dtype;              /* TLI_F32 or TLI_BF16, of the logits */
+    int32_t side, ids_side;     /* TLI_SIDE_*: vocabulary of the rows, of the target ids */
+    int32_t support;            /* TLI_SUPPORT_* */
+    int32_t teacher_dtype;      /* TLI_F32 or TLI_BF16; not read without teacher logits */
+    const void *logits;         /* [device] [N, V]; vocabulary axis contiguous, base aligned to the element */
+    int64_t stride;             /* elements from row to row (0: one row for all) */
+    const int32_t *ids;         /* [device] int32[N, k] */
+    const void *teacher;        /* [device] [N, k] the teacher's logits of these ids; NULL: labels */
+    const float *temperature;   /* [device] float[N]; NULL: 1 */
+    float *loss;                /* [device] out float[N] */
+    float *stats;               /* [device] out float[N, 2]: m, the largest logit that takes part, and the sum of
+                                 * exp((z - m) / tau); what the gradient call reads */
+    int32_t *status;            /* [device] out int32[N] of TLI_ROW_* bits; may be NULL */
+} tli_loss_args;
+
+int tli_loss(tli_ctx *ctx, const tli_loss_args *args, void *cuda_stream);
+
+typedef struct {
+    int32_t N, k, dtype, side, ids_side, support, teacher_dtype;    /* as in tli_loss_args */
+    const void *logits;
+    int64_t stride;
+    const int32_t *ids;
+    const void *teacher;
+    const float *temperature;
+    const float *stats;         /* [device] float[N, 2], of tli_loss() */
+    const float *grad_loss;     /* [device] float[N]: what each row's loss is weighted with; NULL: 1 */
+    void *grad;                 /* [device] out [N, V] in the logits' type: every element of every row is written.  May be
+                                 * `logits` itself with the same stride (in place); rows that overlap others of its own
+                                 * or of the logits are refused (TLI_ERR_ARG) */
+    int64_t grad_stride;        /* elements from row to row, >= V */
+} tli_loss_grad_args;
+
+int tli_loss_grad(tli_ctx *ctx, const tli_loss_grad_args *args, void *cuda_stream);
 
 /*
  * How tli_verify() will run a batch of this shape on this context: [host]

@@ -3,3 +3,4 @@
 #include "tli.cu"
 #include "tli_rows.cu"
 #include "tli_embed.cu"
+#include "tli_loss.cu"

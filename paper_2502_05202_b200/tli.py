@@ -36,14 +36,18 @@ TLI_ROW_FALLBACK = 8
 TLI_ROW_TIMEOUT = 16
 TLI_ROW_BAD_TEMPERATURE = 32
 TLI_ROW_BAD_FILTER = 64
+TLI_ROW_LEFT_OUT = 128
 TLI_SIDE_TARGET = 0
 TLI_SIDE_DRAFTER = 1
+TLI_SUPPORT_ALL = 0
+TLI_SUPPORT_SHARED = 1
 TLI_MAX_B = 65535
 TLI_MAX_K = 64
 TLI_MAX_V = 1048576
 TLI_MAX_SHARDS = 64
 TLI_MAX_TOKENS = 4194304
 TLI_MAX_H = 65536
+TLI_MAX_TARGETS = 256
 TLI_STATIC_SCRATCH_BYTES = 4194304
 
 EXPORTS = ("tli_create", "tli_destroy", "tli_workspace_bytes", "tli_verify", "tli_verify_static", "tli_verify_profile", "tli_set_tiled", "tli_set_max_cluster", "tli_reset", "tli_selftest_bounded_wait",
@@ -51,6 +55,7 @@ EXPORTS = ("tli_create", "tli_destroy", "tli_workspace_bytes", "tli_verify", "tl
            "tli_verify_host_buffer_bytes", "tli_verify_host", "tli_rates_workspace_bytes", "tli_acceptance_rates",
            "tli_sample_workspace_bytes", "tli_sample", "tli_filter_workspace_bytes", "tli_filter",
            "tli_embed", "tli_embed_grad_workspace_bytes", "tli_embed_grad",
+           "tli_loss", "tli_loss_grad",
            "tli_ctx_info",
            "tli_shard_create", "tli_shard_info", "tli_shard_workspace_bytes", "tli_shard_record_bytes", "tli_shard_rows_bytes",
            "tli_shard_stats", "tli_shard_decide", "tli_shard_weights", "tli_shard_select",
@@ -159,6 +164,25 @@ class tli_embed_grad_args(ctypes.Structure):
     ]
 
 
+class tli_loss_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("support", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("stride", ctypes.c_int64), ("ids", ctypes.c_void_p), ("teacher", ctypes.c_void_p),
+        ("temperature", ctypes.c_void_p), ("loss", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("status", ctypes.c_void_p),
+    ]
+
+
+class tli_loss_grad_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("k", ctypes.c_int32), ("dtype", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("support", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("stride", ctypes.c_int64), ("ids", ctypes.c_void_p), ("teacher", ctypes.c_void_p),
+        ("temperature", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("grad_loss", ctypes.c_void_p),
+        ("grad", ctypes.c_void_p), ("grad_stride", ctypes.c_int64),
+    ]
+
+
 class TLIError(RuntimeError):
     def __init__(self, code: int, where: str):
         lib = load()
@@ -209,7 +233,7 @@ def load() -> ctypes.CDLL:
         lib.tli_acceptance_rates.argtypes = [ctypes.c_void_p, ctypes.POINTER(tli_rates_args), ctypes.c_void_p]
         lib.tli_acceptance_rates.restype = ctypes.c_int
         for name, args in (("tli_sample", tli_sample_args), ("tli_filter", tli_filter_args), ("tli_embed", tli_embed_args),
-                           ("tli_embed_grad", tli_embed_grad_args)):
+                           ("tli_embed_grad", tli_embed_grad_args), ("tli_loss", tli_loss_args), ("tli_loss_grad", tli_loss_grad_args)):
             getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.POINTER(args), ctypes.c_void_p]
             getattr(lib, name).restype = ctypes.c_int
         for name in ("tli_sample_workspace_bytes", "tli_filter_workspace_bytes"):
@@ -741,13 +765,15 @@ _PACK_SAMPLE = struct.Struct("@iiiiPqqPPPPPPPPPN").pack
 _PACK_FILTER = struct.Struct("@iiiiPqqPPPPPqqPPN").pack
 _PACK_EMBED = struct.Struct("@iiiiiPPqfPqP").pack
 _PACK_EMBED_GRAD = struct.Struct("@iiiiiiPPqfPqPN").pack
+_PACK_LOSS = struct.Struct("@iiiiiiiPqPPPPPP").pack
+_PACK_LOSS_GRAD = struct.Struct("@iiiiiiiPqPPPPPPq").pack
 
 
 def _packed_entries():
-    """The four entry points as functions of (ctx, packed struct, stream)."""
+    """The entry points of the calls below as functions of (ctx, packed struct, stream)."""
     load()
     lib = ctypes.CDLL(LIB_PATH)                                    # function objects of its own, the library is loaded once
-    entries = [lib.tli_sample, lib.tli_filter, lib.tli_embed, lib.tli_embed_grad]
+    entries = [lib.tli_sample, lib.tli_filter, lib.tli_embed, lib.tli_embed_grad, lib.tli_loss, lib.tli_loss_grad]
     for fn in entries:
         fn.argtypes, fn.restype = [ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p], ctypes.c_int
     return entries
@@ -773,7 +799,8 @@ class Verifier:
             tli_set_tiled(self.ctx, True)
         self._ws: Optional[torch.Tensor] = None
         self._index, self._plans = int(device), {}
-        self._fn_sample, self._fn_filter, self._fn_embed, self._fn_embed_grad = _packed_entries()
+        (self._fn_sample, self._fn_filter, self._fn_embed, self._fn_embed_grad, self._fn_loss,
+         self._fn_loss_grad) = _packed_entries()
         self._kept = threading.local()
 
     def close(self) -> None:
@@ -951,6 +978,67 @@ class Verifier:
         ws = self._scratch(need)
         self._call(self._fn_embed_grad, _PACK_EMBED_GRAD(N, H, _logit_dtype(grad), _logit_dtype(out), ids_side, table_side, ids.data_ptr(),
                                                          grad.data_ptr(), stride, scale, out.data_ptr(), H, ws.data_ptr(), need))
+        return {"grad": out}
+
+    # The losses.  `ids` [N] are labels; `ids` [N, k] with `teacher` [N, k] a teacher's logits of k ids.  `stats` and `target_logits` are
+    # the forward call's.  Like the other calls they record no autograd graph.
+
+    def _targets(self, N: int, ids, teacher, temperature, side: int, ids_side: int, shared: bool):
+        """((k, teacher's dtype, teacher's pointer), support) of a loss call; raises on what the library could not see."""
+        on = self._index
+        self._ids(ids)
+        if teacher is None:
+            k, t_dtype, t_ptr = 1, 0, 0
+            if ids.shape != (N,) and ids.shape != (N, 1):
+                raise ValueError("labels must be [%d]" % N)
+        else:
+            if ids.dim() != 2 or ids.shape[0] != N or teacher.shape != ids.shape or teacher.get_device() != on or not teacher.is_contiguous():
+                raise ValueError("ids and teacher must be contiguous [%d, k] tensors on %s" % (N, self.device))
+            k, t_dtype, t_ptr = ids.shape[1], _logit_dtype(teacher), teacher.data_ptr()
+        if temperature is not None:
+            self._per_row("temperature", temperature, (N,))
+        self._table_rows(side), self._table_rows(ids_side)
+        return k, t_dtype, t_ptr, TLI_SUPPORT_SHARED if shared else TLI_SUPPORT_ALL
+
+    def _per_row(self, name: str, t, shape) -> None:
+        if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous float32 tensor of shape %s on %s" % (name, tuple(shape), self.device))
+
+    def _loss_rows(self, logits, side: int) -> int:
+        if logits.dim() != 2 or logits.shape[1] != self._table_rows(side) or logits.get_device() != self._index:
+            raise ValueError("logits must be [N, %d] on %s" % (self._table_rows(side), self.device))
+        return _matrix("logits", logits)
+
+    def loss(self, logits, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET, ids_side: int = TLI_SIDE_TARGET,
+             shared: bool = False) -> Dict[str, torch.Tensor]:
+        """Loss of every row of ``logits`` [N,V] against labels ``ids`` [N], or a teacher's logits ``teacher`` [N,k] of ``ids`` [N,k];
+        ids of either vocabulary.  ``shared``: the softmax runs over the ids inside the intersection (drafter rows)."""
+        stride, N = self._loss_rows(logits, side), logits.shape[0]
+        k, t_dtype, t_ptr, support = self._targets(N, ids, teacher, temperature, side, ids_side, shared)
+        stats = torch.empty((N, 2), dtype=torch.float32, device=self.device)
+        loss = torch.empty((N,), dtype=torch.float32, device=self.device)
+        status = torch.empty_like(loss, dtype=torch.int32)
+        self._call(self._fn_loss, _PACK_LOSS(
+            N, k, _logit_dtype(logits), side, ids_side, support, t_dtype, logits.data_ptr(), stride, ids.data_ptr(), t_ptr,
+            0 if temperature is None else temperature.data_ptr(), loss.data_ptr(), stats.data_ptr(), status.data_ptr()))
+        return {"loss": loss, "stats": stats, "status": status}
+
+    def loss_grad(self, logits, ids, stats, grad_loss=None, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET,
+                  ids_side: int = TLI_SIDE_TARGET, shared: bool = False, out=None) -> Dict[str, torch.Tensor]:
+        """Gradient of sum(grad_loss * loss) with respect to the logits, in their type (``out=logits``: in place)."""
+        stride, N = self._loss_rows(logits, side), logits.shape[0]
+        k, t_dtype, t_ptr, support = self._targets(N, ids, teacher, temperature, side, ids_side, shared)
+        self._per_row("stats", stats, (N, 2))
+        if grad_loss is not None:
+            self._per_row("grad_loss", grad_loss, (N,))
+        if out is None:
+            out = logits.new_empty(logits.shape)
+        elif out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index:
+            raise ValueError("out must have the logits' type, shape and device")
+        self._call(self._fn_loss_grad, _PACK_LOSS_GRAD(
+            N, k, _logit_dtype(logits), side, ids_side, support, t_dtype, logits.data_ptr(), stride, ids.data_ptr(), t_ptr,
+            0 if temperature is None else temperature.data_ptr(), stats.data_ptr(), 0 if grad_loss is None else grad_loss.data_ptr(),
+            out.data_ptr(), _matrix("out", out)))
         return {"grad": out}
 
     def rates(self, target_logits, drafter_logits, temperature) -> Dict[str, torch.Tensor]:
