@@ -59,7 +59,7 @@ enum {
                                    * later call on the context reports it too, until tli_reset() */
     TLI_ROW_BAD_TEMPERATURE = 32, /* temperature negative or not finite: accepted = 0, next_token = 0 */
     TLI_ROW_BAD_FILTER = 64,      /* top_p or min_p is NaN (tli_sample(), tli_filter()) */
-    TLI_ROW_LEFT_OUT = 128        /* no target id of the row takes part (tli_loss()): loss and gradient 0 */
+    TLI_ROW_LEFT_OUT = 128        /* no target id of the row takes part (tli_loss(), tli_head_loss()): loss and gradient 0 */
 };
 
 /* which of the context's two vocabularies ids, rows of logits or an embedding table belong to */
@@ -71,7 +71,8 @@ enum { TLI_SIDE_TARGET = 0, TLI_SIDE_DRAFTER = 1 };
 #define TLI_MAX_SHARDS 64   /* vocabulary shards (tli_shard_create) */
 #define TLI_MAX_TOKENS 4194304 /* tokens per call of tli_embed() and tli_embed_grad() */
 #define TLI_MAX_H 65536     /* width of an embedding row */
-#define TLI_MAX_TARGETS 256 /* target ids per row of tli_loss() */
+#define TLI_MAX_TARGETS 256 /* target ids per row of tli_loss() and tli_head_loss() */
+#define TLI_MAX_HEAD_TOKENS 262144 /* rows per call of tli_head_loss() and tli_head_loss_grad() */
 #define TLI_STATIC_SCRATCH_BYTES 4194304 /* 4 MiB: scratch built into the library for tli_verify_static() */
 
 /*
@@ -586,7 +587,9 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *args, void *cuda_str
 /*
  * Losses for fine-tuning a drafter (or a target) on tokens of either vocabulary:
  * cross entropy against a label, or the divergence from a teacher's k largest
- * logits, say the target's for a drafter.
+ * logits, say the target's for a drafter.  tli_loss() takes rows of logits;
+ * tli_head_loss() takes hidden rows and the output head's weight and never
+ * writes the logits.
  *
  * Row n has k target ids of vocabulary ids_side, carried to the rows' vocabulary
  * as tli_embed() carries its ids.  With support TLI_SUPPORT_ALL every id of
@@ -648,6 +651,63 @@ typedef struct {
 } tli_loss_grad_args;
 
 int tli_loss_grad(tli_ctx *ctx, const tli_loss_grad_args *args, void *cuda_stream);
+
+/*
+ * The same loss with z = hidden * weight^T, bf16 operands with fp32 sums, the logits
+ * formed tile by tile and never written.  Rows that are left out cost nothing and
+ * may hold anything.
+ */
+typedef struct {
+    int32_t N;                  /* rows, 0 .. TLI_MAX_HEAD_TOKENS */
+    int32_t H;                  /* width of a hidden row, a multiple of 8, 8 .. TLI_MAX_H */
+    int32_t k;
+    int32_t side, ids_side, support, teacher_dtype;                 /* as in tli_loss_args */
+    const void *hidden;         /* [device] bf16 [N, H]; rows contiguous */
+    int64_t hidden_stride;      /* elements from row to row, >= 0 */
+    const void *weight;         /* [device] bf16 [V, H]; 16-byte aligned */
+    int64_t weight_stride;      /* elements from row to row, a multiple of 8, >= H */
+    const int32_t *ids;
+    const void *teacher;
+    const float *temperature;
+    float *loss, *stats;
+    float *target_logits;       /* [device] out float[N, k]: z of the target ids, 0 where one does not take part */
+    int32_t *status;            /* may be NULL */
+    void *workspace;            /* [device] scratch, 256-byte aligned, >= tli_head_loss_workspace_bytes() */
+    size_t workspace_bytes;
+} tli_head_loss_args;
+
+size_t tli_head_loss_workspace_bytes(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side);
+int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *args, void *cuda_stream);
+
+/*
+ * Its gradients: d hidden = g dz * weight and d weight = (g dz)^T * hidden, g = grad_loss.
+ * The logits are formed again for a run of the vocabulary at a time, g dz of that run is kept in
+ * the workspace in bf16 (the operand type of the two products), sums are fp32.
+ */
+typedef struct {
+    int32_t N, H, k, side, ids_side, support, teacher_dtype;        /* as in tli_head_loss_args */
+    const void *hidden;
+    int64_t hidden_stride;
+    const void *weight;
+    int64_t weight_stride;
+    const int32_t *ids;
+    const void *teacher;
+    const float *temperature;
+    const float *stats;         /* [device] float[N, 2], of tli_head_loss() */
+    const float *target_logits; /* [device] float[N, k], of tli_head_loss() */
+    const float *grad_loss;     /* [device] float[N]; NULL: 1 */
+    void *grad_hidden;          /* [device] out bf16 [N, H], every row written; NULL: not wanted */
+    int64_t grad_hidden_stride; /* elements from row to row, >= H */
+    void *grad_weight;          /* [device] out bf16 [V, H], every row written, 16-byte aligned; NULL: not wanted */
+    int64_t grad_weight_stride; /* elements from row to row, a multiple of 8, >= H */
+    int32_t *status;            /* [device] out int32[N]: TLI_ROW_TIMEOUT, or what tli_head_loss() found out about the
+                                 * row's targets and temperature; may be NULL */
+    void *workspace;            /* [device] scratch, 256-byte aligned, >= tli_head_loss_grad_workspace_bytes() */
+    size_t workspace_bytes;
+} tli_head_loss_grad_args;
+
+size_t tli_head_loss_grad_workspace_bytes(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side);
+int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *args, void *cuda_stream);
 
 /*
  * How tli_verify() will run a batch of this shape on this context: [host]

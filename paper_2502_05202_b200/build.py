@@ -8,7 +8,7 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 SRC = os.path.join(_HERE, "csrc", "tli_lib.cu")
-PARTS = [os.path.join(_HERE, "csrc", n) for n in ("tli.cu", "tli_rows.cu", "tli_embed.cu", "tli_loss.cu")]
+PARTS = [os.path.join(_HERE, "csrc", n) for n in ("tli.cu", "tli_rows.cu", "tli_embed.cu", "tli_loss.cu", "tli_head.cu")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(_HERE, "libtli.so")
 

@@ -4,3 +4,4 @@
 #include "tli_rows.cu"
 #include "tli_embed.cu"
 #include "tli_loss.cu"
+#include "tli_head.cu"

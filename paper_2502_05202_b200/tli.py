@@ -48,6 +48,7 @@ TLI_MAX_SHARDS = 64
 TLI_MAX_TOKENS = 4194304
 TLI_MAX_H = 65536
 TLI_MAX_TARGETS = 256
+TLI_MAX_HEAD_TOKENS = 262144
 TLI_STATIC_SCRATCH_BYTES = 4194304
 
 EXPORTS = ("tli_create", "tli_destroy", "tli_workspace_bytes", "tli_verify", "tli_verify_static", "tli_verify_profile", "tli_set_tiled", "tli_set_max_cluster", "tli_reset", "tli_selftest_bounded_wait",
@@ -56,6 +57,7 @@ EXPORTS = ("tli_create", "tli_destroy", "tli_workspace_bytes", "tli_verify", "tl
            "tli_sample_workspace_bytes", "tli_sample", "tli_filter_workspace_bytes", "tli_filter",
            "tli_embed", "tli_embed_grad_workspace_bytes", "tli_embed_grad",
            "tli_loss", "tli_loss_grad",
+           "tli_head_loss_workspace_bytes", "tli_head_loss", "tli_head_loss_grad_workspace_bytes", "tli_head_loss_grad",
            "tli_ctx_info",
            "tli_shard_create", "tli_shard_info", "tli_shard_workspace_bytes", "tli_shard_record_bytes", "tli_shard_rows_bytes",
            "tli_shard_stats", "tli_shard_decide", "tli_shard_weights", "tli_shard_select",
@@ -183,6 +185,30 @@ class tli_loss_grad_args(ctypes.Structure):
     ]
 
 
+class tli_head_loss_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("k", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("support", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+        ("hidden", ctypes.c_void_p), ("hidden_stride", ctypes.c_int64), ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_int64),
+        ("ids", ctypes.c_void_p), ("teacher", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+        ("loss", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("target_logits", ctypes.c_void_p), ("status", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class tli_head_loss_grad_args(ctypes.Structure):
+    _fields_ = [
+        ("N", ctypes.c_int32), ("H", ctypes.c_int32), ("k", ctypes.c_int32), ("side", ctypes.c_int32),
+        ("ids_side", ctypes.c_int32), ("support", ctypes.c_int32), ("teacher_dtype", ctypes.c_int32),
+        ("hidden", ctypes.c_void_p), ("hidden_stride", ctypes.c_int64), ("weight", ctypes.c_void_p), ("weight_stride", ctypes.c_int64),
+        ("ids", ctypes.c_void_p), ("teacher", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+        ("stats", ctypes.c_void_p), ("target_logits", ctypes.c_void_p), ("grad_loss", ctypes.c_void_p),
+        ("grad_hidden", ctypes.c_void_p), ("grad_hidden_stride", ctypes.c_int64),
+        ("grad_weight", ctypes.c_void_p), ("grad_weight_stride", ctypes.c_int64), ("status", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 class TLIError(RuntimeError):
     def __init__(self, code: int, where: str):
         lib = load()
@@ -233,10 +259,14 @@ def load() -> ctypes.CDLL:
         lib.tli_acceptance_rates.argtypes = [ctypes.c_void_p, ctypes.POINTER(tli_rates_args), ctypes.c_void_p]
         lib.tli_acceptance_rates.restype = ctypes.c_int
         for name, args in (("tli_sample", tli_sample_args), ("tli_filter", tli_filter_args), ("tli_embed", tli_embed_args),
-                           ("tli_embed_grad", tli_embed_grad_args), ("tli_loss", tli_loss_args), ("tli_loss_grad", tli_loss_grad_args)):
+                           ("tli_embed_grad", tli_embed_grad_args), ("tli_loss", tli_loss_args), ("tli_loss_grad", tli_loss_grad_args),
+                           ("tli_head_loss", tli_head_loss_args), ("tli_head_loss_grad", tli_head_loss_grad_args)):
             getattr(lib, name).argtypes = [ctypes.c_void_p, ctypes.POINTER(args), ctypes.c_void_p]
             getattr(lib, name).restype = ctypes.c_int
         for name in ("tli_sample_workspace_bytes", "tli_filter_workspace_bytes"):
+            getattr(lib, name).argtypes = [ctypes.c_void_p] + [ctypes.c_int32] * 4
+            getattr(lib, name).restype = ctypes.c_size_t
+        for name in ("tli_head_loss_workspace_bytes", "tli_head_loss_grad_workspace_bytes"):
             getattr(lib, name).argtypes = [ctypes.c_void_p] + [ctypes.c_int32] * 4
             getattr(lib, name).restype = ctypes.c_size_t
         lib.tli_embed_grad_workspace_bytes.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32]
@@ -621,6 +651,14 @@ def tli_embed_grad_workspace_bytes(ctx: int, N: int, H: int) -> int:
     return int(load().tli_embed_grad_workspace_bytes(ctx, N, H))
 
 
+def tli_head_loss_workspace_bytes(ctx: int, N: int, H: int, k: int, side: int) -> int:
+    return int(load().tli_head_loss_workspace_bytes(ctx, N, H, k, side))
+
+
+def tli_head_loss_grad_workspace_bytes(ctx: int, N: int, H: int, k: int, side: int) -> int:
+    return int(load().tli_head_loss_grad_workspace_bytes(ctx, N, H, k, side))
+
+
 def make_embed_grad_args(ids: torch.Tensor, grad: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
                          ids_side: int = TLI_SIDE_TARGET, table_side: int = TLI_SIDE_TARGET) -> tli_embed_grad_args:
     """Fill a tli_embed_grad_args from device tensors (no copies; the tensors must outlive the call)."""
@@ -767,13 +805,16 @@ _PACK_EMBED = struct.Struct("@iiiiiPPqfPqP").pack
 _PACK_EMBED_GRAD = struct.Struct("@iiiiiiPPqfPqPN").pack
 _PACK_LOSS = struct.Struct("@iiiiiiiPqPPPPPP").pack
 _PACK_LOSS_GRAD = struct.Struct("@iiiiiiiPqPPPPPPq").pack
+_PACK_HEAD_LOSS = struct.Struct("@iiiiiiiPqPqPPPPPPPPN").pack
+_PACK_HEAD_LOSS_GRAD = struct.Struct("@iiiiiiiPqPqPPPPPPPqPqPPN").pack
 
 
 def _packed_entries():
     """The entry points of the calls below as functions of (ctx, packed struct, stream)."""
     load()
     lib = ctypes.CDLL(LIB_PATH)                                    # function objects of its own, the library is loaded once
-    entries = [lib.tli_sample, lib.tli_filter, lib.tli_embed, lib.tli_embed_grad, lib.tli_loss, lib.tli_loss_grad]
+    entries = [lib.tli_sample, lib.tli_filter, lib.tli_embed, lib.tli_embed_grad, lib.tli_loss, lib.tli_loss_grad,
+               lib.tli_head_loss, lib.tli_head_loss_grad]
     for fn in entries:
         fn.argtypes, fn.restype = [ctypes.c_void_p, ctypes.c_char_p, ctypes.c_void_p], ctypes.c_int
     return entries
@@ -800,7 +841,7 @@ class Verifier:
         self._ws: Optional[torch.Tensor] = None
         self._index, self._plans = int(device), {}
         (self._fn_sample, self._fn_filter, self._fn_embed, self._fn_embed_grad, self._fn_loss,
-         self._fn_loss_grad) = _packed_entries()
+         self._fn_loss_grad, self._fn_head_loss, self._fn_head_loss_grad) = _packed_entries()
         self._kept = threading.local()
 
     def close(self) -> None:
@@ -1040,6 +1081,58 @@ class Verifier:
             0 if temperature is None else temperature.data_ptr(), stats.data_ptr(), 0 if grad_loss is None else grad_loss.data_ptr(),
             out.data_ptr(), _matrix("out", out)))
         return {"grad": out}
+
+    def _head(self, hidden, weight, k: int, side: int, grad: bool):
+        """(N, H, stride of hidden, stride of weight, scratch) of a head call; raises on what the library could not see."""
+        V, on = self._table_rows(side), self._index
+        if hidden.dim() != 2 or hidden.dtype is not torch.bfloat16 or hidden.get_device() != on:
+            raise ValueError("hidden must be a bfloat16 [N, H] tensor on %s" % self.device)
+        N, H = hidden.shape
+        if weight.dtype is not torch.bfloat16 or weight.shape != (V, H) or weight.get_device() != on:
+            raise ValueError("weight must be a bfloat16 [%d, %d] tensor on %s" % (V, H, self.device))
+        key = (N, H, k, side, grad)
+        need = self._plans.get(key)
+        if need is None:
+            need = self._plan(key, (tli_head_loss_grad_workspace_bytes if grad else tli_head_loss_workspace_bytes)(self.ctx, N, H, k, side))
+        if need == 0:
+            raise TLIError(TLI_ERR_UNSUPPORTED, "tli_head_loss_workspace_bytes (H a multiple of 8 up to %d, N up to %d)" % (TLI_MAX_H, TLI_MAX_HEAD_TOKENS))
+        return N, H, _matrix("hidden", hidden), _matrix("weight", weight), self._scratch(need), need
+
+    def head_loss(self, hidden, weight, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET,
+                  ids_side: int = TLI_SIDE_TARGET, shared: bool = False) -> Dict[str, torch.Tensor]:
+        """:meth:`loss` of the logits ``hidden`` [N,H] x ``weight`` [V,H]^T (bfloat16, summed in fp32), which are not written."""
+        k, t_dtype, t_ptr, support = self._targets(hidden.shape[0], ids, teacher, temperature, side, ids_side, shared)
+        N, H, hs, wst, ws, need = self._head(hidden, weight, k, side, False)
+        dev = self.device
+        stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
+        loss = torch.empty((N,), dtype=torch.float32, device=dev)
+        status = torch.empty_like(loss, dtype=torch.int32)
+        at = torch.empty_like(ids, dtype=torch.float32)
+        self._call(self._fn_head_loss, _PACK_HEAD_LOSS(
+            N, H, k, side, ids_side, support, t_dtype, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr,
+            0 if temperature is None else temperature.data_ptr(), loss.data_ptr(), stats.data_ptr(), at.data_ptr(), status.data_ptr(),
+            ws.data_ptr(), need))
+        return {"loss": loss, "stats": stats, "target_logits": at, "status": status}
+
+    def head_loss_grad(self, hidden, weight, ids, stats, target_logits, grad_loss=None, teacher=None, temperature=None,
+                       side: int = TLI_SIDE_TARGET, ids_side: int = TLI_SIDE_TARGET, shared: bool = False,
+                       hidden_grad: bool = True, weight_grad: bool = True) -> Dict[str, Optional[torch.Tensor]]:
+        """Gradients of sum(grad_loss * loss) with respect to ``hidden`` and ``weight``, in bfloat16 (``None`` where not asked for)."""
+        k, t_dtype, t_ptr, support = self._targets(hidden.shape[0], ids, teacher, temperature, side, ids_side, shared)
+        N, H, hs, wst, ws, need = self._head(hidden, weight, k, side, True)
+        self._per_row("stats", stats, (N, 2))
+        self._per_row("target_logits", target_logits, ids.shape)
+        if grad_loss is not None:
+            self._per_row("grad_loss", grad_loss, (N,))
+        dh = torch.empty((N, H), dtype=torch.bfloat16, device=self.device) if hidden_grad else None
+        dw = torch.empty((weight.shape[0], H), dtype=torch.bfloat16, device=self.device) if weight_grad else None
+        status = torch.empty((N,), dtype=torch.int32, device=self.device)
+        self._call(self._fn_head_loss_grad, _PACK_HEAD_LOSS_GRAD(
+            N, H, k, side, ids_side, support, t_dtype, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr,
+            0 if temperature is None else temperature.data_ptr(), stats.data_ptr(), target_logits.data_ptr(),
+            0 if grad_loss is None else grad_loss.data_ptr(), 0 if dh is None else dh.data_ptr(), H, 0 if dw is None else dw.data_ptr(), H,
+            status.data_ptr(), ws.data_ptr(), need))
+        return {"grad_hidden": dh, "grad_weight": dw, "status": status}
 
     def rates(self, target_logits, drafter_logits, temperature) -> Dict[str, torch.Tensor]:
         """Expected acceptance rates per draft position (mass, alpha_union, alpha_tli); device tensors."""

@@ -7,7 +7,8 @@ import numpy as np
 import loss_oracle as lo
 from paper_2502_05202_b200 import build as tli_build, tli
 
-CALLS = (("tli_loss", tli.tli_loss_args, "_PACK_LOSS"), ("tli_loss_grad", tli.tli_loss_grad_args, "_PACK_LOSS_GRAD"))
+CALLS = (("tli_loss", tli.tli_loss_args, "_PACK_LOSS"), ("tli_loss_grad", tli.tli_loss_grad_args, "_PACK_LOSS_GRAD"),
+         ("tli_head_loss", tli.tli_head_loss_args, "_PACK_HEAD_LOSS"), ("tli_head_loss_grad", tli.tli_head_loss_grad_args, "_PACK_HEAD_LOSS_GRAD"))
 
 
 def test_null_arguments_are_refused():
@@ -16,6 +17,7 @@ def test_null_arguments_are_refused():
     for name, args, _ in CALLS:
         assert getattr(lib, name)(None, ctypes.byref(args()), None) == tli.TLI_ERR_ARG
         assert getattr(lib, name)(None, None, None) == tli.TLI_ERR_ARG
+    assert lib.tli_head_loss_workspace_bytes(None, 1, 8, 1, 0) == 0 and lib.tli_head_loss_grad_workspace_bytes(None, 1, 8, 1, 0) == 0
 
 
 def test_packed_arguments_are_laid_out_as_the_structs():
