@@ -4,19 +4,20 @@
 // A call is a chain of launches:
 //   tli_head_targets_kernel   which rows take part, one bit each; for the gradient what their slopes are made of.
 //   tli_head_gather_kernel    those rows of `hidden` one after the other (work is in proportion to them, any stride and alignment will
-//                             do, and a row that is left out may hold anything).
+//                             do, and a row that is left out may hold anything); for few rows tli_head_prepare_kernel does both.
 //   tli_head_gemm_kernel      <STATS>  forward: (max, sum) of every row over every tile of the vocabulary.
 //   tli_head_loss_kernel               forward: the tiles' pairs joined, the targets' logits, the loss.
-//                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace;
-//   tli_head_patch_kernel              the targets' elements of G again;
+//                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace,
 //                             <GRADS>  d hidden += G * weight and d weight = G^T * hidden of that run, one list of tiles.
 //   tli_head_rows_kernel      d hidden from its fp32 sums to bf16, at the rows' places.
 // The run keeps G near the size of L2 (128 MB), whatever the vocabulary.
 //
 // tli_head_gemm_kernel: persistent, one CTA per SM or one pair (CG = 2) per two SMs.  A tile of D is 128 CG rows x 256 columns of fp32 in
 // tensor memory, two of them, so that the epilogue of one runs under the products of the next.  Warp 0 fills a ring of stages of
-// 64 elements of the contracted axis by TMA, warp 1 issues tcgen05.mma (bf16, fp32 sums), warps 2 to 5 are the epilogue, a thread per
-// row of D.  With CG = 2 each CTA loads half of both operands and the pair's leader issues the products of both.
+// 64 elements of the contracted axis by TMA, warp 1 issues tcgen05.mma (bf16, fp32 sums), warps 2 to 9 are the epilogue: two threads per
+// row of D, 128 columns each (with one thread per row it took 6 us a tile, as long as the products at H = 1024).  What leaves, leaves by
+// TMA from a slab of each warp's own, so that no warp waits for another.  (Four threads per row and slabs for them take the room of a
+// stage: 17 % slower where the products count.)  With CG = 2 each CTA loads half of both operands and the pair's leader issues the products of both.
 // Operands come as they lie in memory: rows along the contracted axis (K-major) or across it (MN-major), 128-byte swizzle either way.
 // All waits are bounded: when one runs out the context's error word is set, every role stops, copies in flight are waited for, tensor
 // memory is given back, and the rows' status says TLI_ROW_TIMEOUT.
@@ -25,11 +26,16 @@
 
 namespace {
 
-constexpr int kHeadThreads = 192;
+constexpr int kHeadEpilogue = 8;           // warps of the epilogue: two per quarter of the rows, 128 columns each
+constexpr int kHeadThreads = 64 + 32 * kHeadEpilogue;
+// The matrix unit cuts what a sum cannot hold (it does not round): a sum of 2048 products of a logit was 1e-5 off where one rounded at every step
+// is 4e-6 off.  The logits that the statistics are made of are therefore summed in parts, which the epilogue adds up: 256 elements where the
+// weight's way through the SM is what counts (no slower than one part), else half of H but 512 to 1024 (8192 x 128 256 x 2048: one part
+// 3.07 ms and 1e-5 off, two 3.16 and 5e-6, four 3.35 and 2e-6).
 constexpr int kHeadK = 64;                 // elements of the contracted axis in a stage: 128 bytes, one swizzle span
 constexpr int kHeadN = 256;                // columns of a tile
 constexpr int kHeadABytes = 128 * kHeadK * 2;
-constexpr int kHeadStageBuf = 128 * 128;   // a slab of the epilogue's on its way out: 128 rows of 128 bytes
+constexpr int kHeadSlab = 32 * 128;        // what a warp of the epilogue has on its way out: 32 rows of 128 bytes
 constexpr int kHeadRowBlock = 32;          // rows per CTA of the targets and gather kernels
 enum : int { HEAD_STATS = 0, HEAD_SLOPE = 1, HEAD_GRADS = 2 };
 
@@ -37,7 +43,7 @@ template <int CG> struct HeadRing {
     static constexpr int kStages = CG == 1 ? 4 : 6;
     static constexpr int kBBytes = kHeadN / CG * kHeadK * 2;
     static constexpr int kStageBytes = kHeadABytes + kBBytes;
-    static constexpr int kSmem = kStages * kStageBytes + 2 * kHeadStageBuf + 1024;
+    static constexpr int kSmem = kStages * kStageBytes + kHeadEpilogue * kHeadSlab + 1024;
 };
 
 struct HeadGemm {
@@ -47,11 +53,13 @@ struct HeadGemm {
     const int *n_valid;
     unsigned *error;
     int H, V, c0, cols;                    // the run of the vocabulary: [c0, c0 + cols)
-    int bn;                                // STATS, SLOPE: columns of a tile
+    int bn, k_part;                        // STATS, SLOPE: columns of a tile; STATS: stages of a part of a sum
+    int early;                             // one row block: what a CTA does first does not depend on how many rows take part
     int a_rows;                            // rows of a box of a
     int splits, first, want_dh, want_dw;   // GRADS: runs the contraction of d hidden is cut into; whether its sums start here
     const uint32_t *mask;
     const float4 *rowp;                    // {s, m, f, -} of a row
+    const int *tid; const float *tval; int k;     // SLOPE: the rows' targets, ids (-1) and elements of G
     float2 *part; long long part_pitch;    // STATS: [tile of the vocabulary][row]
 };
 
@@ -89,6 +97,15 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&x)[32]) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&x)[16]) {
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                   "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(r[i]);
+}
 // A box of a tensor to shared memory.  CG = 2: counted on the barrier at `bar`, which may be the pair's other CTA's.
 template <int CG> __device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     if constexpr (CG == 1)
@@ -116,7 +133,7 @@ struct HeadTile {
 template <int MODE, int CG> struct HeadTiles {
     int mb, nb, hb, t2, total, k2, k3;
     __device__ __forceinline__ HeadTiles(const HeadGemm &P, int rows) {
-        mb = (rows + 128 * CG - 1) / (128 * CG);
+        mb = P.early ? 1 : (rows + 128 * CG - 1) / (128 * CG);
         if constexpr (MODE == HEAD_GRADS) {
             hb = (P.H + kHeadN - 1) / kHeadN;
             nb = (P.cols + 128 * CG - 1) / (128 * CG);
@@ -174,7 +191,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < R::kStages; ++i) { mbar_init(&sm.full[i], 1); mbar_init(&sm.empty[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&sm.tfull[i], 1); mbar_init(&sm.tempty[i], 4 * CG); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&sm.tfull[i], 1); mbar_init(&sm.tempty[i], kHeadEpilogue * CG); }
         mbar_init(&sm.drain, 1);
         sm.error = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -193,10 +210,36 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
     if constexpr (CG == 2) cluster_barrier();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
+    const int first_tile = blockIdx.x / CG, step = gridDim.x / CG;
+    // The weight's boxes of step k of a tile; stages are counted by it.
+    auto load_weight = [&](const HeadTile &w, int k, unsigned st) {
+        const uint32_t b = ring + st * R::kStageBytes + kHeadABytes, bar = CG == 1 ? smem_addr(&sm.full[st]) : cluster_addr(smem_addr(&sm.full[st]), 0u);
+        const int x = w.k0 + k * kHeadK;
+        if constexpr (MODE != HEAD_GRADS) {
+            tensor_load<CG>(b, &P.b, x, P.c0 + w.n + static_cast<int>(rank) * (P.bn / CG), bar);
+        } else {
+            for (int i = 0; i < kHeadN / CG / 64; ++i) tensor_load<CG>(b + i * 8192, &P.b, w.n + static_cast<int>(rank) * (kHeadN / CG) + i * 64, P.c0 + x, bar);
+        }
+    };
+    const unsigned bytes = CG * ((MODE == HEAD_GRADS ? static_cast<unsigned>(kHeadABytes) : P.a_rows * (kHeadK * 2u)) + static_cast<unsigned>((MODE == HEAD_GRADS ? kHeadN : P.bn) / CG) * (kHeadK * 2u));
+    // The weight is an input of the call, and the call's first kernel lets its dependents start only when the kernels before the call are
+    // done: it may be read before the kernels in between are.
+    unsigned early = 0;
+    if (P.early && threadIdx.x == 0) {
+        const HeadTiles<MODE, CG> tiles(P, 1);
+        if (first_tile < (MODE == HEAD_GRADS ? tiles.t2 : tiles.total)) {
+            const HeadTile w = tiles.at(P, first_tile);
+            early = min(w.ks, R::kStages);
+            for (unsigned k = 0; k < early; ++k) {
+                if (rank == 0) mbar_arrive_expect_tx(&sm.full[k], bytes);
+                load_weight(w, k, k);
+            }
+        }
+    }
+    __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = *reinterpret_cast<const volatile int *>(P.n_valid);
     const HeadTiles<MODE, CG> tiles(P, rows);
-    const int first_tile = blockIdx.x / CG, step = gridDim.x / CG;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -206,23 +249,19 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             for (int t = first_tile; t < tiles.total && ok; t += step) {
                 const HeadTile w = tiles.at(P, t);
                 const int m = w.m + static_cast<int>(rank) * 128;
-                const bool dw = MODE == HEAD_GRADS && w.split < 0, dh = MODE == HEAD_GRADS && !dw;
-                const int bn = MODE == HEAD_GRADS ? kHeadN : P.bn;
-                const unsigned bytes = (MODE == HEAD_GRADS ? static_cast<unsigned>(kHeadABytes) : P.a_rows * (kHeadK * 2u)) + static_cast<unsigned>(bn / CG) * (kHeadK * 2u);
                 for (int k = 0; k < w.ks; ++k, ++it) {
                     const unsigned st = it % R::kStages, par = (it / R::kStages + 1) & 1u;
-                    ok = mbar_wait(&sm.empty[st], par, &sm.error, P.error);
-                    if (!ok) break;
                     const uint32_t a = ring + st * R::kStageBytes, b = a + kHeadABytes;
                     const uint32_t bar = CG == 1 ? smem_addr(&sm.full[st]) : cluster_addr(smem_addr(&sm.full[st]), 0u);
-                    if (CG == 1 || rank == 0) mbar_arrive_expect_tx(&sm.full[st], bytes * CG);
                     const int x = w.k0 + k * kHeadK;
-                    if constexpr (MODE != HEAD_GRADS) {
+                    if (it >= early) {
+                        ok = mbar_wait(&sm.empty[st], par, &sm.error, P.error);
+                        if (!ok) break;
+                        if (rank == 0) mbar_arrive_expect_tx(&sm.full[st], bytes);
+                        if (MODE != HEAD_GRADS || w.split >= 0) load_weight(w, k, st);
+                    }
+                    if (MODE != HEAD_GRADS || w.split >= 0) {      // rows [rows, H], or G [rows, run], along the contracted axis
                         tensor_load<CG>(a, &P.a, x, m, bar);
-                        tensor_load<CG>(b, &P.b, x, P.c0 + w.n + static_cast<int>(rank) * (bn / CG), bar);
-                    } else if (dh) {                               // G [rows, run], weight [run, H] across the contracted axis
-                        tensor_load<CG>(a, &P.a, x, m, bar);
-                        for (int i = 0; i < kHeadN / CG / 64; ++i) tensor_load<CG>(b + i * 8192, &P.b, w.n + static_cast<int>(rank) * (kHeadN / CG) + i * 64, P.c0 + x, bar);
                     } else {                                       // both across it
                         for (int i = 0; i < 2; ++i) tensor_load<CG>(a + i * 8192, &P.a2, m + i * 64, x, bar);
                         for (int i = 0; i < kHeadN / CG / 64; ++i) tensor_load<CG>(b + i * 8192, &P.b2, w.n + static_cast<int>(rank) * (kHeadN / CG) + i * 64, x, bar);
@@ -241,29 +280,32 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             const uint32_t base = 1u << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(128 * CG >> 4) << 24;
             unsigned it = 0, acc = 0;
             bool ok = true;
-            for (int t = first_tile; t < tiles.total && ok; t += step, ++acc) {
+            for (int t = first_tile; t < tiles.total && ok; t += step) {
                 const HeadTile w = tiles.at(P, t);
                 const bool dw = MODE == HEAD_GRADS && w.split < 0, dh = MODE == HEAD_GRADS && !dw;
                 const int bn = MODE == HEAD_GRADS ? kHeadN : P.bn;
                 const uint32_t idesc = base | static_cast<uint32_t>(bn >> 3) << 17 | (dw ? 1u << 15 | 1u << 16 : dh ? 1u << 16 : 0u);
                 const uint32_t a_step = dw ? 128u : 2u, b_step = dw || dh ? 128u : 2u;        // 16 elements of the contracted axis, in 16 bytes
-                ok = mbar_wait(&sm.tempty[acc & 1], (acc >> 1 & 1u) ^ 1u, &sm.error, P.error);
-                if (!ok) break;
-                tmem_fence_after();
-                const uint32_t d = tmem + (acc & 1) * kHeadN;
-                for (int k = 0; k < w.ks; ++k, ++it) {
-                    const unsigned st = it % R::kStages;
-                    ok = mbar_wait(&sm.full[st], (it / R::kStages) & 1u, &sm.error, P.error);
+                const int part = MODE == HEAD_STATS ? P.k_part : max(w.ks, 1);
+                for (int k0 = 0; ok && (k0 < w.ks || k0 == 0); k0 += part, ++acc) {
+                    ok = mbar_wait(&sm.tempty[acc & 1], (acc >> 1 & 1u) ^ 1u, &sm.error, P.error);
                     if (!ok) break;
                     tmem_fence_after();
-                    const uint32_t a = ring + st * R::kStageBytes, b = a + kHeadABytes;
-                    // across: blocks of 64 are 8 KB apart, groups of 8 of the contracted axis 1 KB; along: groups of 8 rows 1 KB
-                    uint64_t ad = dw ? umma_desc(a, 8192, 1024) : umma_desc(a, 16, 1024), bd = dw || dh ? umma_desc(b, 8192, 1024) : umma_desc(b, 16, 1024);
+                    const uint32_t d = tmem + (acc & 1) * kHeadN;
+                    for (int k = k0; k < min(w.ks, k0 + part); ++k, ++it) {
+                        const unsigned st = it % R::kStages;
+                        ok = mbar_wait(&sm.full[st], (it / R::kStages) & 1u, &sm.error, P.error);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        const uint32_t a = ring + st * R::kStageBytes, b = a + kHeadABytes;
+                        // across: blocks of 64 are 8 KB apart, groups of 8 of the contracted axis 1 KB; along: groups of 8 rows 1 KB
+                        uint64_t ad = dw ? umma_desc(a, 8192, 1024) : umma_desc(a, 16, 1024), bd = dw || dh ? umma_desc(b, 8192, 1024) : umma_desc(b, 16, 1024);
 #pragma unroll
-                    for (int i = 0; i < kHeadK / 16; ++i) umma<CG>(d, ad + i * a_step, bd + i * b_step, idesc, (k | i) != 0);
-                    umma_commit<CG>(&sm.empty[st]);
+                        for (int i = 0; i < kHeadK / 16; ++i) umma<CG>(d, ad + i * a_step, bd + i * b_step, idesc, (k - k0 | i) != 0);
+                        umma_commit<CG>(&sm.empty[st]);
+                    }
+                    if (ok) umma_commit<CG>(&sm.tfull[acc & 1]);
                 }
-                if (ok) umma_commit<CG>(&sm.tfull[acc & 1]);
             }
             if (!ok) {
                 umma_commit<CG>(&sm.drain);
@@ -271,159 +313,219 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             }
         }
     } else {
-        const int quarter = warp & 3, row = quarter * 32 + lane;
-        const bool issuer = warp == 2 && lane == 0;
-        const uint32_t tm = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-        unsigned acc = 0, slabs = 0;
+        const int quarter = warp & 3, group = warp - 2 >> 2, row = quarter * 32 + lane, c0 = group * 128;
+        const uint32_t mine = slab + (warp - 2) * kHeadSlab;       // this warp's slab
+        const uint32_t tm = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c0;
+        unsigned acc = 0, turn = 0;
         bool ok = true;
-        // the row's 128 bytes of a slab, 16 at a time, and the slab on its way
+        // 16 bytes of this thread's row of the slab; the slab is free again; the slab is full, and lane 0 may send it
+        auto slab_put = [&](int i, const uint4 &v) { st_shared16(mine + lane * 128 + ((i ^ (lane & 7)) << 4), v); };
         auto slab_free = [&]() {
-            if (issuer) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            __syncwarp();                                          // (a barrier counts warps: a parted one would count twice)
-            asm volatile("bar.sync 1, 128;" ::: "memory");
-            return slab + (slabs++ & 1) * kHeadStageBuf;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+            __syncwarp();
         };
         auto slab_full = [&]() {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
-            asm volatile("bar.sync 1, 128;" ::: "memory");
         };
-        auto slab_at = [&](uint32_t s, int i) { return s + row * 128 + ((i ^ (row & 7)) << 4); };
-        for (int t = first_tile; t < tiles.total; t += step, ++acc) {
+        for (int t = first_tile; t < tiles.total; t += step) {
             const HeadTile w = tiles.at(P, t);
-            const int m = w.m + static_cast<int>(rank) * 128, pos = m + row;
+            const int m = w.m + static_cast<int>(rank) * 128, pos = m + row, m_warp = m + quarter * 32;
             // What depends on the row is a value here and no branch: a compiler that makes two paths of one (rows that count and rows that
             // do not) parts the warp in front of the instructions below that a whole warp has to take.
             float s = 0.f, top = 0.f, f = 0.f;
-            uint32_t live = pos < rows ? 0xffffffffu : 0u, store = issuer && (MODE == HEAD_GRADS && w.split < 0 ? P.c0 + m < P.V : m < rows);
+            uint32_t live = pos < rows ? 0xffffffffu : 0u, store = lane == 0 && (MODE == HEAD_GRADS && w.split < 0 ? P.c0 + m_warp < P.V : m_warp < rows);
             asm volatile("" : "+r"(live), "+r"(store));
             if constexpr (MODE != HEAD_GRADS) {
-                const float4 r = __ldg(P.rowp + min(pos, rows - 1));
+                const float4 r = __ldg(P.rowp + max(0, min(pos, rows - 1)));
                 s = r.x; top = r.y; f = r.z;
             }
-            if (lane == 0) ok = ok && mbar_wait(&sm.tfull[acc & 1], acc >> 1 & 1u, &sm.error, P.error);
-            __syncwarp();
-            // (after a time-out the warps still meet at the slabs' barriers, tile by tile, with whatever tensor memory holds)
-            tmem_fence_after();
-            const uint32_t d = tm + (acc & 1) * kHeadN;
+            // A sum has been formed; (after a time-out the warps go on, tile by tile, with whatever tensor memory holds)
+            auto sum_wait = [&]() {
+                if (lane == 0) ok = ok && mbar_wait(&sm.tfull[acc & 1], acc >> 1 & 1u, &sm.error, P.error);
+                __syncwarp();
+                tmem_fence_after();
+                return tm + (acc & 1) * kHeadN;
+            };
+            // ... and has been read
+            auto sum_free = [&]() {
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 1) mbar_arrive(&sm.tempty[acc & 1]);
+                    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr(smem_addr(&sm.tempty[acc & 1]), 0u)) : "memory");
+                }
+                ++acc;
+            };
+            // which of 32 columns from column c of the tile on take part
+            auto columns = [&](int c) {
+                const int left = c < (MODE == HEAD_GRADS ? kHeadN : P.bn) ? P.cols - w.n - c : 0;
+                uint32_t bits = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
+                if (P.mask && left > 0) bits &= __ldg(P.mask + ((P.c0 + w.n + c) >> 5));
+                return bits;
+            };
             if constexpr (MODE == HEAD_STATS) {
-                float best = kMaskBelow, sum = 0.f;
-                if (m < rows) {
+                const bool any = m_warp < rows && c0 < P.bn;       // the same for the warp
+                float x[4][32];
+                const uint32_t d0 = sum_wait();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_load32(d0 + q * 32, x[q]);
+                tmem_wait_load();
+                sum_free();
 #pragma unroll 1
-                    for (int c = 0; c < P.bn; c += 32) {
-                        float x[32];
-                        tmem_load32(d + c, x);
-                        tmem_wait_load();
-                        const int col = w.n + c, left = P.cols - col;
-                        uint32_t bits = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
-                        if (P.mask && left > 0) bits &= __ldg(P.mask + ((P.c0 + col) >> 5));
+                for (int k0 = P.k_part; k0 < w.ks; k0 += P.k_part) {
+                    const uint32_t d = sum_wait();
+                    if (any) {
+#pragma unroll
+                        for (int i0 = 0; i0 < 128; i0 += 16) {
+                            float y[16];
+                            tmem_load16(d + i0, y);
+                            tmem_wait_load();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i0 >> 5][(i0 & 31) + i] += y[i];
+                        }
+                    }
+                    sum_free();
+                }
+                float best = kMaskBelow, sum = 0.f;
+                if (any) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t bits = columns(c0 + q * 32);
                         if (bits != 0xffffffffu) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = bits >> i & 1u ? x[i] : -INFINITY;
+                            for (int i = 0; i < 32; ++i) x[q][i] = bits >> i & 1u ? x[q][i] : -INFINITY;
                         }
-                        float high = x[0];
-#pragma unroll
-                        for (int i = 1; i < 32; ++i) high = fmaxf(high, x[i]);
-                        if (high > best) {
-                            sum *= ex2((best - high) * s);
-                            best = high;
-                        }
-                        const uint64_t s2 = pack2(s, s), c2 = pack2(-best, -best);
-                        uint64_t a2[2] = {pack2(sum, 0.f), 0ull};
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            float y0, y1;
-                            unpack2(mul2(add2(pack2(x[i], x[i + 1]), c2), s2), y0, y1);
-                            a2[i >> 1 & 1] = add2(a2[i >> 1 & 1], pack2(ex2(y0), ex2(y1)));
-                        }
-                        float w0, w1, w2, w3;
-                        unpack2(a2[0], w0, w1);
-                        unpack2(a2[1], w2, w3);
-                        sum = (w0 + w1) + (w2 + w3);
                     }
+                    float high[4] = {best, best, best, best};
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) high[i & 3] = fmaxf(high[i & 3], x[i >> 5][i & 31]);
+                    best = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3]));
+                    const uint64_t s2 = pack2(s, s), c2 = pack2(-best, -best);
+                    uint64_t a2[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int i = 0; i < 128; i += 2) {
+                        float y0, y1;
+                        unpack2(mul2(add2(pack2(x[i >> 5][i & 31], x[i >> 5][i + 1 & 31]), c2), s2), y0, y1);
+                        a2[i >> 1 & 3] = add2(a2[i >> 1 & 3], pack2(ex2(y0), ex2(y1)));
+                    }
+                    float w0, w1;
+                    unpack2(add2(add2(a2[0], a2[1]), add2(a2[2], a2[3])), w0, w1);
+                    sum = w0 + w1;
+                }
+                // the row's two pairs into one (the place is written again two tiles later at the earliest, behind the next tile's barrier)
+                float2 *pairs = reinterpret_cast<float2 *>(head_smem + (slab - smem_addr(head_smem))) + (turn++ & 1) * 128;
+                if (group) pairs[row] = make_float2(best, sum);
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (!group) {
+                    const float2 o = pairs[row];
+                    join_stats(s, best, sum, o.x, o.y);
                     if (live) P.part[static_cast<long long>(w.n / P.bn) * P.part_pitch + pos] = make_float2(best, sum);
                 }
+                __syncwarp();
             } else if constexpr (MODE == HEAD_SLOPE) {
+                // The targets of the warp's 32 rows that lie among its columns: the warp reads all of them side by side and keeps a bit for
+                // each (a thread through its own row's list: 0.19 ms a run instead of 0.08 for 32 targets per row).
+                const int first = P.c0 + w.n + c0, entries = max(0, min(32, rows - m_warp)) * P.k;
+                const long long base = static_cast<long long>(m_warp) * P.k;
+                uint32_t hit[TLI_MAX_TARGETS / 32], hits = 0;
+#pragma unroll
+                for (int b = 0; b < TLI_MAX_TARGETS / 32; ++b) {
+                    hit[b] = 0;
+                    if (b * 32 >= P.k) continue;
+#pragma unroll 8
+                    for (int i = 0; i < 32; ++i) {
+                        const int e = (b * 32 + i) * 32 + lane;
+                        const int v = e < entries ? __ldg(P.tid + base + e) - first : -1;
+                        hit[b] |= (static_cast<unsigned>(v) < 128u ? 1u : 0u) << i;
+                    }
+                    hits |= hit[b];
+                }
+                const bool some = __any_sync(0xffffffffu, hits != 0);
+                const uint32_t d = sum_wait();
 #pragma unroll 1
-                for (int c = 0; c < P.bn; c += 64) {
-                    const uint32_t to = slab_free();
+                for (int c = 0; c < 128; c += 64) {
+                    float x[2][32];
+                    tmem_load32(d + c, x[0]);
+                    tmem_load32(d + c + 32, x[1]);
+                    tmem_wait_load();
+                    slab_free();
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float x[32];
-                        tmem_load32(d + c + h * 32, x);
-                        tmem_wait_load();
-                        const int col = w.n + c + h * 32, left = P.cols - col;
-                        uint32_t bits = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
-                        if (P.mask && left > 0) bits &= __ldg(P.mask + ((P.c0 + col) >> 5));
-                        bits &= live;
+                        const uint32_t bits = columns(c0 + c + h * 32) & live;
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             float y[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
-                                y[j] = ex2((x[i + j] - top) * s) * f;
+                                y[j] = ex2((x[h][i + j] - top) * s) * f;
                                 y[j] = bits >> (i + j) & 1u ? y[j] : 0.f;
                             }
-                            st_shared16(slab_at(to, h * 4 + i / 8), pack_vector<TLI_BF16>(y));
+                            slab_put(h * 4 + i / 8, pack_vector<TLI_BF16>(y));
                         }
                     }
-                    slab_full();
-                    if (issuer) {
-                        if (store) tensor_store(&P.out, w.n + c, m, to);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    if (some) {
+                        __syncwarp();
+#pragma unroll
+                        for (int b = 0; b < TLI_MAX_TARGETS / 32; ++b)
+                            for (uint32_t left = hit[b]; left; left &= left - 1) {
+                                const int e = (b * 32 + __ffs(left) - 1) * 32 + lane, v = __ldg(P.tid + base + e) - first - c, r = e / P.k;
+                                if (static_cast<unsigned>(v) < 64u)
+                                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(mine + r * 128 + (((v >> 3) ^ (r & 7)) << 4) + (v & 7) * 2),
+                                                 "h"(__bfloat16_as_ushort(__float2bfloat16_rn(__ldg(P.tval + base + e)))) : "memory");
+                            }
+                        __syncwarp();
                     }
+                    slab_full();
+                    if (store) tensor_store(&P.out, w.n + c0 + c, m_warp, mine);
+                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
+                sum_free();
             } else if (w.split >= 0) {                             // d hidden: fp32 sums, 32 columns a slab
+                const uint32_t d = sum_wait();
 #pragma unroll 1
-                for (int c = 0; c < kHeadN && w.n + c < P.H; c += 32) {
-                    const uint32_t to = slab_free();
+                for (int h = 0; h < 128 && w.n + c0 + h < P.H; h += 32) {
                     float x[32];
-                    tmem_load32(d + c, x);
+                    tmem_load32(d + h, x);
                     tmem_wait_load();
+                    slab_free();
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) x[i + j] = w.ks ? x[i + j] : 0.f;     // (a split of a short run may have no step)
-                        st_shared16(slab_at(to, i / 4), make_uint4(__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])));
+                        slab_put(i / 4, make_uint4(__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])));
                     }
                     slab_full();
-                    if (issuer) {
-                        if (store) tensor_store3(&P.out2, w.n + c, m, w.split, to, !P.first);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    }
+                    if (store) tensor_store3(&P.out2, w.n + c0 + h, m_warp, w.split, mine, !P.first);
+                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
+                sum_free();
             } else {                                               // d weight: bf16, 64 columns a slab
+                const uint32_t d = sum_wait();
 #pragma unroll 1
-                for (int c = 0; c < kHeadN && w.n + c < P.H; c += 64) {
-                    const uint32_t to = slab_free();
+                for (int c = 0; c < 128 && w.n + c0 + c < P.H; c += 64) {
+                    float x[2][32];
+                    tmem_load32(d + c, x[0]);
+                    tmem_load32(d + c + 32, x[1]);
+                    tmem_wait_load();
+                    slab_free();
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float x[32];
-                        tmem_load32(d + c + h * 32, x);
-                        tmem_wait_load();
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             float y[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = w.ks ? x[i + j] : 0.f;
-                            st_shared16(slab_at(to, h * 4 + i / 8), pack_vector<TLI_BF16>(y));
+                            for (int j = 0; j < 8; ++j) y[j] = w.ks ? x[h][i + j] : 0.f;
+                            slab_put(h * 4 + i / 8, pack_vector<TLI_BF16>(y));
                         }
-                    }
                     slab_full();
-                    if (issuer) {
-                        if (store) tensor_store(&P.out, w.n + c, P.c0 + m, to);
-                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                    }
+                    if (store) tensor_store(&P.out, w.n + c0 + c, P.c0 + m_warp, mine);
+                    if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
-            }
-            tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (CG == 1) mbar_arrive(&sm.tempty[acc & 1]);
-                else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr(smem_addr(&sm.tempty[acc & 1]), 0u)) : "memory");
+                sum_free();
             }
         }
-        if (issuer) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tmem_fence_before();
@@ -451,7 +553,8 @@ struct HeadRows {
     uint32_t *taking;                      // a bit per row, a word per CTA of the targets kernel
     int *n_valid, *pos;                    // rows that take part; place of a row among them, -1
     float4 *by_row, *rowp;                 // {s, m, f, -} of a row; of the rows that take part, in their order
-    int *tid; float *tval;                 // gradient: the targets' ids (-1) and elements of G
+    int *tid; float *tval;                 // gradient: the targets' ids (-1) and elements of G, of all rows
+    int *tid_of; float *tval_of;           // ... of the rows that take part, in their order
     __nv_bfloat16 *rows;                   // [N, H]
     const float2 *part; long long part_pitch; int tiles;
     __nv_bfloat16 *G; long long pitch; int c0, cols;
@@ -459,79 +562,161 @@ struct HeadRows {
     __nv_bfloat16 *grad_hidden; long long grad_hidden_stride; int out_vec;
 };
 
-// A warp per row.  GRAD: also what the row's slope is made of and its targets' elements, g/tau (q - mass).
+// Row `row` by one warp: whether it takes part, and in r what a tile of it needs.  GRAD: also its targets' elements, g/tau (q - mass).
+template <bool GRAD> __device__ __forceinline__ bool head_row(const HeadRows &P, long long row, float4 &r) {
+    constexpr int Q = TLI_MAX_TARGETS / 32;
+    const int lane = threadIdx.x & 31, k = P.T.k;
+    int id[Q];
+    float t[Q];
+    bool any = false;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        id[q] = -1; t[q] = 0.f;
+        if (q * 32 + lane < k) id[q] = row_target(P.T, row, q * 32 + lane, t[q]);
+        any |= id[q] >= 0;
+    }
+    any = __any_sync(0xffffffffu, any);
+    float tau, s;
+    const bool scale_ok = row_scale(P.T.tau, row, tau, s);
+    bool takes = any && scale_ok;
+    const int status = (any ? 0 : TLI_ROW_LEFT_OUT) | (scale_ok ? 0 : TLI_ROW_BAD_TEMPERATURE);
+    r = make_float4(s, 0.f, 0.f, 0.f);
+    if constexpr (GRAD) {
+        const RowSlope slope(P.T.tau, P.stats, P.g, row);
+        takes = takes && !slope.zero;
+        r.y = slope.m; r.z = slope.f;
+        if (takes) {
+            float mass[Q], W = 1.f;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) mass[q] = 1.f;
+            if (P.T.teacher) {
+                float tm = -INFINITY, w[Q];
+#pragma unroll
+                for (int q = 0; q < Q; ++q) if (id[q] >= 0) tm = fmaxf(tm, t[q]);
+                tm = warp_max(tm);
+                W = 0.f;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    w[q] = id[q] >= 0 ? ex2((t[q] - tm) * s) : 0.f;
+                    W += w[q];
+                    mass[q] = 0.f;
+                }
+                W = warp_sum(W);
+#pragma unroll
+                for (int b = 0; b < Q; ++b) {
+                    if (b * 32 >= k) break;
+                    for (int l = 0; l < 32; ++l) {
+                        const int other = __shfl_sync(0xffffffffu, id[b], l);
+                        const float more = __shfl_sync(0xffffffffu, w[b], l);
+#pragma unroll
+                        for (int q = 0; q < Q; ++q) {
+                            if (q * 32 >= k) break;
+                            mass[q] += id[q] == other ? more : 0.f;
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const long long at = row * k + q * 32 + lane;
+                if (q * 32 + lane >= k) break;
+                P.tid[at] = id[q];
+                if (id[q] >= 0) P.tval[at] = fmaf(-slope.h, mass[q] / W, slope(__ldg(P.target_logits + at)));
+            }
+        }
+    }
+    if (lane == 0 && P.status) P.status[row] = status | (!takes && !status ? TLI_ROW_FALLBACK : 0);
+    return takes;
+}
+// The same question alone, by one thread.
+template <bool GRAD> __device__ __forceinline__ bool head_takes(const HeadRows &P, long long row) {
+    float tau, s, t;
+    if (!row_scale(P.T.tau, row, tau, s) || (GRAD && __ldg(P.stats + 2 * row + 1) == 0.f)) return false;
+    for (int j = 0; j < P.T.k; ++j)
+        if (row_target(P.T, row, j, t) >= 0) return true;
+    return false;
+}
+// A row of `hidden` (and its targets, for the gradient) to place pos, by one warp, eight vectors of a lane on their way.
+__device__ __forceinline__ void head_copy(const HeadRows &P, long long row, long long pos) {
+    const int lane = threadIdx.x & 31;
+    if (P.tid_of)
+        for (int j = lane; j < P.T.k; j += 32) {                   // (by the lanes that have written them, if this kernel has)
+            P.tid_of[pos * P.T.k + j] = __ldcg(P.tid + row * P.T.k + j);
+            P.tval_of[pos * P.T.k + j] = __ldcg(P.tval + row * P.T.k + j);
+        }
+    __nv_bfloat16 *to = P.rows + pos * P.H;
+    const __nv_bfloat16 *from = P.hidden + row * P.hidden_stride;
+    if (P.vec) {
+        const int nv = P.H / 8;
+#pragma unroll 1
+        for (int i0 = lane; i0 < nv; i0 += 256) {
+            uint4 v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) if (i0 + q * 32 < nv) v[q] = __ldg(reinterpret_cast<const uint4 *>(from) + i0 + q * 32);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) if (i0 + q * 32 < nv) reinterpret_cast<uint4 *>(to)[i0 + q * 32] = v[q];
+        }
+    } else {
+#pragma unroll 4
+        for (int i = lane; i < P.H; i += 32) to[i] = from[i];
+    }
+}
+// The number of rows that take part, and zeros behind them up to the next multiple of kHeadK (the contraction of d weight goes that far).
+__device__ __forceinline__ void head_end(const HeadRows &P, int total) {
+    if (threadIdx.x == 0) *P.n_valid = total;
+    const long long end = min(static_cast<long long>(P.T.N), (static_cast<long long>(total) + kHeadK - 1) / kHeadK * kHeadK);
+    const long long nv = (end - total) * (P.H / 8);
+    for (long long i = threadIdx.x; i < nv; i += blockDim.x) reinterpret_cast<uint4 *>(P.rows + static_cast<long long>(total) * P.H)[i] = make_uint4(0, 0, 0, 0);
+}
+
+constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
+constexpr int kHeadOneLaunch = 2048;       // lookups up to which every CTA looks at all rows before its own, instead of a launch that does
+
+// Few rows: both steps at once.
+template <bool GRAD>
+__global__ void __launch_bounds__(kGatherThreads) tli_head_prepare_kernel(const __grid_constant__ HeadRows P) {
+    __shared__ int sums[kGatherRows], taking[kGatherRows];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (not before: see the early loads of the weight)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row0 = blockIdx.x * kGatherRows, row = row0 + warp;
+    int before = 0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < row0; i += kGatherThreads) before += head_takes<GRAD>(P, i);
+    float4 r;
+    const bool takes = row < P.T.N && head_row<GRAD>(P, row, r);
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (lane == 0) { sums[warp] = before; taking[warp] = takes; }
+    __syncthreads();
+    int total = 0, pos = 0;
+#pragma unroll
+    for (int i = 0; i < kGatherRows; ++i) {
+        total += sums[i] + taking[i];
+        pos += sums[i] + (i < warp ? taking[i] : 0);
+    }
+    if (row < P.T.N) {
+        if (lane == 0) {
+            P.pos[row] = takes ? pos : -1;
+            if (takes) P.rowp[pos] = r;
+        }
+        if (takes) head_copy(P, row, pos);
+    }
+    if (blockIdx.x == gridDim.x - 1) head_end(P, total);
+}
+
 template <bool GRAD>
 __global__ void __launch_bounds__(kHeadRowBlock * 32) tli_head_targets_kernel(const __grid_constant__ HeadRows P) {
-    constexpr int Q = TLI_MAX_TARGETS / 32;
     __shared__ uint32_t word;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (not before: see the early loads of the weight)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long row = static_cast<long long>(blockIdx.x) * kHeadRowBlock + warp;
     if (threadIdx.x == 0) word = 0;
     __syncthreads();
     if (row < P.T.N) {
-        int id[Q];
-        float t[Q];
-        bool any = false;
-#pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            id[q] = -1; t[q] = 0.f;
-            if (q * 32 + lane < k) id[q] = row_target(P.T, row, q * 32 + lane, t[q]);
-            any |= id[q] >= 0;
-        }
-        any = __any_sync(0xffffffffu, any);
-        float tau, s;
-        const bool scale_ok = row_scale(P.T.tau, row, tau, s);
-        bool takes = any && scale_ok;
-        int status = (any ? 0 : TLI_ROW_LEFT_OUT) | (scale_ok ? 0 : TLI_ROW_BAD_TEMPERATURE);
-        float4 r = make_float4(s, 0.f, 0.f, 0.f);
-        if constexpr (GRAD) {
-            const RowSlope slope(P.T.tau, P.stats, P.g, row);
-            takes = takes && !slope.zero;
-            r = make_float4(slope.s, slope.m, slope.f, 0.f);
-            if (takes) {
-                float mass[Q], W = 1.f;
-                if (P.T.teacher) {
-                    float tm = -INFINITY, w[Q];
-#pragma unroll
-                    for (int q = 0; q < Q; ++q) if (id[q] >= 0) tm = fmaxf(tm, t[q]);
-                    tm = warp_max(tm);
-                    W = 0.f;
-#pragma unroll
-                    for (int q = 0; q < Q; ++q) {
-                        w[q] = id[q] >= 0 ? ex2((t[q] - tm) * s) : 0.f;
-                        W += w[q];
-                        mass[q] = 0.f;
-                    }
-                    W = warp_sum(W);
-#pragma unroll
-                    for (int b = 0; b < Q; ++b) {
-                        if (b * 32 >= k) break;
-                        for (int l = 0; l < 32; ++l) {
-                            const int other = __shfl_sync(0xffffffffu, id[b], l);
-                            const float more = __shfl_sync(0xffffffffu, w[b], l);
-#pragma unroll
-                            for (int q = 0; q < Q; ++q) mass[q] += id[q] == other ? more : 0.f;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int q = 0; q < Q; ++q) mass[q] = 1.f;
-                }
-#pragma unroll
-                for (int q = 0; q < Q; ++q) {
-                    const long long at = row * k + q * 32 + lane;
-                    if (q * 32 + lane >= k) break;
-                    P.tid[at] = id[q];
-                    if (id[q] >= 0) P.tval[at] = fmaf(-slope.h, mass[q] / W, slope(__ldg(P.target_logits + at)));
-                }
-            }
-        }
+        float4 r;
+        const bool takes = head_row<GRAD>(P, row, r);
         if (lane == 0) {
             P.by_row[row] = r;
-            if (GRAD && P.status) P.status[row] = status | (!takes && !status ? TLI_ROW_FALLBACK : 0);
-            if (!GRAD && P.status) P.status[row] = status;
             if (takes) atomicOr(&word, 1u << warp);
         }
     }
@@ -539,49 +724,33 @@ __global__ void __launch_bounds__(kHeadRowBlock * 32) tli_head_targets_kernel(co
     if (threadIdx.x == 0) P.taking[blockIdx.x] = word;
 }
 
-// The rows that take part, in order.  The last CTA leaves their number, and zeros up to the next multiple of kHeadK (the contraction of
-// d weight goes that far).
-constexpr int kGatherThreads = 256;
+// The rows that take part, in order, a warp each.
 __global__ void __launch_bounds__(kGatherThreads) tli_head_gather_kernel(const __grid_constant__ HeadRows P) {
-    constexpr int WARPS = kGatherThreads / 32;
-    __shared__ int sums[WARPS];
+    __shared__ int sums[kGatherRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int row = blockIdx.x * kGatherRows + warp, at = blockIdx.x * kGatherRows / kHeadRowBlock;
     int before = 0;
-    for (int i = threadIdx.x; i < b; i += kGatherThreads) before += __popc(__ldcg(P.taking + i));
+    for (int i = threadIdx.x; i < at; i += kGatherThreads) before += __popc(__ldcg(P.taking + i));
     before = __reduce_add_sync(0xffffffffu, before);
     if (lane == 0) sums[warp] = before;
     __syncthreads();
     before = 0;
 #pragma unroll
-    for (int i = 0; i < WARPS; ++i) before += sums[i];
-    const uint32_t word = __ldcg(P.taking + b);
-    for (int r = warp; r < kHeadRowBlock; r += WARPS) {
-        const long long row = static_cast<long long>(b) * kHeadRowBlock + r;
-        if (row >= P.T.N) break;
-        const bool takes = word >> r & 1u;
-        const long long pos = before + __popc(word & ((1u << r) - 1u));
+    for (int i = 0; i < kGatherRows; ++i) before += sums[i];
+    const uint32_t word = __ldcg(P.taking + at);
+    if (row < P.T.N) {
+        const int bit = row % kHeadRowBlock;
+        const bool takes = word >> bit & 1u;
+        const int pos = before + __popc(word & ((1u << bit) - 1u));
         if (lane == 0) {
-            P.pos[row] = takes ? static_cast<int>(pos) : -1;
+            P.pos[row] = takes ? pos : -1;
             if (takes) P.rowp[pos] = __ldcg(P.by_row + row);
         }
-        if (!takes) continue;
-        __nv_bfloat16 *to = P.rows + pos * P.H;
-        const __nv_bfloat16 *from = P.hidden + row * P.hidden_stride;
-        if (P.vec) {
-            for (int i = lane; i < P.H / 8; i += 32) reinterpret_cast<uint4 *>(to)[i] = __ldg(reinterpret_cast<const uint4 *>(from) + i);
-        } else {
-            for (int i = lane; i < P.H; i += 32) to[i] = from[i];
-        }
+        if (takes) head_copy(P, row, pos);
     }
-    if (b == static_cast<int>(gridDim.x) - 1) {
-        const int total = before + __popc(word);
-        if (threadIdx.x == 0) *P.n_valid = total;
-        const long long end = min(static_cast<long long>(P.T.N), (static_cast<long long>(total) + kHeadK - 1) / kHeadK * kHeadK);
-        const long long nv = (end - total) * (P.H / 8);
-        for (long long i = threadIdx.x; i < nv; i += kGatherThreads) reinterpret_cast<uint4 *>(P.rows + static_cast<long long>(total) * P.H)[i] = make_uint4(0, 0, 0, 0);
-    }
+    if (blockIdx.x == gridDim.x - 1) head_end(P, before + __popc(word));
 }
 
 // ---- forward: the loss of eight rows per CTA ----
@@ -599,69 +768,84 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
     constexpr int Q = TLI_MAX_TARGETS / 32;
     __shared__ float sh_m[32][kHeadLossRows], sh_s[32][kHeadLossRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
-    const long long row0 = static_cast<long long>(blockIdx.x) * kHeadLossRows;
+    const long long row0 = static_cast<long long>(blockIdx.x) * kHeadLossRows, row = row0 + warp, at = row * k;
+    // The targets' logits are made of the call's inputs: a CTA that finds room beside the products begins with them.
+    int id[Q];
+    float t[Q], z[Q], tau = 1.f, s = 1.f;
+    bool takes = false;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) { id[q] = -1; t[q] = 0.f; z[q] = 0.f; }
+    if (row < P.T.N) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (q * 32 + lane < k) id[q] = row_target(P.T, row, q * 32 + lane, t[q]);
+            takes |= id[q] >= 0;
+        }
+        takes = __any_sync(0xffffffffu, takes);
+        takes = row_scale(P.T.tau, row, tau, s) && takes;
+    }
+    if (takes) {
+        const __nv_bfloat16 *h = P.hidden + row * P.hidden_stride;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (q * 32 >= k) break;
+            for (int l = 0; l < 32 && q * 32 + l < k; ++l) {
+                const int v = __shfl_sync(0xffffffffu, id[q], l);
+                if (v < 0) continue;
+                float dot = 0.f;
+                const __nv_bfloat16 *w = P.weight + v * P.weight_stride;
+                if (P.vec) {
+#pragma unroll 4
+                    for (int i = lane; i < P.H / 8; i += 32) dot = dot_bf16(__ldg(reinterpret_cast<const uint4 *>(h) + i), __ldg(reinterpret_cast<const uint4 *>(w) + i), dot);
+                } else {
+#pragma unroll 4
+                    for (int i = lane; i < P.H; i += 32) dot = fmaf(__bfloat162float(h[i]), __bfloat162float(w[i]), dot);
+                }
+                dot = warp_sum(dot);
+                if (l == lane) z[q] = dot;
+            }
+        }
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (row < P.T.N) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (q * 32 + lane < k) P.target_logits[at + q * 32 + lane] = z[q];
+    }
     {
         const int r = threadIdx.x & 7, t0 = threadIdx.x >> 3;      // neighbouring threads: neighbouring rows of a tile
-        const long long row = row0 + r;
-        const int pos = row < P.T.N ? __ldcg(P.pos + row) : -1;
+        const int pos = row0 + r < P.T.N ? __ldcg(P.pos + row0 + r) : -1;
         float m = kMaskBelow, sum = 0.f;
         if (pos >= 0) {
-            const float s = __ldcg(&P.rowp[pos].x);
-            for (int t = t0; t < P.tiles; t += 32) {
-                const float2 p = __ldcg(P.part + t * P.part_pitch + pos);
-                join_stats(s, m, sum, p.x, p.y);
+            const float sc = __ldcg(&P.rowp[pos].x);
+            const float2 *part = P.part + pos;
+#pragma unroll 1
+            for (int i = t0; i < P.tiles; i += 32 * 4) {
+                float2 p[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) p[q] = i + q * 32 < P.tiles ? __ldcg(part + (i + q * 32) * P.part_pitch) : make_float2(kMaskBelow, 0.f);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) join_stats(sc, m, sum, p[q].x, p[q].y);
             }
         }
         sh_m[t0][r] = m; sh_s[t0][r] = sum;
     }
     __syncthreads();
-    const long long row = row0 + warp;
     if (row >= P.T.N) return;
-    const int pos = __ldcg(P.pos + row);
-    const long long at = row * k;
-    if (pos < 0) {
-        for (int j = lane; j < k; j += 32) P.target_logits[at + j] = 0.f;
+    const int timeout = *reinterpret_cast<const volatile unsigned *>(P.error) ? TLI_ROW_TIMEOUT : 0;
+    if (!takes) {
         if (lane == 0) {
             P.loss[row] = 0.f;
             reinterpret_cast<float2 *>(P.stats)[row] = make_float2(0.f, 0.f);
-            if (P.status && *reinterpret_cast<const volatile unsigned *>(P.error)) P.status[row] |= TLI_ROW_TIMEOUT;
+            if (P.status && timeout) P.status[row] |= timeout;
         }
         return;
     }
-    float tau, s;
-    row_scale(P.T.tau, row, tau, s);
     float m = sh_m[lane][warp], sum = sh_s[lane][warp];
     const float top = warp_max(m);
     sum = warp_sum(sum * ex2((m - top) * s));
     m = top;
-    // the targets' logits, a target at a time
-    const uint4 *h = reinterpret_cast<const uint4 *>(P.rows + static_cast<long long>(pos) * P.H);
-    int id[Q];
-    float t[Q], z[Q];
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        id[q] = -1; t[q] = 0.f; z[q] = 0.f;
-        if (q * 32 + lane < k) id[q] = row_target(P.T, row, q * 32 + lane, t[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < Q; ++q) {
-        if (q * 32 >= k) break;
-        for (int l = 0; l < 32 && q * 32 + l < k; ++l) {
-            const int v = __shfl_sync(0xffffffffu, id[q], l);
-            float dot = 0.f;
-            if (v >= 0) {
-                const uint4 *w = reinterpret_cast<const uint4 *>(P.weight + v * P.weight_stride);
-                for (int i = lane; i < P.H / 8; i += 32) dot = dot_bf16(__ldg(h + i), __ldg(w + i), dot);
-                dot = warp_sum(dot);
-            }
-            if (l == lane) z[q] = dot;
-        }
-    }
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-        if (q * 32 + lane < k) P.target_logits[at + q * 32 + lane] = z[q];
     float W = 1.f, ent;
     if (P.T.teacher) {
         float tm = -INFINITY;
@@ -684,52 +868,44 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
         const bool none = sum == 0.f, bad = sum != sum || W != W;
         P.loss[row] = none ? 0.f : bad ? NAN : logf(sum) + (P.T.teacher ? ent / W - logf(W) : ent);
         reinterpret_cast<float2 *>(P.stats)[row] = none ? make_float2(0.f, 0.f) : make_float2(m, bad ? NAN : sum);
-        if (P.status) {
-            const int timeout = *reinterpret_cast<const volatile unsigned *>(P.error) ? TLI_ROW_TIMEOUT : 0;
-            P.status[row] = timeout | (none ? TLI_ROW_FALLBACK : bad ? TLI_ROW_NONFINITE : 0);
-        }
+        if (P.status) P.status[row] = timeout | (none ? TLI_ROW_FALLBACK : bad ? TLI_ROW_NONFINITE : 0);
     }
 }
 
-// ---- backward: the targets' elements of a run of G, and d hidden at its rows' places ----
-
-__global__ void __launch_bounds__(256) tli_head_patch_kernel(const __grid_constant__ HeadRows P) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= static_cast<long long>(P.T.N) * P.T.k) return;
-    const int pos = __ldcg(P.pos + i / P.T.k);
-    if (pos < 0) return;
-    const int v = __ldcg(P.tid + i) - P.c0;
-    if (v < 0 || v >= P.cols) return;
-    P.G[pos * P.pitch + v] = __float2bfloat16_rn(__ldcg(P.tval + i));
-}
+// ---- backward: d hidden at its rows' places ----
 
 __global__ void __launch_bounds__(256) tli_head_rows_kernel(const __grid_constant__ HeadRows P) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int units = P.H / 8;
+    const int units = P.H / 4;
     const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
     if (i >= static_cast<long long>(P.T.N) * units) return;
     const long long row = i / units;
     const int u = static_cast<int>(i % units), pos = __ldcg(P.pos + row);
     if (u == 0 && P.status && *reinterpret_cast<const volatile unsigned *>(P.error)) P.status[row] |= TLI_ROW_TIMEOUT;
     if (!P.grad_hidden) return;
-    float x[8] = {};
+    float x[4] = {};
     if (pos >= 0) {
-        for (int sp = 0; sp < P.splits; ++sp) {
-            const float4 *p = reinterpret_cast<const float4 *>(P.sums + (static_cast<long long>(sp) * P.T.N + pos) * P.H + u * 8);
-            const float4 a = __ldcg(p), b = __ldcg(p + 1);
-            x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
-            x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        const float *p = P.sums + static_cast<long long>(pos) * P.H + u * 4;
+        const long long next = static_cast<long long>(P.T.N) * P.H;
+#pragma unroll 1
+        for (int sp = 0; sp < P.splits; sp += 8) {
+            float4 a[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) a[q] = sp + q < P.splits ? __ldcg(reinterpret_cast<const float4 *>(p + (sp + q) * next)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) { x[0] += a[q].x; x[1] += a[q].y; x[2] += a[q].z; x[3] += a[q].w; }
         }
     }
-    __nv_bfloat16 *to = P.grad_hidden + row * P.grad_hidden_stride + u * 8;
+    __nv_bfloat16 *to = P.grad_hidden + row * P.grad_hidden_stride + u * 4;
     if (P.out_vec) {
-        *reinterpret_cast<uint4 *>(to) = pack_vector<TLI_BF16>(x);
+        uint32_t w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(x[2 * j + 1]), "f"(x[2 * j]));
+        *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) to[j] = __float2bfloat16_rn(x[j]);
+        for (int j = 0; j < 4; ++j) to[j] = __float2bfloat16_rn(x[j]);
     }
 }
 
@@ -765,7 +941,7 @@ constexpr int kHeadMinSteps = 8;                       // of the contraction in 
 struct HeadPlan {
     int cg, bn, tiles;                     // CTAs per tile; columns of a forward tile, tiles of the vocabulary
     int run, runs, splits;                 // backward: columns of a run of G, runs, cuts of d hidden's contraction
-    size_t taking, n_valid, pos, by_row, rowp, tid, tval, rows, part, G, sums, total;
+    size_t taking, n_valid, pos, by_row, rowp, tid, tval, tid_of, tval_of, rows, part, G, sums, total;
 };
 
 HeadPlan head_plan(int N, int H, int k, int V, int num_sms, bool grad) {
@@ -800,9 +976,11 @@ HeadPlan head_plan(int N, int H, int k, int V, int num_sms, bool grad) {
         L.run = static_cast<int>(align_up((V + L.runs - 1) / L.runs, kHeadN));
         L.runs = (V + L.run - 1) / L.run;
         const int blocks = (N + 128 * L.cg - 1) / (128 * L.cg) * ((H + kHeadN - 1) / kHeadN), steps = (std::min(V, L.run) + kHeadK - 1) / kHeadK;
-        L.splits = std::max(1, std::min((num_sms / L.cg + blocks - 1) / std::max(blocks, 1), steps / kHeadMinSteps));
+        L.splits = std::max(1, std::min(num_sms / L.cg / std::max(blocks, 1), steps / kHeadMinSteps));
         L.tid = take(4 * n * k);
         L.tval = take(4 * n * k);
+        L.tid_of = take(4 * n * k);
+        L.tval_of = take(4 * n * k);
         L.G = take(2 * n * L.run);
         L.sums = take(4 * n * H * L.splits);
     }
@@ -838,6 +1016,14 @@ template <typename K> int launch_plain(K kernel, const HeadRows &P, long long bl
     cfg.gridDim = dim3(static_cast<unsigned>(blocks)); cfg.blockDim = dim3(threads);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P);
     return e == cudaSuccess ? TLI_OK : cuda_fail(e, what);
+}
+
+// Which rows take part, and those one after the other.
+template <bool GRAD> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
+    const long long N = R.T.N, gathers = (N + kGatherRows - 1) / kGatherRows;
+    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD>, R, gathers, kGatherThreads, stream, "launch tli_head_prepare_kernel");
+    const int rc = launch_plain(tli_head_targets_kernel<GRAD>, R, (N + kHeadRowBlock - 1) / kHeadRowBlock, kHeadRowBlock * 32, stream, "launch tli_head_targets_kernel");
+    return rc == TLI_OK ? launch_plain(tli_head_gather_kernel, R, gathers, kGatherThreads, stream, "launch tli_head_gather_kernel") : rc;
 }
 
 size_t head_workspace(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side, bool grad) {
@@ -902,14 +1088,13 @@ int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *a, void *cuda_stream) 
     R.part = reinterpret_cast<const float2 *>(reinterpret_cast<char *>(a->workspace) + L.part); R.part_pitch = a->N; R.tiles = L.tiles;
     HeadGemm G;
     head_gemm_common(R, ctx, G);
-    G.cols = R.V; G.bn = L.bn;
+    G.cols = R.V; G.bn = L.bn; G.early = a->N <= 128 * L.cg;
+    G.k_part = L.cg == 1 ? 4 : std::min(16, std::max(8, (R.H + 2 * kHeadK - 1) / (2 * kHeadK)));
     G.a_rows = std::min(128, (a->N + 7) / 8 * 8);
     G.part = const_cast<float2 *>(R.part); G.part_pitch = R.part_pitch;
     if (!tensor_map(&G.a, false, R.rows, R.H, a->N, R.H, G.a_rows) || !tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, L.bn / L.cg)) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
-    const long long blocks = (a->N + kHeadRowBlock - 1) / kHeadRowBlock;
-    rc = launch_plain(tli_head_targets_kernel<false>, R, blocks, kHeadRowBlock * 32, stream, "launch tli_head_targets_kernel");
-    if (rc == TLI_OK) rc = launch_plain(tli_head_gather_kernel, R, blocks, kGatherThreads, stream, "launch tli_head_gather_kernel");
+    rc = launch_head_rows<false>(R, stream);
     if (rc == TLI_OK) rc = launch_head_gemm<HEAD_STATS>(G, L.cg, ctx, static_cast<long long>(L.tiles) * ((a->N + 128 * L.cg - 1) / (128 * L.cg)), stream);
     if (rc == TLI_OK) rc = launch_plain(tli_head_loss_kernel, R, (a->N + kHeadLossRows - 1) / kHeadLossRows, 256, stream, "launch tli_head_loss_kernel");
     return rc;
@@ -930,6 +1115,7 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     char *ws = reinterpret_cast<char *>(a->workspace);
     R.stats = const_cast<float *>(a->stats); R.target_logits = const_cast<float *>(a->target_logits); R.g = a->grad_loss; R.status = a->status;
     R.tid = reinterpret_cast<int *>(ws + L.tid); R.tval = reinterpret_cast<float *>(ws + L.tval);
+    R.tid_of = reinterpret_cast<int *>(ws + L.tid_of); R.tval_of = reinterpret_cast<float *>(ws + L.tval_of);
     R.G = reinterpret_cast<__nv_bfloat16 *>(ws + L.G); R.pitch = L.run;
     R.sums = reinterpret_cast<const float *>(ws + L.sums); R.splits = L.splits;
     R.grad_hidden = reinterpret_cast<__nv_bfloat16 *>(a->grad_hidden); R.grad_hidden_stride = a->grad_hidden_stride;
@@ -943,31 +1129,29 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     }
     HeadGemm S, G;
     head_gemm_common(R, ctx, S);
-    S.bn = kHeadN;
+    head_gemm_common(R, ctx, G);
+    S.tid = R.tid_of; S.tval = R.tval_of; S.k = a->k;
+    S.bn = kHeadN; S.early = G.early = N <= 128 * L.cg;
     S.a_rows = std::min(128, (N + 7) / 8 * 8);
     bool maps = tensor_map(&S.a, false, R.rows, R.H, N, R.H, S.a_rows) && tensor_map(&S.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadN / L.cg) &&
-                tensor_map(&S.out, false, R.G, L.run, N, L.run, 128);
-    head_gemm_common(R, ctx, G);
+                tensor_map(&S.out, false, R.G, L.run, N, L.run, 32) && tensor_map(&G.a, false, R.G, L.run, N, L.run, 128);
     G.splits = L.splits; G.want_dh = a->grad_hidden != nullptr; G.want_dw = a->grad_weight != nullptr;
-    G.a = S.out;
     maps = maps && tensor_map(&G.a2, false, R.G, L.run, N, L.run, kHeadK) && tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadK) &&
-           tensor_map(&G.b2, false, R.rows, R.H, N, R.H, kHeadK) && tensor_map(&G.out2, true, R.sums, R.H, N, R.H, 128, L.splits);
-    if (maps && a->grad_weight) maps = tensor_map(&G.out, false, a->grad_weight, R.H, R.V, a->grad_weight_stride, 128);
+           tensor_map(&G.b2, false, R.rows, R.H, N, R.H, kHeadK) && tensor_map(&G.out2, true, R.sums, R.H, N, R.H, 32, L.splits);
+    if (maps && a->grad_weight) maps = tensor_map(&G.out, false, a->grad_weight, R.H, R.V, a->grad_weight_stride, 32);
     if (!maps) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
-    const long long blocks = (N + kHeadRowBlock - 1) / kHeadRowBlock, mb = (N + 128 * L.cg - 1) / (128 * L.cg), hb = (R.H + kHeadN - 1) / kHeadN;
-    rc = launch_plain(tli_head_targets_kernel<true>, R, blocks, kHeadRowBlock * 32, stream, "launch tli_head_targets_kernel");
-    if (rc == TLI_OK) rc = launch_plain(tli_head_gather_kernel, R, blocks, kGatherThreads, stream, "launch tli_head_gather_kernel");
+    const long long mb = (N + 128 * L.cg - 1) / (128 * L.cg), hb = (R.H + kHeadN - 1) / kHeadN;
+    rc = launch_head_rows<true>(R, stream);
     for (int i = 0; i < L.runs && rc == TLI_OK; ++i) {
         const int c0 = i * L.run, cols = std::min(L.run, R.V - c0);
         S.c0 = G.c0 = R.c0 = c0;
         S.cols = G.cols = R.cols = cols;
         G.first = i == 0;
         rc = launch_head_gemm<HEAD_SLOPE>(S, L.cg, ctx, mb * ((cols + kHeadN - 1) / kHeadN), stream);
-        if (rc == TLI_OK) rc = launch_plain(tli_head_patch_kernel, R, (static_cast<long long>(N) * a->k + 255) / 256, 256, stream, "launch tli_head_patch_kernel");
         if (rc == TLI_OK) rc = launch_head_gemm<HEAD_GRADS>(G, L.cg, ctx, mb * hb * L.splits + (cols + 128 * L.cg - 1) / (128 * L.cg) * hb, stream);
     }
     if (rc == TLI_OK && (a->grad_hidden || a->status))
-        rc = launch_plain(tli_head_rows_kernel, R, (static_cast<long long>(N) * (R.H / 8) + 255) / 256, 256, stream, "launch tli_head_rows_kernel");
+        rc = launch_plain(tli_head_rows_kernel, R, (static_cast<long long>(N) * (R.H / 4) + 255) / 256, 256, stream, "launch tli_head_rows_kernel");
     return rc;
 }
 
