@@ -15,8 +15,13 @@
 namespace {
 
 constexpr int kLossThreads = 256;
-constexpr int kLossBatch = 8;              // 16-byte vectors a thread has on their way
+// 16-byte vectors a thread has on their way.  bf16 rows are half compute: they want warps (six CTAs per SM) more than loads in flight.  1500 of
+// 50 257 over the intersection: 54 us with eight and three CTAs, 46 with four and four, 42 with four and six; 8192 of 128 256: 361 with four and
+// six, 377 with two and six.  fp32 rows the other way: 4096 of 256 000 in 613 us with eight, 648 with four.  (The next batch asked for before
+// this one is worked on costs registers, hence warps: 48 us.)
+template <int DT> constexpr int kLossBatch = DT == TLI_F32 ? 8 : 4;
 constexpr int kLossMaxCluster = 8;
+constexpr long long kLossFill = 8;         // CTAs per SM that rows are cut for
 constexpr float kMaskBelow = -1e30f;       // a logit below it is a mask
 constexpr float kLog2e = 1.4426950408889634f;
 static_assert(TLI_MAX_TARGETS <= kLossThreads, "a thread per target");
@@ -143,8 +148,8 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kLossThreads) tli_loss_kernel(const __grid_constant__ LossParams P) {
-    constexpr int WARPS = kLossThreads / 32;
+__global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_kernel(const __grid_constant__ LossParams P) {
+    constexpr int WARPS = kLossThreads / 32, kBatch = kLossBatch<DT>;
     __shared__ float sh[WARPS], sh_m[WARPS], sh_s[WARPS];
     __shared__ float part[kLossMaxCluster][2];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -154,11 +159,19 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_kernel(const __grid_con
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const RowView<DT> rv(P.z, row * P.stride, P.V);
     const int nvec = rv.nvec(), per = (nvec + C - 1) / C, v0 = rank * per, v1 = min(nvec, v0 + per);
-    int v[kLossBatch];
-    uint4 raw[kLossBatch];
     float tau, s, teacher = 0.f, z_t = 0.f;
+    uint4 raw[kBatch];
+    auto load = [&](int at) {
+        int v[kBatch];
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) v[q] = at + q * kLossThreads;
+        row_vectors<DT, kBatch>(rv.vec0, rv.row, rv.head, P.V, v1, P.T.mask, v, raw);
+    };
+    load(v0 + tid);                                                // (on their way while the targets are looked up)
     const bool scale_ok = row_scale(P.T.tau, row, tau, s);
     const int target = tid < P.T.k ? row_target(P.T, row, tid, teacher) : -1;
+    float m = kMaskBelow, sum = 0.f;
+    if (v0 + tid < v1) loss_batch<DT, kBatch>(raw, s, m, sum);
     const int any = __syncthreads_or(target >= 0);                 // the same in every CTA of the cluster, as is scale_ok
     if (!any || !scale_ok) {
         if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
@@ -170,13 +183,10 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_kernel(const __grid_con
         return;
     }
     if (rank == 0 && target >= 0) z_t = load_elt<DT>(rv.row, target);
-    float m = kMaskBelow, sum = 0.f;
 #pragma unroll 1
-    for (int at = v0 + tid; at < v1; at += kLossThreads * kLossBatch) {
-#pragma unroll
-        for (int q = 0; q < kLossBatch; ++q) v[q] = at + q * kLossThreads;
-        row_vectors<DT, kLossBatch>(rv.vec0, rv.row, rv.head, P.V, v1, P.T.mask, v, raw);
-        loss_batch<DT, kLossBatch>(raw, s, m, sum);
+    for (int at = v0 + tid + kLossThreads * kBatch; at < v1; at += kLossThreads * kBatch) {
+        load(at);
+        loss_batch<DT, kBatch>(raw, s, m, sum);
     }
     const float wm = warp_max(m);
     sum = warp_sum(sum * ex2((m - wm) * s));
@@ -198,7 +208,13 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_kernel(const __grid_con
     }
     // the targets: ln p_j = (t_j - max t)/tau - ln W
     float ent, W = 1.f;
-    if (P.T.teacher) {
+    if (P.T.teacher && P.T.k <= 32) {                              // one warp has all of them
+        if (tid >= 32) return;
+        const float tm = warp_max(target >= 0 ? teacher : -INFINITY);
+        const float w = target >= 0 ? ex2((teacher - tm) * s) : 0.f;
+        W = warp_sum(w);
+        ent = warp_sum(w != 0.f ? w * (((m - z_t) + (teacher - tm)) / tau) : 0.f);
+    } else if (P.T.teacher) {
         const float tm = block_max<WARPS>(target >= 0 ? teacher : -INFINITY, sh);
         const float w = target >= 0 ? ex2((teacher - tm) * s) : 0.f;
         W = block_sum<WARPS>(w, sh);
@@ -257,7 +273,7 @@ template <int THREADS> __device__ __forceinline__ float target_mass(const Target
 
 template <int DT>
 __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __grid_constant__ LossParams P) {
-    constexpr int EPV = Elt<DT>::kPerVec;
+    constexpr int EPV = Elt<DT>::kPerVec, kBatch = kLossBatch<DT>;
     __shared__ float sh[kLossThreads / 32], sh_w[TLI_MAX_TARGETS];
     __shared__ int sh_id[TLI_MAX_TARGETS];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -269,6 +285,16 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
     const RowSlope slope(P.T.tau, P.stats, P.g, row);
     char *out = reinterpret_cast<char *>(P.grad) + row * P.grad_stride * Elt<DT>::kBytes;
     const int e_lo = max(0, v0 * EPV - rv.head), e_hi = min(P.V, v1 * EPV - rv.head);
+    uint4 raw[kBatch];
+    auto load = [&](int at) {
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+            const int v = at + q * kLossThreads, e0 = v * EPV - rv.head;
+            raw[q] = make_uint4(Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord);
+            if (v < v1) raw[q] = e0 >= 0 && e0 + EPV <= P.V ? __ldcg(rv.vec0 + v) : ragged_vector<DT>(rv.row, e0, P.V);
+        }
+    };
+    load(v0 + tid);                                                // (on their way while the targets are looked up)
     // the targets of this run, their logits before anything is overwritten (the gradient may lie on the logits)
     int target = -1;
     float teacher = 0.f, z_t = 0.f;
@@ -279,16 +305,9 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
     float mass = 1.f;
     if (any && P.T.teacher) mass = target_mass<kLossThreads>(P.T, target, teacher, slope.s, sh, sh_id, sh_w);
 #pragma unroll 1
-    for (int at = v0 + tid; at < v1; at += kLossThreads * kLossBatch) {
-        uint4 raw[kLossBatch];
+    for (int at = v0 + tid; at < v1; ) {
 #pragma unroll
-        for (int q = 0; q < kLossBatch; ++q) {
-            const int v = at + q * kLossThreads, e0 = v * EPV - rv.head;
-            raw[q] = make_uint4(Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord);
-            if (v < v1 && !slope.zero) raw[q] = e0 >= 0 && e0 + EPV <= P.V ? __ldcg(rv.vec0 + v) : ragged_vector<DT>(rv.row, e0, P.V);
-        }
-#pragma unroll
-        for (int q = 0; q < kLossBatch; ++q) {
+        for (int q = 0; q < kBatch; ++q) {
             const int v = at + q * kLossThreads, e0 = v * EPV - rv.head;
             if (v >= v1) break;
             if (P.T.mask) raw[q] = mask_vector<DT>(raw[q], P.T.mask, e0);
@@ -304,6 +323,8 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
                     if (e0 + i >= 0 && e0 + i < P.V) set_element<DT>(out, e0 + i, x[i]);
             }
         }
+        at += kLossThreads * kBatch;
+        if (at < v1 && !slope.zero) load(at);
     }
     if (any) {
         __syncthreads();
@@ -362,7 +383,7 @@ int tli_loss(tli_ctx *ctx, const tli_loss_args *a, void *cuda_stream) {
     // CTAs per row: as many as keep every SM busy, none with less than a batch per thread
     const long long nvec = (V + (a->dtype == TLI_F32 ? 3 : 7)) / (a->dtype == TLI_F32 ? 4 : 8) + 1;
     P.cluster = 1;
-    while (P.cluster < kLossMaxCluster && static_cast<long long>(P.cluster) * a->N < 4LL * ctx->num_sms && nvec > 2LL * P.cluster * kLossThreads) P.cluster *= 2;
+    while (P.cluster < kLossMaxCluster && static_cast<long long>(P.cluster) * a->N < kLossFill * ctx->num_sms && nvec > 2LL * P.cluster * kLossThreads) P.cluster *= 2;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
     pdl_config(cfg, attr, reinterpret_cast<cudaStream_t>(cuda_stream));
@@ -395,8 +416,9 @@ int tli_loss_grad(tli_ctx *ctx, const tli_loss_grad_args *a, void *cuda_stream) 
     P.same_grid = reinterpret_cast<uintptr_t>(a->grad) % 16 == reinterpret_cast<uintptr_t>(a->logits) % 16 &&
                   (a->N == 1 || (a->grad_stride - a->stride) * elt % 16 == 0);
     const long long nvec = (V + 16 / elt - 1) / (16 / elt) + 1;    // one more where a row begins inside a vector
-    P.seg = kLossThreads * kLossBatch;
-    while (P.seg > kLossThreads && (nvec + P.seg - 1) / P.seg * a->N < 4LL * ctx->num_sms) P.seg /= 2;
+    P.seg = static_cast<int>(nvec);
+    while (P.seg > kLossThreads && (nvec + P.seg - 1) / P.seg * a->N < kLossFill * ctx->num_sms) P.seg = (P.seg + 1) / 2;
+    P.seg = (P.seg + kLossThreads - 1) / kLossThreads * kLossThreads;
     P.nseg = static_cast<int>((nvec + P.seg - 1) / P.seg);
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];

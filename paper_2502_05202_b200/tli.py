@@ -1024,112 +1024,127 @@ class Verifier:
     # The losses.  `ids` [N] are labels; `ids` [N, k] with `teacher` [N, k] a teacher's logits of k ids.  `stats` and `target_logits` are
     # the forward call's.  Like the other calls they record no autograd graph.
 
-    def _targets(self, N: int, ids, teacher, temperature, side: int, ids_side: int, shared: bool):
-        """((k, teacher's dtype, teacher's pointer), support) of a loss call; raises on what the library could not see."""
-        on = self._index
-        self._ids(ids)
+    def _loss_plan(self, N: int, ids, teacher, side: int, ids_side: int, shared: bool):
+        """What a loss call needs of its targets, from shapes and types alone: the part of its argument struct behind its sizes."""
         if teacher is None:
-            k, t_dtype, t_ptr = 1, 0, 0
+            k, t_dtype = 1, 0
             if ids.shape != (N,) and ids.shape != (N, 1):
                 raise ValueError("labels must be [%d]" % N)
         else:
-            if ids.dim() != 2 or ids.shape[0] != N or teacher.shape != ids.shape or teacher.get_device() != on or not teacher.is_contiguous():
-                raise ValueError("ids and teacher must be contiguous [%d, k] tensors on %s" % (N, self.device))
-            k, t_dtype, t_ptr = ids.shape[1], _logit_dtype(teacher), teacher.data_ptr()
-        if temperature is not None:
-            self._per_row("temperature", temperature, (N,))
+            if ids.dim() != 2 or ids.shape[0] != N or teacher.shape != ids.shape:
+                raise ValueError("ids and teacher must be [%d, k]" % N)
+            k, t_dtype = ids.shape[1], _logit_dtype(teacher)
         self._table_rows(side), self._table_rows(ids_side)
-        return k, t_dtype, t_ptr, TLI_SUPPORT_SHARED if shared else TLI_SUPPORT_ALL
+        return k, (side, ids_side, TLI_SUPPORT_SHARED if shared else TLI_SUPPORT_ALL, t_dtype)
 
     def _per_row(self, name: str, t, shape) -> None:
         if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError("%s must be a contiguous float32 tensor of shape %s on %s" % (name, tuple(shape), self.device))
 
-    def _loss_rows(self, logits, side: int) -> int:
-        if logits.dim() != 2 or logits.shape[1] != self._table_rows(side) or logits.get_device() != self._index:
+    def _loss_args(self, kind: str, x, ids, teacher, temperature, side: int, ids_side: int, shared: bool, more=()):
+        """The plan of a loss call with rows ``x`` (worked out once per shape), the teacher's and the temperature's pointers."""
+        on = self._index
+        if x.get_device() != on:
+            raise ValueError("%s must be on %s" % ("hidden" if more else "logits", self.device))
+        self._ids(ids)
+        key = (kind, x.shape, x.stride(), x.dtype, ids.shape, None if teacher is None else (teacher.shape, teacher.dtype), side, ids_side, shared, *more)
+        plan = self._plans.get(key)
+        if plan is None:
+            plan = self._plan(key, getattr(self, kind)(x, ids, teacher, side, ids_side, shared, *more))
+        t_ptr = tau_ptr = 0
+        if teacher is not None:
+            if teacher.get_device() != on or not teacher.is_contiguous():
+                raise ValueError("teacher must be contiguous, on %s" % self.device)
+            t_ptr = teacher.data_ptr()
+        if temperature is not None:
+            self._per_row("temperature", temperature, plan[0])
+            tau_ptr = temperature.data_ptr()
+        return plan, t_ptr, tau_ptr
+
+    def _row_losses(self, logits, ids, teacher, side, ids_side, shared):
+        if logits.dim() != 2 or logits.shape[1] != self._table_rows(side):
             raise ValueError("logits must be [N, %d] on %s" % (self._table_rows(side), self.device))
-        return _matrix("logits", logits)
+        N = logits.shape[0]
+        k, rest = self._loss_plan(N, ids, teacher, side, ids_side, shared)
+        return (N,), (N, 2), (N, k, _logit_dtype(logits), *rest), _matrix("logits", logits)
 
     def loss(self, logits, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET, ids_side: int = TLI_SIDE_TARGET,
              shared: bool = False) -> Dict[str, torch.Tensor]:
         """Loss of every row of ``logits`` [N,V] against labels ``ids`` [N], or a teacher's logits ``teacher`` [N,k] of ``ids`` [N,k];
         ids of either vocabulary.  ``shared``: the softmax runs over the ids inside the intersection (drafter rows)."""
-        stride, N = self._loss_rows(logits, side), logits.shape[0]
-        k, t_dtype, t_ptr, support = self._targets(N, ids, teacher, temperature, side, ids_side, shared)
-        stats = torch.empty((N, 2), dtype=torch.float32, device=self.device)
-        loss = torch.empty((N,), dtype=torch.float32, device=self.device)
+        (one, two, head, stride), t_ptr, tau_ptr = self._loss_args("_row_losses", logits, ids, teacher, temperature, side, ids_side, shared)
+        stats = logits.new_empty(two, dtype=torch.float32)
+        loss = stats.new_empty(one)
         status = torch.empty_like(loss, dtype=torch.int32)
-        self._call(self._fn_loss, _PACK_LOSS(
-            N, k, _logit_dtype(logits), side, ids_side, support, t_dtype, logits.data_ptr(), stride, ids.data_ptr(), t_ptr,
-            0 if temperature is None else temperature.data_ptr(), loss.data_ptr(), stats.data_ptr(), status.data_ptr()))
+        self._call(self._fn_loss, _PACK_LOSS(*head, logits.data_ptr(), stride, ids.data_ptr(), t_ptr, tau_ptr, loss.data_ptr(), stats.data_ptr(),
+                                             status.data_ptr()))
         return {"loss": loss, "stats": stats, "status": status}
 
     def loss_grad(self, logits, ids, stats, grad_loss=None, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET,
                   ids_side: int = TLI_SIDE_TARGET, shared: bool = False, out=None) -> Dict[str, torch.Tensor]:
         """Gradient of sum(grad_loss * loss) with respect to the logits, in their type (``out=logits``: in place)."""
-        stride, N = self._loss_rows(logits, side), logits.shape[0]
-        k, t_dtype, t_ptr, support = self._targets(N, ids, teacher, temperature, side, ids_side, shared)
-        self._per_row("stats", stats, (N, 2))
+        (one, two, head, stride), t_ptr, tau_ptr = self._loss_args("_row_losses", logits, ids, teacher, temperature, side, ids_side, shared)
+        self._per_row("stats", stats, two)
         if grad_loss is not None:
-            self._per_row("grad_loss", grad_loss, (N,))
+            self._per_row("grad_loss", grad_loss, one)
         if out is None:
             out = logits.new_empty(logits.shape)
-        elif out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index:
+        elif out is not logits and (out.dtype is not logits.dtype or out.shape != logits.shape or out.get_device() != self._index):
             raise ValueError("out must have the logits' type, shape and device")
-        self._call(self._fn_loss_grad, _PACK_LOSS_GRAD(
-            N, k, _logit_dtype(logits), side, ids_side, support, t_dtype, logits.data_ptr(), stride, ids.data_ptr(), t_ptr,
-            0 if temperature is None else temperature.data_ptr(), stats.data_ptr(), 0 if grad_loss is None else grad_loss.data_ptr(),
-            out.data_ptr(), _matrix("out", out)))
+        self._call(self._fn_loss_grad, _PACK_LOSS_GRAD(*head, logits.data_ptr(), stride, ids.data_ptr(), t_ptr, tau_ptr, stats.data_ptr(),
+                                                       0 if grad_loss is None else grad_loss.data_ptr(), out.data_ptr(), _matrix("out", out)))
         return {"grad": out}
 
-    def _head(self, hidden, weight, k: int, side: int, grad: bool):
-        """(N, H, stride of hidden, stride of weight, scratch) of a head call; raises on what the library could not see."""
-        V, on = self._table_rows(side), self._index
-        if hidden.dim() != 2 or hidden.dtype is not torch.bfloat16 or hidden.get_device() != on:
+    def _head_losses(self, hidden, ids, teacher, side, ids_side, shared, grad, w_shape, w_stride, w_dtype):
+        if hidden.dim() != 2 or hidden.dtype is not torch.bfloat16:
             raise ValueError("hidden must be a bfloat16 [N, H] tensor on %s" % self.device)
         N, H = hidden.shape
-        if weight.dtype is not torch.bfloat16 or weight.shape != (V, H) or weight.get_device() != on:
-            raise ValueError("weight must be a bfloat16 [%d, %d] tensor on %s" % (V, H, self.device))
-        key = (N, H, k, side, grad)
-        need = self._plans.get(key)
-        if need is None:
-            need = self._plan(key, (tli_head_loss_grad_workspace_bytes if grad else tli_head_loss_workspace_bytes)(self.ctx, N, H, k, side))
+        V = self._table_rows(side)
+        if w_dtype is not torch.bfloat16 or w_shape != (V, H) or (H > 1 and w_stride[1] != 1):
+            raise ValueError("weight must be a bfloat16 [%d, %d] tensor with contiguous rows on %s" % (V, H, self.device))
+        k, rest = self._loss_plan(N, ids, teacher, side, ids_side, shared)
+        need = (tli_head_loss_grad_workspace_bytes if grad else tli_head_loss_workspace_bytes)(self.ctx, N, H, k, side)
         if need == 0:
-            raise TLIError(TLI_ERR_UNSUPPORTED, "tli_head_loss_workspace_bytes (H a multiple of 8 up to %d, N up to %d)" % (TLI_MAX_H, TLI_MAX_HEAD_TOKENS))
-        return N, H, _matrix("hidden", hidden), _matrix("weight", weight), self._scratch(need), need
+            raise TLIError(TLI_ERR_UNSUPPORTED, "tli_head_loss_workspace_bytes (H a multiple of 8 up to %d, N up to %d, k up to %d)"
+                           % (TLI_MAX_H, TLI_MAX_HEAD_TOKENS, TLI_MAX_TARGETS))
+        return (N,), (N, 2), (N, H, k, *rest), _matrix("hidden", hidden), w_stride[0], need
 
     def head_loss(self, hidden, weight, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET,
                   ids_side: int = TLI_SIDE_TARGET, shared: bool = False) -> Dict[str, torch.Tensor]:
         """:meth:`loss` of the logits ``hidden`` [N,H] x ``weight`` [V,H]^T (bfloat16, summed in fp32), which are not written."""
-        k, t_dtype, t_ptr, support = self._targets(hidden.shape[0], ids, teacher, temperature, side, ids_side, shared)
-        N, H, hs, wst, ws, need = self._head(hidden, weight, k, side, False)
-        dev = self.device
-        stats = torch.empty((N, 2), dtype=torch.float32, device=dev)
-        loss = torch.empty((N,), dtype=torch.float32, device=dev)
+        if weight.get_device() != self._index:
+            raise ValueError("weight must be on %s" % self.device)
+        (one, two, head, hs, wst, need), t_ptr, tau_ptr = self._loss_args(
+            "_head_losses", hidden, ids, teacher, temperature, side, ids_side, shared, (False, weight.shape, weight.stride(), weight.dtype))
+        stats = hidden.new_empty(two, dtype=torch.float32)
+        loss = stats.new_empty(one)
         status = torch.empty_like(loss, dtype=torch.int32)
         at = torch.empty_like(ids, dtype=torch.float32)
+        ws = self._scratch(need)
         self._call(self._fn_head_loss, _PACK_HEAD_LOSS(
-            N, H, k, side, ids_side, support, t_dtype, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr,
-            0 if temperature is None else temperature.data_ptr(), loss.data_ptr(), stats.data_ptr(), at.data_ptr(), status.data_ptr(),
-            ws.data_ptr(), need))
+            *head, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr, tau_ptr, loss.data_ptr(), stats.data_ptr(),
+            at.data_ptr(), status.data_ptr(), ws.data_ptr(), need))
         return {"loss": loss, "stats": stats, "target_logits": at, "status": status}
 
     def head_loss_grad(self, hidden, weight, ids, stats, target_logits, grad_loss=None, teacher=None, temperature=None,
                        side: int = TLI_SIDE_TARGET, ids_side: int = TLI_SIDE_TARGET, shared: bool = False,
                        hidden_grad: bool = True, weight_grad: bool = True) -> Dict[str, Optional[torch.Tensor]]:
         """Gradients of sum(grad_loss * loss) with respect to ``hidden`` and ``weight``, in bfloat16 (``None`` where not asked for)."""
-        k, t_dtype, t_ptr, support = self._targets(hidden.shape[0], ids, teacher, temperature, side, ids_side, shared)
-        N, H, hs, wst, ws, need = self._head(hidden, weight, k, side, True)
-        self._per_row("stats", stats, (N, 2))
+        if weight.get_device() != self._index:
+            raise ValueError("weight must be on %s" % self.device)
+        (one, two, head, hs, wst, need), t_ptr, tau_ptr = self._loss_args(
+            "_head_losses", hidden, ids, teacher, temperature, side, ids_side, shared, (True, weight.shape, weight.stride(), weight.dtype))
+        self._per_row("stats", stats, two)
         self._per_row("target_logits", target_logits, ids.shape)
         if grad_loss is not None:
-            self._per_row("grad_loss", grad_loss, (N,))
-        dh = torch.empty((N, H), dtype=torch.bfloat16, device=self.device) if hidden_grad else None
-        dw = torch.empty((weight.shape[0], H), dtype=torch.bfloat16, device=self.device) if weight_grad else None
-        status = torch.empty((N,), dtype=torch.int32, device=self.device)
+            self._per_row("grad_loss", grad_loss, one)
+        H = head[1]
+        dh = hidden.new_empty(hidden.shape) if hidden_grad else None
+        dw = weight.new_empty(weight.shape) if weight_grad else None
+        status = stats.new_empty(one, dtype=torch.int32)
+        ws = self._scratch(need)
         self._call(self._fn_head_loss_grad, _PACK_HEAD_LOSS_GRAD(
-            N, H, k, side, ids_side, support, t_dtype, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr,
-            0 if temperature is None else temperature.data_ptr(), stats.data_ptr(), target_logits.data_ptr(),
+            *head, hidden.data_ptr(), hs, weight.data_ptr(), wst, ids.data_ptr(), t_ptr, tau_ptr, stats.data_ptr(), target_logits.data_ptr(),
             0 if grad_loss is None else grad_loss.data_ptr(), 0 if dh is None else dh.data_ptr(), H, 0 if dw is None else dw.data_ptr(), H,
             status.data_ptr(), ws.data_ptr(), need))
         return {"grad_hidden": dh, "grad_weight": dw, "status": status}
