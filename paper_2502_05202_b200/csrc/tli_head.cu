@@ -36,7 +36,6 @@ constexpr int kHeadK = 64;                 // elements of the contracted axis in
 constexpr int kHeadN = 256;                // columns of a tile
 constexpr int kHeadABytes = 128 * kHeadK * 2;
 constexpr int kHeadSlab = 32 * 128;        // what a warp of the epilogue has on its way out: 32 rows of 128 bytes
-constexpr int kHeadRowBlock = 32;          // rows per CTA of the targets and gather kernels
 enum : int { HEAD_STATS = 0, HEAD_SLOPE = 1, HEAD_GRADS = 2 };
 
 template <int CG> struct HeadRing {
@@ -130,47 +129,59 @@ struct HeadTile {
     int k0, ks;                            // first element of the contracted axis, steps of kHeadK
     int split;                             // GRADS: of d hidden; -1: a tile of d weight
 };
+// The tiles of CTA (pair) `cta` of `ctas`, one after the other.  GRADS: d hidden's tiles are the long ones and come first, dealt out in turn;
+// where they do not come out even, the CTAs with one less begin with as many more of d weight's tiles as one of them is worth.  Tiles side
+// by side run at the same time: they share the operand that is not in L2.
 template <int MODE, int CG> struct HeadTiles {
-    int mb, nb, hb, t2, total, k2, k3;
-    __device__ __forceinline__ HeadTiles(const HeadGemm &P, int rows) {
+    int cta, ctas, mb, nb, hb, t2, t3, k2, k3, extra, ahead;
+    __device__ __forceinline__ HeadTiles(const HeadGemm &P, int rows, int cta_, int ctas_) {
+        cta = cta_; ctas = ctas_;
         mb = P.early ? 1 : (rows + 128 * CG - 1) / (128 * CG);
         if constexpr (MODE == HEAD_GRADS) {
             hb = (P.H + kHeadN - 1) / kHeadN;
             nb = (P.cols + 128 * CG - 1) / (128 * CG);
             t2 = P.want_dh ? mb * hb * P.splits : 0;
-            total = t2 + (P.want_dw ? nb * hb : 0);
+            t3 = P.want_dw ? nb * hb : 0;
             k2 = (P.cols + kHeadK - 1) / kHeadK;
             k3 = (rows + kHeadK - 1) / kHeadK;
+            extra = t2 % ctas;                                     // CTAs with one more tile of d hidden
+            ahead = (k2 / P.splits + kTileSteps) / (k3 + kTileSteps);
         } else {
-            hb = t2 = k3 = 0;
+            hb = t3 = k3 = extra = ahead = 0;
             nb = (P.cols + P.bn - 1) / P.bn;
-            total = mb * nb;
+            t2 = mb * nb;
             k2 = (P.H + kHeadK - 1) / kHeadK;
         }
     }
-    __device__ __forceinline__ HeadTile at(const HeadGemm &P, int t) const {
-        HeadTile w;
+    static constexpr int kTileSteps = 3;                           // what a tile costs beside its steps, in steps
+    // the CTA's i-th tile; false: it has no more
+    __device__ __forceinline__ bool get(const HeadGemm &P, int i, HeadTile &w) const {
+        const int t = cta + i * ctas;
         w.split = 0;
         if constexpr (MODE == HEAD_GRADS) {
-            w.n = t % hb * kHeadN;
-            if (t < t2) {                                          // d hidden: a row block's columns next to one another
+            const int mine = t2 / ctas + (cta < extra);
+            if (i < mine) {                                        // d hidden: a row block's columns next to one another
                 const int r = t / hb;
+                w.n = t % hb * kHeadN;
                 w.m = r % mb * 128 * CG;
                 w.split = r / mb;
                 const int a = static_cast<int>(static_cast<long long>(k2) * w.split / P.splits), b = static_cast<int>(static_cast<long long>(k2) * (w.split + 1) / P.splits);
                 w.k0 = a * kHeadK; w.ks = b - a;
-            } else {
-                w.n = (t - t2) % hb * kHeadN;
-                w.m = (t - t2) / hb * 128 * CG;
-                w.split = -1;
-                w.k0 = 0; w.ks = k3;
+                return true;
             }
+            const int j = i - mine, before = ahead * (ctas - extra);      // tiles of the CTAs that are ahead
+            const int u = cta < extra ? before + j * ctas + cta : j < ahead ? j * (ctas - extra) + cta - extra : before + (j - ahead) * ctas + cta;
+            w.n = u % hb * kHeadN;
+            w.m = u / hb * 128 * CG;
+            w.split = -1;
+            w.k0 = 0; w.ks = k3;
+            return u < t3;
         } else {                                                   // the row blocks of a tile of the weight next to one another
-            w.m = t % mb * 128 * CG;
-            w.n = t / mb * P.bn;
+            w.m = t % max(mb, 1) * 128 * CG;
+            w.n = t / max(mb, 1) * P.bn;
             w.k0 = 0; w.ks = k2;
+            return t < t2;
         }
-        return w;
     }
 };
 
@@ -194,6 +205,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
         for (int i = 0; i < 2; ++i) { mbar_init(&sm.tfull[i], 1); mbar_init(&sm.tempty[i], kHeadEpilogue * CG); }
         mbar_init(&sm.drain, 1);
         sm.error = 0;
+        for (const CUtensorMap *map : {&P.a, &P.b, &P.a2, &P.b2, &P.out, &P.out2})
+            if (MODE == HEAD_GRADS || (map != &P.a2 && map != &P.b2 && map != &P.out2 && (MODE == HEAD_SLOPE || map != &P.out)))
+                asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -210,7 +224,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
     if constexpr (CG == 2) cluster_barrier();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
-    const int first_tile = blockIdx.x / CG, step = gridDim.x / CG;
+    const int cta = blockIdx.x / CG, ctas = gridDim.x / CG;
     // The weight's boxes of step k of a tile; stages are counted by it.
     auto load_weight = [&](const HeadTile &w, int k, unsigned st) {
         const uint32_t b = ring + st * R::kStageBytes + kHeadABytes, bar = CG == 1 ? smem_addr(&sm.full[st]) : cluster_addr(smem_addr(&sm.full[st]), 0u);
@@ -226,9 +240,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
     // done: it may be read before the kernels in between are.
     unsigned early = 0;
     if (P.early && threadIdx.x == 0) {
-        const HeadTiles<MODE, CG> tiles(P, 1);
-        if (first_tile < (MODE == HEAD_GRADS ? tiles.t2 : tiles.total)) {
-            const HeadTile w = tiles.at(P, first_tile);
+        HeadTile w;
+        if (HeadTiles<MODE, CG>(P, 1, cta, ctas).get(P, 0, w) && w.split >= 0) {
             early = min(w.ks, R::kStages);
             for (unsigned k = 0; k < early; ++k) {
                 if (rank == 0) mbar_arrive_expect_tx(&sm.full[k], bytes);
@@ -239,15 +252,15 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
     __syncwarp();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int rows = *reinterpret_cast<const volatile int *>(P.n_valid);
-    const HeadTiles<MODE, CG> tiles(P, rows);
+    const HeadTiles<MODE, CG> tiles(P, rows, cta, ctas);
+    HeadTile w;
 
     if (warp == 0) {
         if (lane == 0) {
             asm volatile("fence.proxy.async;" ::: "memory");       // what kernels before this one stored, to the copies' view
             unsigned it = 0;
             bool ok = true;
-            for (int t = first_tile; t < tiles.total && ok; t += step) {
-                const HeadTile w = tiles.at(P, t);
+            for (int i = 0; ok && tiles.get(P, i, w); ++i) {
                 const int m = w.m + static_cast<int>(rank) * 128;
                 for (int k = 0; k < w.ks; ++k, ++it) {
                     const unsigned st = it % R::kStages, par = (it / R::kStages + 1) & 1u;
@@ -280,8 +293,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             const uint32_t base = 1u << 4 | 1u << 7 | 1u << 10 | static_cast<uint32_t>(128 * CG >> 4) << 24;
             unsigned it = 0, acc = 0;
             bool ok = true;
-            for (int t = first_tile; t < tiles.total && ok; t += step) {
-                const HeadTile w = tiles.at(P, t);
+            for (int i = 0; ok && tiles.get(P, i, w); ++i) {
                 const bool dw = MODE == HEAD_GRADS && w.split < 0, dh = MODE == HEAD_GRADS && !dw;
                 const int bn = MODE == HEAD_GRADS ? kHeadN : P.bn;
                 const uint32_t idesc = base | static_cast<uint32_t>(bn >> 3) << 17 | (dw ? 1u << 15 | 1u << 16 : dh ? 1u << 16 : 0u);
@@ -328,8 +340,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         };
-        for (int t = first_tile; t < tiles.total; t += step) {
-            const HeadTile w = tiles.at(P, t);
+        for (int i = 0; tiles.get(P, i, w); ++i) {
             const int m = w.m + static_cast<int>(rank) * 128, pos = m + row, m_warp = m + quarter * 32;
             // What depends on the row is a value here and no branch: a compiler that makes two paths of one (rows that count and rows that
             // do not) parts the warp in front of the instructions below that a whole warp has to take.
@@ -540,6 +551,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
 
 // ---- rows and targets ----
 
+constexpr int kHeadNear = 4;
+
 struct HeadRows {
     TargetParams T;
     int H, V;
@@ -550,11 +563,12 @@ struct HeadRows {
     int *status;
     const unsigned *error;
     // in the workspace
-    uint32_t *taking;                      // a bit per row, a word per CTA of the targets kernel
+    uint32_t *taking;                      // a bit per row, a byte per CTA of the targets kernel
     int *n_valid, *pos;                    // rows that take part; place of a row among them, -1
     float4 *by_row, *rowp;                 // {s, m, f, -} of a row; of the rows that take part, in their order
     int *tid; float *tval;                 // gradient: the targets' ids (-1) and elements of G, of all rows
     int *tid_of; float *tval_of;           // ... of the rows that take part, in their order
+    int *near_id; float *near_off;         // ... the kHeadNear largest of a row, and what bf16 leaves off them
     __nv_bfloat16 *rows;                   // [N, H]
     const float2 *part; long long part_pitch; int tiles;
     __nv_bfloat16 *G; long long pitch; int c0, cols;
@@ -616,12 +630,36 @@ template <bool GRAD> __device__ __forceinline__ bool head_row(const HeadRows &P,
                     }
                 }
             }
+            float val[Q];
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 const long long at = row * k + q * 32 + lane;
                 if (q * 32 + lane >= k) break;
                 P.tid[at] = id[q];
-                if (id[q] >= 0) P.tval[at] = fmaf(-slope.h, mass[q] / W, slope(__ldg(P.target_logits + at)));
+                if (id[q] >= 0) P.tval[at] = val[q] = fmaf(-slope.h, mass[q] / W, slope(__ldg(P.target_logits + at)));
+            }
+            // The row's few largest elements of G are most of it, and their rounding most of the error of d hidden: what it leaves off is kept.
+            // (The same id twice is one element.)
+#pragma unroll 1
+            for (int n = 0; n < kHeadNear; ++n) {
+                float most = -1.f, v = 0.f;
+                int v_id = -1;
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (q * 32 >= k) break;
+                    if (id[q] >= 0 && fabsf(val[q]) > most) { most = fabsf(val[q]); v = val[q]; v_id = id[q]; }
+                }
+                const float all = warp_max(most);
+                const unsigned who = __ballot_sync(0xffffffffu, v_id >= 0 && most == all);
+                const int from = who ? __ffs(who) - 1 : 0;
+                v = __shfl_sync(0xffffffffu, v, from);
+                v_id = who ? __shfl_sync(0xffffffffu, v_id, from) : -1;
+                if (lane == 0) {
+                    P.near_id[row * kHeadNear + n] = v_id;
+                    P.near_off[row * kHeadNear + n] = v - __bfloat162float(__float2bfloat16_rn(v));
+                }
+#pragma unroll
+                for (int q = 0; q < Q; ++q) id[q] = id[q] == v_id ? -1 : id[q];
             }
         }
     }
@@ -636,31 +674,40 @@ template <bool GRAD> __device__ __forceinline__ bool head_takes(const HeadRows &
         if (row_target(P.T, row, j, t) >= 0) return true;
     return false;
 }
-// A row of `hidden` (and its targets, for the gradient) to place pos, by one warp, eight vectors of a lane on their way.
-__device__ __forceinline__ void head_copy(const HeadRows &P, long long row, long long pos) {
-    const int lane = threadIdx.x & 31;
-    if (P.tid_of)
-        for (int j = lane; j < P.T.k; j += 32) {                   // (by the lanes that have written them, if this kernel has)
-            P.tid_of[pos * P.T.k + j] = __ldcg(P.tid + row * P.T.k + j);
-            P.tval_of[pos * P.T.k + j] = __ldcg(P.tval + row * P.T.k + j);
-        }
-    __nv_bfloat16 *to = P.rows + pos * P.H;
-    const __nv_bfloat16 *from = P.hidden + row * P.hidden_stride;
-    if (P.vec) {
-        const int nv = P.H / 8;
-#pragma unroll 1
-        for (int i0 = lane; i0 < nv; i0 += 256) {
-            uint4 v[8];
+// A row of `hidden` (and its targets, for the gradient) to its place, by one warp: the first 256 vectors are read ahead of knowing it.
+struct HeadCopy {
+    static constexpr int kAhead = 8;
+    uint4 v[kAhead];
+    __device__ __forceinline__ void load(const HeadRows &P, long long row) {
+        if (!P.vec) return;
+        const uint4 *from = reinterpret_cast<const uint4 *>(P.hidden + row * P.hidden_stride);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) if (i0 + q * 32 < nv) v[q] = __ldg(reinterpret_cast<const uint4 *>(from) + i0 + q * 32);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) if (i0 + q * 32 < nv) reinterpret_cast<uint4 *>(to)[i0 + q * 32] = v[q];
+        for (int q = 0; q < kAhead; ++q) {
+            const int i = (threadIdx.x & 31) + q * 32;
+            if (i < P.H / 8) v[q] = __ldg(from + i);
         }
-    } else {
-#pragma unroll 4
-        for (int i = lane; i < P.H; i += 32) to[i] = from[i];
     }
-}
+    __device__ __forceinline__ void store(const HeadRows &P, long long row, long long pos) const {
+        const int lane = threadIdx.x & 31;
+        if (P.tid_of)
+            for (int j = lane; j < P.T.k; j += 32) {               // (by the lanes that have written them, if this kernel has)
+                P.tid_of[pos * P.T.k + j] = __ldcg(P.tid + row * P.T.k + j);
+                P.tval_of[pos * P.T.k + j] = __ldcg(P.tval + row * P.T.k + j);
+            }
+        __nv_bfloat16 *to = P.rows + pos * P.H;
+        const __nv_bfloat16 *from = P.hidden + row * P.hidden_stride;
+        if (P.vec) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                if (lane + q * 32 < P.H / 8) reinterpret_cast<uint4 *>(to)[lane + q * 32] = v[q];
+#pragma unroll 8
+            for (int i = lane + kAhead * 32; i < P.H / 8; i += 32) reinterpret_cast<uint4 *>(to)[i] = __ldg(reinterpret_cast<const uint4 *>(from) + i);
+        } else {
+#pragma unroll 4
+            for (int i = lane; i < P.H; i += 32) to[i] = from[i];
+        }
+    }
+};
 // The number of rows that take part, and zeros behind them up to the next multiple of kHeadK (the contraction of d weight goes that far).
 __device__ __forceinline__ void head_end(const HeadRows &P, int total) {
     if (threadIdx.x == 0) *P.n_valid = total;
@@ -672,20 +719,29 @@ __device__ __forceinline__ void head_end(const HeadRows &P, int total) {
 constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
 constexpr int kHeadOneLaunch = 2048;       // lookups up to which every CTA looks at all rows before its own, instead of a launch that does
 
-// Few rows: both steps at once.
+// Few rows: both steps at once.  Eight warps have a row each, eight more count those before them meanwhile.
 template <bool GRAD>
-__global__ void __launch_bounds__(kGatherThreads) tli_head_prepare_kernel(const __grid_constant__ HeadRows P) {
+__global__ void __launch_bounds__(2 * kGatherThreads, 1) tli_head_prepare_kernel(const __grid_constant__ HeadRows P) {
     __shared__ int sums[kGatherRows], taking[kGatherRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (not before: see the early loads of the weight)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row0 = blockIdx.x * kGatherRows, row = row0 + warp;
-    int before = 0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < row0; i += kGatherThreads) before += head_takes<GRAD>(P, i);
+    bool takes = false;
     float4 r;
-    const bool takes = row < P.T.N && head_row<GRAD>(P, row, r);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (lane == 0) { sums[warp] = before; taking[warp] = takes; }
+    HeadCopy copy;
+    if (warp < kGatherRows) {
+        if (row < P.T.N) {
+            copy.load(P, row);                                     // (on its way while the targets are looked up)
+            takes = head_row<GRAD>(P, row, r);
+        }
+        if (lane == 0) taking[warp] = takes;
+    } else {
+        int before = 0;
+#pragma unroll 4
+        for (int i = threadIdx.x - kGatherThreads; i < row0; i += kGatherThreads) before += head_takes<GRAD>(P, i);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) sums[warp - kGatherRows] = before;
+    }
     __syncthreads();
     int total = 0, pos = 0;
 #pragma unroll
@@ -693,44 +749,48 @@ __global__ void __launch_bounds__(kGatherThreads) tli_head_prepare_kernel(const 
         total += sums[i] + taking[i];
         pos += sums[i] + (i < warp ? taking[i] : 0);
     }
-    if (row < P.T.N) {
+    if (warp < kGatherRows && row < P.T.N) {
         if (lane == 0) {
             P.pos[row] = takes ? pos : -1;
             if (takes) P.rowp[pos] = r;
         }
-        if (takes) head_copy(P, row, pos);
+        if (takes) copy.store(P, row, pos);
     }
     if (blockIdx.x == gridDim.x - 1) head_end(P, total);
 }
 
+// A bit per row, eight rows per CTA.
 template <bool GRAD>
-__global__ void __launch_bounds__(kHeadRowBlock * 32) tli_head_targets_kernel(const __grid_constant__ HeadRows P) {
-    __shared__ uint32_t word;
+__global__ void __launch_bounds__(kGatherThreads) tli_head_targets_kernel(const __grid_constant__ HeadRows P) {
+    __shared__ int taking[kGatherRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (not before: see the early loads of the weight)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long row = static_cast<long long>(blockIdx.x) * kHeadRowBlock + warp;
-    if (threadIdx.x == 0) word = 0;
-    __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * kGatherRows + warp;
+    bool takes = false;
     if (row < P.T.N) {
         float4 r;
-        const bool takes = head_row<GRAD>(P, row, r);
-        if (lane == 0) {
-            P.by_row[row] = r;
-            if (takes) atomicOr(&word, 1u << warp);
-        }
+        takes = head_row<GRAD>(P, row, r);
+        if (lane == 0) P.by_row[row] = r;
     }
+    if (lane == 0) taking[warp] = takes;
     __syncthreads();
-    if (threadIdx.x == 0) P.taking[blockIdx.x] = word;
+    if (threadIdx.x == 0) {
+        unsigned bits = 0;
+#pragma unroll
+        for (int i = 0; i < kGatherRows; ++i) bits |= static_cast<unsigned>(taking[i]) << i;
+        reinterpret_cast<unsigned char *>(P.taking)[blockIdx.x] = static_cast<unsigned char>(bits);
+    }
 }
 
 // The rows that take part, in order, a warp each.
 __global__ void __launch_bounds__(kGatherThreads) tli_head_gather_kernel(const __grid_constant__ HeadRows P) {
     __shared__ int sums[kGatherRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int row = blockIdx.x * kGatherRows + warp, at = blockIdx.x * kGatherRows / kHeadRowBlock;
+    const int row = blockIdx.x * kGatherRows + warp, at = row / 32;
+    HeadCopy copy;
+    if (row < P.T.N) copy.load(P, row);                            // (an input of the call: before the targets are there)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     int before = 0;
     for (int i = threadIdx.x; i < at; i += kGatherThreads) before += __popc(__ldcg(P.taking + i));
     before = __reduce_add_sync(0xffffffffu, before);
@@ -739,16 +799,17 @@ __global__ void __launch_bounds__(kGatherThreads) tli_head_gather_kernel(const _
     before = 0;
 #pragma unroll
     for (int i = 0; i < kGatherRows; ++i) before += sums[i];
-    const uint32_t word = __ldcg(P.taking + at);
+    uint32_t word = __ldcg(P.taking + at);
+    if (P.T.N - at * 32 < 32) word &= (1u << (P.T.N - at * 32)) - 1u;     // (of the last word only the rows there are)
     if (row < P.T.N) {
-        const int bit = row % kHeadRowBlock;
+        const int bit = row & 31;
         const bool takes = word >> bit & 1u;
         const int pos = before + __popc(word & ((1u << bit) - 1u));
         if (lane == 0) {
             P.pos[row] = takes ? pos : -1;
             if (takes) P.rowp[pos] = __ldcg(P.by_row + row);
         }
-        if (takes) head_copy(P, row, pos);
+        if (takes) copy.store(P, row, pos);
     }
     if (blockIdx.x == gridDim.x - 1) head_end(P, before + __popc(word));
 }
@@ -807,6 +868,8 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
             }
         }
     }
+    float tau_r = 1.f, s_r = 1.f;                                  // of the row whose tiles this thread joins
+    if (row0 + (threadIdx.x & 7) < P.T.N) row_scale(P.T.tau, row0 + (threadIdx.x & 7), tau_r, s_r);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (row < P.T.N) {
 #pragma unroll
@@ -818,7 +881,6 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
         const int pos = row0 + r < P.T.N ? __ldcg(P.pos + row0 + r) : -1;
         float m = kMaskBelow, sum = 0.f;
         if (pos >= 0) {
-            const float sc = __ldcg(&P.rowp[pos].x);
             const float2 *part = P.part + pos;
 #pragma unroll 1
             for (int i = t0; i < P.tiles; i += 32 * 4) {
@@ -826,7 +888,7 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
 #pragma unroll
                 for (int q = 0; q < 4; ++q) p[q] = i + q * 32 < P.tiles ? __ldcg(part + (i + q * 32) * P.part_pitch) : make_float2(kMaskBelow, 0.f);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) join_stats(sc, m, sum, p[q].x, p[q].y);
+                for (int q = 0; q < 4; ++q) join_stats(s_r, m, sum, p[q].x, p[q].y);
             }
         }
         sh_m[t0][r] = m; sh_s[t0][r] = sum;
@@ -897,6 +959,17 @@ __global__ void __launch_bounds__(256) tli_head_rows_kernel(const __grid_constan
             for (int q = 0; q < 8; ++q) { x[0] += a[q].x; x[1] += a[q].y; x[2] += a[q].z; x[3] += a[q].w; }
         }
     }
+    if (pos >= 0) {
+#pragma unroll
+        for (int n = 0; n < kHeadNear; ++n) {
+            const int v = __ldcg(P.near_id + row * kHeadNear + n);
+            if (v < 0) break;
+            const float off = __ldcg(P.near_off + row * kHeadNear + n);
+            const uint2 w = __ldg(reinterpret_cast<const uint2 *>(P.weight + v * P.weight_stride + u * 4));
+            x[0] = fmaf(off, bf16_lo(w.x), x[0]); x[1] = fmaf(off, bf16_hi(w.x), x[1]);
+            x[2] = fmaf(off, bf16_lo(w.y), x[2]); x[3] = fmaf(off, bf16_hi(w.y), x[3]);
+        }
+    }
     __nv_bfloat16 *to = P.grad_hidden + row * P.grad_hidden_stride + u * 4;
     if (P.out_vec) {
         uint32_t w[2];
@@ -941,7 +1014,7 @@ constexpr int kHeadMinSteps = 8;                       // of the contraction in 
 struct HeadPlan {
     int cg, bn, tiles;                     // CTAs per tile; columns of a forward tile, tiles of the vocabulary
     int run, runs, splits;                 // backward: columns of a run of G, runs, cuts of d hidden's contraction
-    size_t taking, n_valid, pos, by_row, rowp, tid, tval, tid_of, tval_of, rows, part, G, sums, total;
+    size_t taking, n_valid, pos, by_row, rowp, tid, tval, tid_of, tval_of, near_id, near_off, rows, part, G, sums, total;
 };
 
 HeadPlan head_plan(int N, int H, int k, int V, int num_sms, bool grad) {
@@ -960,7 +1033,7 @@ HeadPlan head_plan(int N, int H, int k, int V, int num_sms, bool grad) {
     }
     L.tiles = (V + L.bn - 1) / L.bn;
     size_t off = 0;
-    const size_t n = static_cast<size_t>(N), words = (n + kHeadRowBlock - 1) / kHeadRowBlock;
+    const size_t n = static_cast<size_t>(N), words = (n + 31) / 32;
     auto take = [&](size_t bytes) { const size_t at = off; off = align_up(off + bytes, 256); return at; };
     L.taking = take(4 * words);
     L.n_valid = take(4);
@@ -981,6 +1054,8 @@ HeadPlan head_plan(int N, int H, int k, int V, int num_sms, bool grad) {
         L.tval = take(4 * n * k);
         L.tid_of = take(4 * n * k);
         L.tval_of = take(4 * n * k);
+        L.near_id = take(4 * n * kHeadNear);
+        L.near_off = take(4 * n * kHeadNear);
         L.G = take(2 * n * L.run);
         L.sums = take(4 * n * H * L.splits);
     }
@@ -1021,8 +1096,8 @@ template <typename K> int launch_plain(K kernel, const HeadRows &P, long long bl
 // Which rows take part, and those one after the other.
 template <bool GRAD> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
     const long long N = R.T.N, gathers = (N + kGatherRows - 1) / kGatherRows;
-    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD>, R, gathers, kGatherThreads, stream, "launch tli_head_prepare_kernel");
-    const int rc = launch_plain(tli_head_targets_kernel<GRAD>, R, (N + kHeadRowBlock - 1) / kHeadRowBlock, kHeadRowBlock * 32, stream, "launch tli_head_targets_kernel");
+    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD>, R, gathers, 2 * kGatherThreads, stream, "launch tli_head_prepare_kernel");
+    const int rc = launch_plain(tli_head_targets_kernel<GRAD>, R, gathers, kGatherThreads, stream, "launch tli_head_targets_kernel");
     return rc == TLI_OK ? launch_plain(tli_head_gather_kernel, R, gathers, kGatherThreads, stream, "launch tli_head_gather_kernel") : rc;
 }
 
@@ -1116,6 +1191,7 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     R.stats = const_cast<float *>(a->stats); R.target_logits = const_cast<float *>(a->target_logits); R.g = a->grad_loss; R.status = a->status;
     R.tid = reinterpret_cast<int *>(ws + L.tid); R.tval = reinterpret_cast<float *>(ws + L.tval);
     R.tid_of = reinterpret_cast<int *>(ws + L.tid_of); R.tval_of = reinterpret_cast<float *>(ws + L.tval_of);
+    R.near_id = reinterpret_cast<int *>(ws + L.near_id); R.near_off = reinterpret_cast<float *>(ws + L.near_off);
     R.G = reinterpret_cast<__nv_bfloat16 *>(ws + L.G); R.pitch = L.run;
     R.sums = reinterpret_cast<const float *>(ws + L.sums); R.splits = L.splits;
     R.grad_hidden = reinterpret_cast<__nv_bfloat16 *>(a->grad_hidden); R.grad_hidden_stride = a->grad_hidden_stride;
