@@ -696,7 +696,8 @@ typedef struct {
     const float *stats;         /* [device] float[N, 2], of tli_head_loss() */
     const float *target_logits; /* [device] float[N, k], of tli_head_loss() */
     const float *grad_loss;     /* [device] float[N]; NULL: 1 */
-    void *grad_hidden;          /* [device] out bf16 [N, H], every row written; NULL: not wanted */
+    void *grad_hidden;          /* [device] out bf16 [N, H], every row written; NULL: not wanted.  May be `hidden`; the two
+                                 * gradients and the weight may not overlap (TLI_ERR_ARG) */
     int64_t grad_hidden_stride; /* elements from row to row, >= H */
     void *grad_weight;          /* [device] out bf16 [V, H], every row written, 16-byte aligned; NULL: not wanted */
     int64_t grad_weight_stride; /* elements from row to row, a multiple of 8, >= H */

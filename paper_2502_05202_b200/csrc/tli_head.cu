@@ -345,7 +345,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             // What depends on the row is a value here and no branch: a compiler that makes two paths of one (rows that count and rows that
             // do not) parts the warp in front of the instructions below that a whole warp has to take.
             float s = 0.f, top = 0.f, f = 0.f;
-            uint32_t live = pos < rows ? 0xffffffffu : 0u, store = lane == 0 && (MODE == HEAD_GRADS && w.split < 0 ? P.c0 + m_warp < P.V : m_warp < rows);
+            // (G is contracted over its rows in steps of kHeadK: the zeros of the last one are stored too)
+            const int rows_stored = MODE == HEAD_SLOPE ? (rows + kHeadK - 1) / kHeadK * kHeadK : rows;
+            uint32_t live = pos < rows ? 0xffffffffu : 0u, store = lane == 0 && (MODE == HEAD_GRADS && w.split < 0 ? P.c0 + m_warp < P.V : m_warp < rows_stored);
             asm volatile("" : "+r"(live), "+r"(store));
             if constexpr (MODE != HEAD_GRADS) {
                 const float4 r = __ldg(P.rowp + max(0, min(pos, rows - 1)));
@@ -577,8 +579,8 @@ struct HeadRows {
 };
 
 // Row `row` by one warp: whether it takes part, and in r what a tile of it needs.  GRAD: also its targets' elements, g/tau (q - mass).
-template <bool GRAD> __device__ __forceinline__ bool head_row(const HeadRows &P, long long row, float4 &r) {
-    constexpr int Q = TLI_MAX_TARGETS / 32;
+// Q: targets per lane, 1 or TLI_MAX_TARGETS / 32 (the short form is a quarter of the code: read once, code is what these kernels wait for).
+template <bool GRAD, int Q> __device__ __forceinline__ bool head_row(const HeadRows &P, long long row, float4 &r) {
     const int lane = threadIdx.x & 31, k = P.T.k;
     int id[Q];
     float t[Q];
@@ -720,11 +722,10 @@ constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
 constexpr int kHeadOneLaunch = 2048;       // lookups up to which every CTA looks at all rows before its own, instead of a launch that does
 
 // Few rows: both steps at once.  Eight warps have a row each, eight more count those before them meanwhile.
-template <bool GRAD>
+template <bool GRAD, int Q>
 __global__ void __launch_bounds__(2 * kGatherThreads, 1) tli_head_prepare_kernel(const __grid_constant__ HeadRows P) {
     __shared__ int sums[kGatherRows], taking[kGatherRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // (not before: see the early loads of the weight)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row0 = blockIdx.x * kGatherRows, row = row0 + warp;
     bool takes = false;
     float4 r;
@@ -732,17 +733,38 @@ __global__ void __launch_bounds__(2 * kGatherThreads, 1) tli_head_prepare_kernel
     if (warp < kGatherRows) {
         if (row < P.T.N) {
             copy.load(P, row);                                     // (on its way while the targets are looked up)
-            takes = head_row<GRAD>(P, row, r);
+            takes = head_row<GRAD, Q>(P, row, r);
         }
         if (lane == 0) taking[warp] = takes;
     } else {
         int before = 0;
-#pragma unroll 4
-        for (int i = threadIdx.x - kGatherThreads; i < row0; i += kGatherThreads) before += head_takes<GRAD>(P, i);
+        if (P.T.k == 1 && !P.T.teacher) {                          // labels: four rows' lookups at a time, step by step
+#pragma unroll 1
+            for (int i0 = threadIdx.x - kGatherThreads; i0 < row0; i0 += 4 * kGatherThreads) {
+                int id[4];
+                bool in[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int i = i0 + q * kGatherThreads;
+                    in[q] = i < row0;
+                    id[q] = in[q] ? __ldg(P.T.ids + i) : -1;
+                    float tau, s;
+                    if (in[q]) in[q] = (!P.T.tau || row_scale(P.T.tau, i, tau, s)) && !(GRAD && __ldg(P.stats + 2 * i + 1) == 0.f);
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) id[q] = table_id(P.T.map, P.T.n_ids, id[q]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) before += in[q] && id[q] >= 0 && (!P.T.mask || (__ldg(P.T.mask + (id[q] >> 5)) >> (id[q] & 31) & 1u));
+            }
+        } else {
+            for (int i = threadIdx.x - kGatherThreads; i < row0; i += kGatherThreads) before += head_takes<GRAD>(P, i);
+        }
         before = __reduce_add_sync(0xffffffffu, before);
         if (lane == 0) sums[warp - kGatherRows] = before;
     }
     __syncthreads();
+    // (Not before the wait: see the early loads of the weight.  And not before the lookups: behind 28 MB of weight each of them took 4 us.)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int total = 0, pos = 0;
 #pragma unroll
     for (int i = 0; i < kGatherRows; ++i) {
@@ -760,7 +782,7 @@ __global__ void __launch_bounds__(2 * kGatherThreads, 1) tli_head_prepare_kernel
 }
 
 // A bit per row, eight rows per CTA.
-template <bool GRAD>
+template <bool GRAD, int Q>
 __global__ void __launch_bounds__(kGatherThreads) tli_head_targets_kernel(const __grid_constant__ HeadRows P) {
     __shared__ int taking[kGatherRows];
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -769,7 +791,7 @@ __global__ void __launch_bounds__(kGatherThreads) tli_head_targets_kernel(const 
     bool takes = false;
     if (row < P.T.N) {
         float4 r;
-        takes = head_row<GRAD>(P, row, r);
+        takes = head_row<GRAD, Q>(P, row, r);
         if (lane == 0) P.by_row[row] = r;
     }
     if (lane == 0) taking[warp] = takes;
@@ -825,8 +847,8 @@ __device__ __forceinline__ float dot_bf16(const uint4 &a, const uint4 &b, float 
     for (int i = 0; i < 8; ++i) acc = fmaf(x[i], y[i], acc);
     return acc;
 }
+template <int Q>
 __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constant__ HeadRows P) {
-    constexpr int Q = TLI_MAX_TARGETS / 32;
     __shared__ float sh_m[32][kHeadLossRows], sh_s[32][kHeadLossRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
@@ -1094,11 +1116,14 @@ template <typename K> int launch_plain(K kernel, const HeadRows &P, long long bl
 }
 
 // Which rows take part, and those one after the other.
-template <bool GRAD> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
+template <bool GRAD, int Q> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
     const long long N = R.T.N, gathers = (N + kGatherRows - 1) / kGatherRows;
-    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD>, R, gathers, 2 * kGatherThreads, stream, "launch tli_head_prepare_kernel");
-    const int rc = launch_plain(tli_head_targets_kernel<GRAD>, R, gathers, kGatherThreads, stream, "launch tli_head_targets_kernel");
+    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD, Q>, R, gathers, 2 * kGatherThreads, stream, "launch tli_head_prepare_kernel");
+    const int rc = launch_plain(tli_head_targets_kernel<GRAD, Q>, R, gathers, kGatherThreads, stream, "launch tli_head_targets_kernel");
     return rc == TLI_OK ? launch_plain(tli_head_gather_kernel, R, gathers, kGatherThreads, stream, "launch tli_head_gather_kernel") : rc;
+}
+template <bool GRAD> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
+    return R.T.k <= 32 ? launch_head_rows<GRAD, 1>(R, stream) : launch_head_rows<GRAD, TLI_MAX_TARGETS / 32>(R, stream);
 }
 
 size_t head_workspace(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side, bool grad) {
@@ -1106,6 +1131,15 @@ size_t head_workspace(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32
     if (side != TLI_SIDE_TARGET && side != TLI_SIDE_DRAFTER) return 0;
     return head_plan(N, H, k, side == TLI_SIDE_TARGET ? ctx->V_t : ctx->V_d, ctx->num_sms, grad).total;
 }
+
+// The bytes from the first to the last element of a bf16 matrix.
+struct Span {
+    const char *begin, *end;
+    Span(const void *p, int64_t rows, int64_t stride, int64_t width) : begin(static_cast<const char *>(p)), end(begin) {
+        if (p && rows > 0) end += ((rows - 1) * stride + width) * 2;
+    }
+    bool meets(const Span &o) const { return begin < o.end && o.begin < end; }
+};
 
 // What both head calls check and set up alike.
 int prepare_head(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side, int32_t ids_side, int32_t support, const void *hidden, int64_t hidden_stride,
@@ -1171,7 +1205,9 @@ int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *a, void *cuda_stream) 
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     rc = launch_head_rows<false>(R, stream);
     if (rc == TLI_OK) rc = launch_head_gemm<HEAD_STATS>(G, L.cg, ctx, static_cast<long long>(L.tiles) * ((a->N + 128 * L.cg - 1) / (128 * L.cg)), stream);
-    if (rc == TLI_OK) rc = launch_plain(tli_head_loss_kernel, R, (a->N + kHeadLossRows - 1) / kHeadLossRows, 256, stream, "launch tli_head_loss_kernel");
+    const long long groups = (a->N + kHeadLossRows - 1) / kHeadLossRows;
+    if (rc == TLI_OK && a->k <= 32) rc = launch_plain(tli_head_loss_kernel<1>, R, groups, 256, stream, "launch tli_head_loss_kernel");
+    else if (rc == TLI_OK) rc = launch_plain(tli_head_loss_kernel<TLI_MAX_TARGETS / 32>, R, groups, 256, stream, "launch tli_head_loss_kernel");
     return rc;
 }
 
@@ -1187,6 +1223,9 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     if (!a->grad_hidden && !a->grad_weight) return TLI_ERR_ARG;
     if (a->grad_hidden && (reinterpret_cast<uintptr_t>(a->grad_hidden) % 2 || (a->N > 1 && a->grad_hidden_stride < a->H))) return TLI_ERR_ARG;
     if (a->grad_weight && (!on_vectors(a->grad_weight, a->grad_weight_stride, 2) || a->grad_weight_stride < a->H)) return TLI_ERR_ARG;
+    // (hidden has been copied when the gradients are written, the weight is read to the end)
+    const Span dh(a->grad_hidden, a->N, a->grad_hidden_stride, a->H), dw(a->grad_weight, R.V, a->grad_weight_stride, a->H), w(a->weight, R.V, a->weight_stride, a->H);
+    if (dh.meets(w) || dw.meets(w) || dh.meets(dw)) return TLI_ERR_ARG;
     char *ws = reinterpret_cast<char *>(a->workspace);
     R.stats = const_cast<float *>(a->stats); R.target_logits = const_cast<float *>(a->target_logits); R.g = a->grad_loss; R.status = a->status;
     R.tid = reinterpret_cast<int *>(ws + L.tid); R.tval = reinterpret_cast<float *>(ws + L.tval);

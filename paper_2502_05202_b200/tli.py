@@ -1071,7 +1071,10 @@ class Verifier:
     def loss(self, logits, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET, ids_side: int = TLI_SIDE_TARGET,
              shared: bool = False) -> Dict[str, torch.Tensor]:
         """Loss of every row of ``logits`` [N,V] against labels ``ids`` [N], or a teacher's logits ``teacher`` [N,k] of ``ids`` [N,k];
-        ids of either vocabulary.  ``shared``: the softmax runs over the ids inside the intersection (drafter rows)."""
+        ids of either vocabulary.  ``shared``: the softmax runs over the ids inside the intersection (drafter rows).  Returns ``loss`` [N],
+        ``stats`` [N,2] (for :meth:`loss_grad`) and ``status`` [N]; no autograd graph is recorded."""
+        if logits.requires_grad and torch.is_grad_enabled():
+            warnings.warn("loss() records no autograd graph: the logits get their gradient from loss_grad(), or detach them", stacklevel=2)
         (one, two, head, stride), t_ptr, tau_ptr = self._loss_args("_row_losses", logits, ids, teacher, temperature, side, ids_side, shared)
         stats = logits.new_empty(two, dtype=torch.float32)
         loss = stats.new_empty(one)
@@ -1112,6 +1115,8 @@ class Verifier:
     def head_loss(self, hidden, weight, ids, teacher=None, temperature=None, side: int = TLI_SIDE_TARGET,
                   ids_side: int = TLI_SIDE_TARGET, shared: bool = False) -> Dict[str, torch.Tensor]:
         """:meth:`loss` of the logits ``hidden`` [N,H] x ``weight`` [V,H]^T (bfloat16, summed in fp32), which are not written."""
+        if (hidden.requires_grad or weight.requires_grad) and torch.is_grad_enabled():
+            warnings.warn("head_loss() records no autograd graph: gradients come from head_loss_grad(), or detach its inputs", stacklevel=2)
         if weight.get_device() != self._index:
             raise ValueError("weight must be on %s" % self.device)
         (one, two, head, hs, wst, need), t_ptr, tau_ptr = self._loss_args(

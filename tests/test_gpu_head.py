@@ -273,6 +273,66 @@ def test_nothing():
     assert f["loss"].shape == (0,) and b["grad_hidden"].shape == (0, 64) and (b["grad_weight"] == 0).all()
 
 
+@pytest.mark.parametrize("N", [1, 20, 33, 64, 65, 97, 130, 200, 300])
+def test_scratch_that_holds_nan(N):
+    """Nothing of the workspace is read that the call has not written."""
+    rng = np.random.default_rng(N)
+    V, H = 700, 136
+    m = make_map(rng, V, V, 0.5)
+    v = tli.Verifier(V, V, m)
+    h, w, ids, teacher = inputs(rng, N, H, V, 3, V)
+    ids[0] = np.flatnonzero(m >= 0)[:3]
+    d = dict(teacher=teacher, side=D, ids_side=D, shared=True)
+    d_ids = torch.from_numpy(ids).cuda()
+    f = v.head_loss(h, w, d_ids, **d)
+    b = v.head_loss_grad(h, w, d_ids, f["stats"], f["target_logits"], **d)
+    assert all(torch.isfinite(x).all() for x in (f["loss"], f["stats"], b["grad_hidden"], b["grad_weight"]))
+    v._scratch = lambda need: torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    f2 = v.head_loss(h, w, d_ids, **d)
+    b2 = v.head_loss_grad(h, w, d_ids, f["stats"], f["target_logits"], **d)
+    assert all(torch.equal(f[k], f2[k]) for k in f) and all(torch.equal(b[k], b2[k]) for k in b)
+
+
+def test_a_first_call_that_is_captured():
+    code = """
+import numpy as np, torch
+from paper_2502_05202_b200 import tli
+v = tli.Verifier(500, 2, np.array([0, -1], np.int32))
+for N in (8, 300):
+    h, w = torch.randn(N, 64, device="cuda").bfloat16(), torch.randn(500, 64, device="cuda").bfloat16()
+    ids = torch.arange(N, device="cuda", dtype=torch.int32)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f = v.head_loss(h, w, ids)
+        b = v.head_loss_grad(h, w, ids, f["stats"], f["target_logits"])
+    g.replay()
+    torch.cuda.synchronize()
+    e = v.head_loss(h, w, ids)
+    assert torch.equal(e["loss"], f["loss"]) and torch.equal(v.head_loss_grad(h, w, ids, e["stats"], e["target_logits"])["grad_weight"], b["grad_weight"])
+"""
+    import os
+    import subprocess
+    import sys
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+
+def test_hidden_gradient_in_place():
+    rng = np.random.default_rng(11)
+    v = tli.Verifier(300, 2, np.array([0, -1], np.int32))
+    for N in (40, 300):
+        h, w, ids, _ = inputs(rng, N, 64, 300, 0, 300)
+        d_ids = torch.from_numpy(ids).cuda()
+        f = v.head_loss(h, w, d_ids)
+        want = v.head_loss_grad(h, w, d_ids, f["stats"], f["target_logits"])
+        dw = torch.empty_like(w)
+        ws = torch.empty(tli.tli_head_loss_grad_workspace_bytes(v.ctx, N, 64, 1, 0), dtype=torch.uint8, device="cuda")
+        a = tli.tli_head_loss_grad_args(N, 64, 1, 0, 0, 0, 0, h.data_ptr(), 64, w.data_ptr(), 64, d_ids.data_ptr(), None, None, f["stats"].data_ptr(),
+                                        f["target_logits"].data_ptr(), None, h.data_ptr(), 64, dw.data_ptr(), 64, None, ws.data_ptr(), ws.numel())
+        assert tli.load().tli_head_loss_grad(v.ctx, ctypes.byref(a), torch.cuda.current_stream().cuda_stream) == tli.TLI_OK
+        assert torch.equal(h, want["grad_hidden"]) and torch.equal(dw, want["grad_weight"])
+
+
 def test_captured_replayed_and_on_two_streams():
     rng = np.random.default_rng(8)
     V = 3000
@@ -378,7 +438,8 @@ def test_refusals():
         assert f(N=tli.TLI_MAX_HEAD_TOKENS + 1) == tli.TLI_ERR_UNSUPPORTED and f(H=tli.TLI_MAX_H + 8) == tli.TLI_ERR_UNSUPPORTED
     assert forward(loss=None) == tli.TLI_ERR_ARG
     for bad in (dict(grad_hidden=None, grad_weight=None), dict(grad_hidden=dh.data_ptr() + 1), dict(grad_hidden_stride=H - 1), dict(grad_weight=dw.data_ptr() + 8),
-                dict(grad_weight_stride=H + 4), dict(grad_weight_stride=8)):
+                dict(grad_weight_stride=H + 4), dict(grad_weight_stride=8), dict(grad_weight=w.data_ptr()), dict(grad_hidden=w.data_ptr() + 32),
+                dict(grad_hidden=dw.data_ptr()), dict(grad_weight=w.data_ptr() + 16 * (V - 1) * 2)):
         assert back(**bad) == tli.TLI_ERR_ARG, bad
     assert back(grad_hidden=None) == tli.TLI_OK and back(grad_weight=None) == tli.TLI_OK
     for size in (tli.tli_head_loss_workspace_bytes, tli.tli_head_loss_grad_workspace_bytes):
