@@ -10,7 +10,8 @@
 //                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace,
 //                             <GRADS>  d hidden += G * weight and d weight = G^T * hidden of that run, one list of tiles.
 //   tli_head_rows_kernel      d hidden from its fp32 sums to bf16, at the rows' places.
-// The run keeps G near the size of L2 (128 MB), whatever the vocabulary.
+// A run's G has 256 MB at most, whatever the vocabulary: 8192 tokens x 128 256 x 2048 in 9.9 ms; with 128 MB, about what L2 holds, 11.2 (more launches and
+// shorter sums of d hidden), with 64 MB 10.9, with 32 MB 14.1, with 512 MB 10.2.
 //
 // tli_head_gemm_kernel: persistent, one CTA per SM or one pair (CG = 2) per two SMs.  A tile of D is 128 CG rows x 256 columns of fp32 in
 // tensor memory, two of them, so that the epilogue of one runs under the products of the next.  Warp 0 fills a ring of stages of
@@ -1030,7 +1031,7 @@ bool tensor_map(CUtensorMap *map, bool f32, const void *base, long long inner, l
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr long long kHeadRunBytes = 128ll << 20;       // of G
+constexpr long long kHeadRunBytes = 256ll << 20;       // of G
 constexpr int kHeadMinSteps = 8;                       // of the contraction in a split of d hidden
 
 struct HeadPlan {

@@ -162,8 +162,8 @@ def test_long_contractions():
 def test_runs_of_the_vocabulary():
     """More rows than one run of G holds for the whole vocabulary; the last run is a short one."""
     rng = np.random.default_rng(2)
-    V, N, k = 6000, 20000, 2
-    m = make_map(rng, 6100, V)
+    V, N, k = 20000, 20000, 2
+    m = make_map(rng, 6100, V, 0.3)
     v = tli.Verifier(6100, V, m)
     h, w, ids, teacher = inputs(rng, N, 64, V, k, V)
     d = dict(teacher=teacher, side=D, ids_side=D)
