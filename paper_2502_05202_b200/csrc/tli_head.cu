@@ -720,7 +720,7 @@ __device__ __forceinline__ void head_end(const HeadRows &P, int total) {
 }
 
 constexpr int kGatherThreads = 256, kGatherRows = kGatherThreads / 32;
-constexpr int kHeadOneLaunch = 2048;       // lookups up to which every CTA looks at all rows before its own, instead of a launch that does
+constexpr int kHeadOneLaunch = 1024;       // lookups up to which every CTA looks at all rows before its own, instead of a launch that does
 
 // Few rows: both steps at once.  Eight warps have a row each, eight more count those before them meanwhile.
 template <bool GRAD, int Q>
@@ -837,9 +837,8 @@ __global__ void __launch_bounds__(kGatherThreads) tli_head_gather_kernel(const _
     if (blockIdx.x == gridDim.x - 1) head_end(P, before + __popc(word));
 }
 
-// ---- forward: the loss of eight rows per CTA ----
+// ---- forward: the loss ----
 
-constexpr int kHeadLossRows = 8;
 __device__ __forceinline__ float dot_bf16(const uint4 &a, const uint4 &b, float acc) {
     float x[8], y[8];
     unpack<TLI_BF16>(a, x);
@@ -848,12 +847,13 @@ __device__ __forceinline__ float dot_bf16(const uint4 &a, const uint4 &b, float 
     for (int i = 0; i < 8; ++i) acc = fmaf(x[i], y[i], acc);
     return acc;
 }
-template <int Q>
+// ROWS rows per CTA: eight, a warp each, for few targets; one, its targets dealt out to the warps four at a time, for more.
+template <int Q, int ROWS>
 __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constant__ HeadRows P) {
-    __shared__ float sh_m[32][kHeadLossRows], sh_s[32][kHeadLossRows];
+    __shared__ float sh_m[256 / ROWS][ROWS], sh_s[256 / ROWS][ROWS], sh_z[ROWS == 1 ? Q * 32 : 1];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
-    const long long row0 = static_cast<long long>(blockIdx.x) * kHeadLossRows, row = row0 + warp, at = row * k;
+    const long long row0 = static_cast<long long>(blockIdx.x) * ROWS, row = row0 + (ROWS == 1 ? 0 : warp), at = row * k;
     // The targets' logits are made of the call's inputs: a CTA that finds room beside the products begins with them.
     int id[Q];
     float t[Q], z[Q], tau = 1.f, s = 1.f;
@@ -874,42 +874,67 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             if (q * 32 >= k) break;
-            for (int l = 0; l < 32 && q * 32 + l < k; ++l) {
-                const int v = __shfl_sync(0xffffffffu, id[q], l);
-                if (v < 0) continue;
-                float dot = 0.f;
-                const __nv_bfloat16 *w = P.weight + v * P.weight_stride;
-                if (P.vec) {
-#pragma unroll 4
-                    for (int i = lane; i < P.H / 8; i += 32) dot = dot_bf16(__ldg(reinterpret_cast<const uint4 *>(h) + i), __ldg(reinterpret_cast<const uint4 *>(w) + i), dot);
-                } else {
-#pragma unroll 4
-                    for (int i = lane; i < P.H; i += 32) dot = fmaf(__bfloat162float(h[i]), __bfloat162float(w[i]), dot);
+#pragma unroll 1
+            for (int l = ROWS == 1 ? warp * 4 : 0; l < 32 && q * 32 + l < k; l += ROWS == 1 ? 32 : 4) {
+                float dot[4] = {};
+                const __nv_bfloat16 *w[4];
+                bool on[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int v = __shfl_sync(0xffffffffu, id[q], l + u);
+                    on[u] = v >= 0;
+                    w[u] = P.weight + max(v, 0) * P.weight_stride;
                 }
-                dot = warp_sum(dot);
-                if (l == lane) z[q] = dot;
+                if (P.vec) {
+#pragma unroll 2
+                    for (int i = lane; i < P.H / 8; i += 32) {
+                        const uint4 x = __ldg(reinterpret_cast<const uint4 *>(h) + i);
+                        uint4 y[4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) y[u] = on[u] ? __ldg(reinterpret_cast<const uint4 *>(w[u]) + i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) if (on[u]) dot[u] = dot_bf16(x, y[u], dot[u]);
+                    }
+                } else {
+                    for (int i = lane; i < P.H; i += 32) {
+                        const float x = __bfloat162float(h[i]);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) if (on[u]) dot[u] = fmaf(x, __bfloat162float(w[u][i]), dot[u]);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    dot[u] = warp_sum(dot[u]);
+                    if (ROWS == 1 && lane == u) sh_z[q * 32 + l + u] = on[u] ? dot[u] : 0.f;
+                    if (ROWS > 1 && l + u == lane && on[u]) z[q] = dot[u];
+                }
             }
         }
     }
+    if (ROWS == 1) {
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < Q; ++q) if (id[q] >= 0 && takes) z[q] = sh_z[q * 32 + lane];
+    }
     float tau_r = 1.f, s_r = 1.f;                                  // of the row whose tiles this thread joins
-    if (row0 + (threadIdx.x & 7) < P.T.N) row_scale(P.T.tau, row0 + (threadIdx.x & 7), tau_r, s_r);
+    if (row0 + threadIdx.x % ROWS < P.T.N) row_scale(P.T.tau, row0 + threadIdx.x % ROWS, tau_r, s_r);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (row < P.T.N) {
+    if (row < P.T.N && (ROWS > 1 || warp == 0)) {
 #pragma unroll
         for (int q = 0; q < Q; ++q)
             if (q * 32 + lane < k) P.target_logits[at + q * 32 + lane] = z[q];
     }
     {
-        const int r = threadIdx.x & 7, t0 = threadIdx.x >> 3;      // neighbouring threads: neighbouring rows of a tile
+        const int r = threadIdx.x % ROWS, t0 = threadIdx.x / ROWS; // neighbouring threads: neighbouring rows of a tile
         const int pos = row0 + r < P.T.N ? __ldcg(P.pos + row0 + r) : -1;
         float m = kMaskBelow, sum = 0.f;
         if (pos >= 0) {
             const float2 *part = P.part + pos;
 #pragma unroll 1
-            for (int i = t0; i < P.tiles; i += 32 * 4) {
+            for (int i = t0; i < P.tiles; i += 256 / ROWS * 4) {
                 float2 p[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) p[q] = i + q * 32 < P.tiles ? __ldcg(part + (i + q * 32) * P.part_pitch) : make_float2(kMaskBelow, 0.f);
+                for (int q = 0; q < 4; ++q) p[q] = i + q * (256 / ROWS) < P.tiles ? __ldcg(part + (i + q * (256 / ROWS)) * P.part_pitch) : make_float2(kMaskBelow, 0.f);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) join_stats(s_r, m, sum, p[q].x, p[q].y);
             }
@@ -917,7 +942,7 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
         sh_m[t0][r] = m; sh_s[t0][r] = sum;
     }
     __syncthreads();
-    if (row >= P.T.N) return;
+    if (row >= P.T.N || (ROWS == 1 && warp > 0)) return;
     const int timeout = *reinterpret_cast<const volatile unsigned *>(P.error) ? TLI_ROW_TIMEOUT : 0;
     if (!takes) {
         if (lane == 0) {
@@ -928,6 +953,8 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
         return;
     }
     float m = sh_m[lane][warp], sum = sh_s[lane][warp];
+#pragma unroll
+    for (int i = 32; i < 256 / ROWS; i += 32) join_stats(s, m, sum, sh_m[lane + i][warp], sh_s[lane + i][warp]);
     const float top = warp_max(m);
     sum = warp_sum(sum * ex2((m - top) * s));
     m = top;
@@ -1206,9 +1233,11 @@ int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *a, void *cuda_stream) 
     cudaStream_t stream = reinterpret_cast<cudaStream_t>(cuda_stream);
     rc = launch_head_rows<false>(R, stream);
     if (rc == TLI_OK) rc = launch_head_gemm<HEAD_STATS>(G, L.cg, ctx, static_cast<long long>(L.tiles) * ((a->N + 128 * L.cg - 1) / (128 * L.cg)), stream);
-    const long long groups = (a->N + kHeadLossRows - 1) / kHeadLossRows;
-    if (rc == TLI_OK && a->k <= 32) rc = launch_plain(tli_head_loss_kernel<1>, R, groups, 256, stream, "launch tli_head_loss_kernel");
-    else if (rc == TLI_OK) rc = launch_plain(tli_head_loss_kernel<TLI_MAX_TARGETS / 32>, R, groups, 256, stream, "launch tli_head_loss_kernel");
+    if (rc != TLI_OK) return rc;
+    // 1000 rows of 32 targets (V 4136, H 1960): 80 us a call with a warp per row and a target at a time, 72 with four at a time, 47 with a CTA per row
+    if (a->k <= 4) rc = launch_plain(tli_head_loss_kernel<1, 8>, R, (a->N + 7) / 8, 256, stream, "launch tli_head_loss_kernel");
+    else if (a->k <= 32) rc = launch_plain(tli_head_loss_kernel<1, 1>, R, a->N, 256, stream, "launch tli_head_loss_kernel");
+    else rc = launch_plain(tli_head_loss_kernel<TLI_MAX_TARGETS / 32, 1>, R, a->N, 256, stream, "launch tli_head_loss_kernel");
     return rc;
 }
 
