@@ -3,7 +3,7 @@
 //
 //   tli_loss_kernel        one thread-block cluster (1 to 8 CTAs) per row: running (max, sum) per thread in one pass over the
 //                          row, joined through warps, the CTA and distributed shared memory; the row's targets beside it.
-//   tli_loss_grad_kernel   a run of 32 KB of a row per CTA: g/tau q everywhere, then the targets' elements again.
+//   tli_loss_grad_kernel   a row, or a run of it where rows are few, per CTA: g/tau q everywhere, then the targets' elements again.
 //
 // Both are passes over the logits: bound by DRAM, and for bf16 rows near the special-function unit's rate (one ex2 per
 // element; 16 a clock and SM are 4.4e12/s where 6.5 TB/s of bf16 are 3.3e12/s).
@@ -147,6 +147,9 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
+// Bound by DRAM on large batches: 4096 fp32 rows of 256 000 (4.2 GB) in 0.61 ms, 6.8 TB/s; 8192 bf16 rows of 128 256 (2.1 GB) in 0.36 ms, 5.8 TB/s, the
+// special-function unit close behind.  On smaller ones by what a row costs beside its bytes (lookups, joins) and by how its CTAs fill the SMs: 1500
+// bf16 rows of 50 257 over the intersection, 20 targets each, 41 us for 151 MB, 34 without mask and with even rows.
 template <int DT>
 __global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_kernel(const __grid_constant__ LossParams P) {
     constexpr int WARPS = kLossThreads / 32, kBatch = kLossBatch<DT>;
@@ -271,6 +274,8 @@ template <int THREADS> __device__ __forceinline__ float target_mass(const Target
     return mass / W;
 }
 
+// Bound by DRAM: 8192 bf16 rows of 128 256 (2.1 GB read, 2.1 written) in 0.65 ms, 6.4 TB/s; 2048 of 49 152 with 32 targets and a mask in 76 us, 5.3 TB/s
+// (92 us with 32 KB of a row per CTA: the targets are then looked up three times a row).
 template <int DT>
 __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __grid_constant__ LossParams P) {
     constexpr int EPV = Elt<DT>::kPerVec, kBatch = kLossBatch<DT>;
