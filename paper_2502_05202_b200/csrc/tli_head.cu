@@ -34,9 +34,9 @@ namespace {
 constexpr int kHeadEpilogue = 8;           // warps of the epilogue: two per quarter of the rows, 128 columns each
 constexpr int kHeadThreads = 64 + 32 * kHeadEpilogue;
 // The matrix unit cuts what a sum cannot hold (it does not round): a sum of 2048 products of a logit was 1e-5 off where one rounded at every step
-// is 4e-6 off.  The logits that the statistics are made of are therefore summed in parts, which the epilogue adds up: 256 elements where the
-// weight's way through the SM is what counts (no slower than one part), else half of H but 512 to 1024 (8192 x 128 256 x 2048: one part
-// 3.07 ms and 1e-5 off, two 3.16 and 5e-6, four 3.35 and 2e-6).
+// is 4e-6 off.  The logits that the statistics are made of are therefore summed in parts, which the epilogue adds up: 128 elements where the
+// weight's way through the SM is what counts (one token: 32.3 us, 31.6 with 256, 33.5 with 64), else half of H but 512 to 1024 (8192 x
+// 128 256 x 2048: one part 3.07 ms and 1e-5 off, two 3.16 and 5e-6, four 3.35 and 2e-6).
 constexpr int kHeadK = 64;                 // elements of the contracted axis in a stage: 128 bytes, one swizzle span
 constexpr int kHeadN = 256;                // columns of a tile
 constexpr int kHeadABytes = 128 * kHeadK * 2;
@@ -1230,7 +1230,7 @@ int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *a, void *cuda_stream) 
     HeadGemm G;
     head_gemm_common(R, ctx, G);
     G.cols = R.V; G.bn = L.bn; G.early = a->N <= 128 * L.cg;
-    G.k_part = L.cg == 1 ? 4 : std::min(16, std::max(8, (R.H + 2 * kHeadK - 1) / (2 * kHeadK)));
+    G.k_part = L.cg == 1 ? 2 : std::min(16, std::max(8, (R.H + 2 * kHeadK - 1) / (2 * kHeadK)));
     G.a_rows = std::min(128, (a->N + 7) / 8 * 8);
     G.part = const_cast<float2 *>(R.part); G.part_pitch = R.part_pitch;
     if (!tensor_map(&G.a, false, R.rows, R.H, a->N, R.H, G.a_rows) || !tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, L.bn / L.cg)) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
