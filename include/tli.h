@@ -602,7 +602,7 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *args, void *cuda_str
  *     loss = sum over targets j of p_j (ln p_j - ln q[id_j])
  *     d loss / d z[v] = (q[v] - sum over j with id_j == v of p_j) / tau
  * The same id twice in a row counts twice.  A logit below -1e30 counts as -inf in the
- * sum.  Rows without a target that takes part (TLI_ROW_LEFT_OUT), without a logit above
+ * sum (at temperatures up to 1e20).  Rows without a target that takes part (TLI_ROW_LEFT_OUT), without a logit above
  * -inf (TLI_ROW_FALLBACK) or with a temperature that is not positive and finite, or whose
  * reciprocal is not (TLI_ROW_BAD_TEMPERATURE) have loss 0, stats 0 and gradient 0; NaN or
  * +inf among the logits or teacher logits that take part gives a loss and a gradient row

@@ -7,7 +7,7 @@
 //                             do, and a row that is left out may hold anything); for few rows tli_head_prepare_kernel does both.
 //   tli_head_gemm_kernel      <STATS>  forward: (max, sum) of every row over every tile of the vocabulary.
 //   tli_head_loss_kernel               forward: the tiles' pairs joined, the targets' logits, the loss.
-//                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace,
+//                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace;
 //                             <GRADS>  d hidden += G * weight and d weight = G^T * hidden of that run, one list of tiles.
 //   tli_head_rows_kernel      d hidden from its fp32 sums to bf16, at the rows' places.
 // A run's G has 256 MB at most, whatever the vocabulary: 8192 tokens x 128 256 x 2048 in 9.9 ms; with 128 MB, about what L2 holds, 11.2 (more launches and
@@ -289,6 +289,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             // every stage handed back: no arrival is under way when the CTA leaves
             for (unsigned j = it > R::kStages ? it - R::kStages : 0; j < it && ok; ++j) ok = mbar_wait(&sm.empty[j % R::kStages], (j / R::kStages) & 1u, &sm.error, P.error);
             if (!ok && rank == 0) {                                // no CTA of the pair may leave while copies to it are in flight
+                it = max(it, early);
                 for (unsigned j = it > R::kStages ? it - R::kStages : 0; j < it; ++j)
                     for (unsigned i = 0; i < kWaitLimit && !mbar_test(&sm.full[j % R::kStages], (j / R::kStages) & 1u); ++i) __nanosleep(64);
             }
@@ -471,13 +472,20 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t bits = columns(c0 + c + h * 32) & live;
+                        const bool whole = __all_sync(0xffffffffu, bits == 0xffffffffu);      // nothing to leave out, as in most tiles
+                        const uint64_t s2 = pack2(s, s), t2 = pack2(-top, -top), f2 = pack2(f, f);
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             float y[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                y[j] = ex2((x[h][i + j] - top) * s) * f;
-                                y[j] = bits >> (i + j) & 1u ? y[j] : 0.f;
+                            for (int j = 0; j < 8; j += 2) {
+                                float a, b;
+                                unpack2(mul2(add2(pack2(x[h][i + j], x[h][i + j + 1]), t2), s2), a, b);
+                                unpack2(mul2(pack2(ex2(a), ex2(b)), f2), y[j], y[j + 1]);
+                            }
+                            if (!whole) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) y[j] = bits >> (i + j) & 1u ? y[j] : 0.f;
                             }
                             slab_put(h * 4 + i / 8, pack_vector<TLI_BF16>(y));
                         }
@@ -507,10 +515,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     tmem_load32(d + h, x);
                     tmem_wait_load();
                     slab_free();
+                    if (w.ks == 0) {                               // (a split of a short run may have no step)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[i] = 0.f;
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[i + j] = w.ks ? x[i + j] : 0.f;     // (a split of a short run may have no step)
                         slab_put(i / 4, make_uint4(__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]), __float_as_uint(x[i + 3])));
                     }
                     slab_full();
@@ -527,13 +537,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     tmem_load32(d + c + 32, x[1]);
                     tmem_wait_load();
                     slab_free();
+                    if (w.ks == 0) {                               // (no row takes part)
+#pragma unroll
+                        for (int i = 0; i < 64; ++i) x[i >> 5][i & 31] = 0.f;
+                    }
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             float y[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) y[j] = w.ks ? x[h][i + j] : 0.f;
+                            for (int j = 0; j < 8; ++j) y[j] = x[h][i + j];
                             slab_put(h * 4 + i / 8, pack_vector<TLI_BF16>(y));
                         }
                     slab_full();

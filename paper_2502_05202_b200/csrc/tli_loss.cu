@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_
             st_cluster_f32(to, m);
             st_cluster_f32(to + 4, sum);
         }
+        __syncwarp();
         cluster_barrier();
         if (rank > 0) return;
         for (int i = 1; i < C; ++i) join_stats(s, m, sum, part[i][0], part[i][1]);
