@@ -462,8 +462,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                 }
                 const bool some = __any_sync(0xffffffffu, hits != 0);
                 const uint32_t d = sum_wait();
+                const int columns_here = m_warp < rows_stored ? 128 : 0;      // (32 rows none of which is stored: nothing to do)
 #pragma unroll 1
-                for (int c = 0; c < 128; c += 64) {
+                for (int c = 0; c < columns_here; c += 64) {
                     float x[2][32];
                     tmem_load32(d + c, x[0]);
                     tmem_load32(d + c + 32, x[1]);
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
             } else if (w.split >= 0) {                             // d hidden: fp32 sums, 32 columns a slab
                 const uint32_t d = sum_wait();
 #pragma unroll 1
-                for (int h = 0; h < 128 && w.n + c0 + h < P.H; h += 32) {
+                for (int h = 0; h < 128 && w.n + c0 + h < P.H && m_warp < rows; h += 32) {
                     float x[32];
                     tmem_load32(d + h, x);
                     tmem_wait_load();
@@ -593,12 +594,12 @@ struct HeadRows {
     __nv_bfloat16 *rows;                   // [N, H]
     const float2 *part; long long part_pitch; int tiles;
     __nv_bfloat16 *G; long long pitch; int c0, cols;
-    const float *sums; int splits;         // d hidden: [splits][N, H]
+    const float *sums; int splits, groups; // d hidden: [splits][N, H]; threads that share them
     __nv_bfloat16 *grad_hidden; long long grad_hidden_stride; int out_vec;
 };
 
 // Row `row` by one warp: whether it takes part, and in r what a tile of it needs.  GRAD: also its targets' elements, g/tau (q - mass).
-// Q: targets per lane, 1 or TLI_MAX_TARGETS / 32 (the short form is a quarter of the code: read once, code is what these kernels wait for).
+// Q: targets per lane, 1, 2, 4 or TLI_MAX_TARGETS / 32 (the short forms have less code: read once, code is what these kernels wait for).
 template <bool GRAD, int Q> __device__ __forceinline__ bool head_row(const HeadRows &P, long long row, float4 &r) {
     const int lane = threadIdx.x & 31, k = P.T.k;
     int id[Q];
@@ -640,6 +641,7 @@ template <bool GRAD, int Q> __device__ __forceinline__ bool head_row(const HeadR
 #pragma unroll
                 for (int b = 0; b < Q; ++b) {
                     if (b * 32 >= k) break;
+#pragma unroll 8
                     for (int l = 0; l < 32; ++l) {
                         const int other = __shfl_sync(0xffffffffu, id[b], l);
                         const float more = __shfl_sync(0xffffffffu, w[b], l);
@@ -867,7 +869,7 @@ __device__ __forceinline__ float dot_bf16(const uint4 &a, const uint4 &b, float 
 }
 // ROWS rows per CTA: eight, a warp each, for few targets; one, its targets dealt out to the warps four at a time, for more.
 template <int Q, int ROWS>
-__global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constant__ HeadRows P) {
+__global__ void __launch_bounds__(256, 4) tli_head_loss_kernel(const __grid_constant__ HeadRows P) {
     __shared__ float sh_m[256 / ROWS][ROWS], sh_s[256 / ROWS][ROWS], sh_z[ROWS == 1 ? Q * 32 : 1];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
@@ -1004,29 +1006,42 @@ __global__ void __launch_bounds__(256) tli_head_loss_kernel(const __grid_constan
 
 // ---- backward: d hidden at its rows' places ----
 
-__global__ void __launch_bounds__(256) tli_head_rows_kernel(const __grid_constant__ HeadRows P) {
+// Four columns of a row by P.groups threads, which share the splits (3 rows of 96 columns in 148 splits by one thread each: 35 us).
+constexpr int kRowsThreads = 256;
+template <bool SHARED>
+__global__ void __launch_bounds__(kRowsThreads) tli_head_rows_kernel(const __grid_constant__ HeadRows P) {
+    __shared__ float4 shared[SHARED ? kRowsThreads : 1];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int units = P.H / 4;
-    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= static_cast<long long>(P.T.N) * units) return;
-    const long long row = i / units;
-    const int u = static_cast<int>(i % units), pos = __ldcg(P.pos + row);
-    if (u == 0 && P.status && *reinterpret_cast<const volatile unsigned *>(P.error)) P.status[row] |= TLI_ROW_TIMEOUT;
+    const int groups = SHARED ? P.groups : 1, units = P.H / 4, tx = kRowsThreads / groups, group = SHARED ? threadIdx.x / tx : 0;
+    const long long i = static_cast<long long>(blockIdx.x) * tx + threadIdx.x % tx, row = i / units;
+    const bool in = i < static_cast<long long>(P.T.N) * units;
+    const int u = static_cast<int>(i % units), pos = in ? __ldcg(P.pos + row) : -1;
+    if (in && group == 0 && u == 0 && P.status && *reinterpret_cast<const volatile unsigned *>(P.error)) P.status[row] |= TLI_ROW_TIMEOUT;
     if (!P.grad_hidden) return;
     float x[4] = {};
     if (pos >= 0) {
         const float *p = P.sums + static_cast<long long>(pos) * P.H + u * 4;
         const long long next = static_cast<long long>(P.T.N) * P.H;
 #pragma unroll 1
-        for (int sp = 0; sp < P.splits; sp += 8) {
+        for (int sp = group; sp < P.splits; sp += 8 * groups) {
             float4 a[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) a[q] = sp + q < P.splits ? __ldcg(reinterpret_cast<const float4 *>(p + (sp + q) * next)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int q = 0; q < 8; ++q) a[q] = sp + q * groups < P.splits ? __ldcg(reinterpret_cast<const float4 *>(p + (sp + q * groups) * next)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int q = 0; q < 8; ++q) { x[0] += a[q].x; x[1] += a[q].y; x[2] += a[q].z; x[3] += a[q].w; }
         }
     }
+    if (SHARED) {
+        shared[threadIdx.x] = make_float4(x[0], x[1], x[2], x[3]);
+        __syncthreads();
+        if (group == 0)
+            for (int g = 1; g < groups; ++g) {
+                const float4 a = shared[g * tx + threadIdx.x];
+                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w;
+            }
+    }
+    if (group > 0 || !in) return;
     if (pos >= 0) {
 #pragma unroll
         for (int n = 0; n < kHeadNear; ++n) {
@@ -1164,12 +1179,14 @@ template <typename K> int launch_plain(K kernel, const HeadRows &P, long long bl
 // Which rows take part, and those one after the other.
 template <bool GRAD, int Q> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
     const long long N = R.T.N, gathers = (N + kGatherRows - 1) / kGatherRows;
-    if (N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD, Q>, R, gathers, 2 * kGatherThreads, stream, "launch tli_head_prepare_kernel");
+    if (Q == 1 && N * R.T.k <= kHeadOneLaunch) return launch_plain(tli_head_prepare_kernel<GRAD, 1>, R, gathers, 2 * kGatherThreads, stream, "launch tli_head_prepare_kernel");
     const int rc = launch_plain(tli_head_targets_kernel<GRAD, Q>, R, gathers, kGatherThreads, stream, "launch tli_head_targets_kernel");
     return rc == TLI_OK ? launch_plain(tli_head_gather_kernel, R, gathers, kGatherThreads, stream, "launch tli_head_gather_kernel") : rc;
 }
 template <bool GRAD> int launch_head_rows(const HeadRows &R, cudaStream_t stream) {
-    return R.T.k <= 32 ? launch_head_rows<GRAD, 1>(R, stream) : launch_head_rows<GRAD, TLI_MAX_TARGETS / 32>(R, stream);
+    if (R.T.k <= 32) return launch_head_rows<GRAD, 1>(R, stream);
+    if (R.T.k <= 64) return launch_head_rows<GRAD, 2>(R, stream);
+    return R.T.k <= 128 ? launch_head_rows<GRAD, 4>(R, stream) : launch_head_rows<GRAD, TLI_MAX_TARGETS / 32>(R, stream);
 }
 
 size_t head_workspace(const tli_ctx *ctx, int32_t N, int32_t H, int32_t k, int32_t side, bool grad) {
@@ -1255,6 +1272,7 @@ int tli_head_loss(tli_ctx *ctx, const tli_head_loss_args *a, void *cuda_stream) 
     // 1000 rows of 32 targets (V 4136, H 1960): 80 us a call with a warp per row and a target at a time, 72 with four at a time, 47 with a CTA per row
     if (a->k <= 4) rc = launch_plain(tli_head_loss_kernel<1, 8>, R, (a->N + 7) / 8, 256, stream, "launch tli_head_loss_kernel");
     else if (a->k <= 32) rc = launch_plain(tli_head_loss_kernel<1, 1>, R, a->N, 256, stream, "launch tli_head_loss_kernel");
+    else if (a->k <= 128) rc = launch_plain(tli_head_loss_kernel<4, 1>, R, a->N, 256, stream, "launch tli_head_loss_kernel");
     else rc = launch_plain(tli_head_loss_kernel<TLI_MAX_TARGETS / 32, 1>, R, a->N, 256, stream, "launch tli_head_loss_kernel");
     return rc;
 }
@@ -1313,8 +1331,14 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
         rc = launch_head_gemm<HEAD_SLOPE>(S, L.cg, ctx, mb * ((cols + kHeadN - 1) / kHeadN), stream);
         if (rc == TLI_OK) rc = launch_head_gemm<HEAD_GRADS>(G, L.cg, ctx, mb * hb * L.splits + (cols + 128 * L.cg - 1) / (128 * L.cg) * hb, stream);
     }
-    if (rc == TLI_OK && (a->grad_hidden || a->status))
-        rc = launch_plain(tli_head_rows_kernel, R, (static_cast<long long>(N) * (R.H / 4) + 255) / 256, 256, stream, "launch tli_head_rows_kernel");
+    R.groups = 1;
+    while (R.groups < 32 && R.groups * 8 < L.splits) R.groups *= 2;        // eight splits a thread, on their way together
+    const long long per_cta = kRowsThreads / R.groups;
+    if (rc == TLI_OK && (a->grad_hidden || a->status)) {
+        const long long ctas = (static_cast<long long>(N) * (R.H / 4) + per_cta - 1) / per_cta;
+        rc = R.groups > 1 ? launch_plain(tli_head_rows_kernel<true>, R, ctas, kRowsThreads, stream, "launch tli_head_rows_kernel")
+                          : launch_plain(tli_head_rows_kernel<false>, R, ctas, kRowsThreads, stream, "launch tli_head_rows_kernel");
+    }
     return rc;
 }
 

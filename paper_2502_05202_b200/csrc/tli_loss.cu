@@ -14,7 +14,9 @@
 
 namespace {
 
-constexpr int kLossThreads = 256;
+// Threads of a CTA: 64 for rows that are a batch or two of theirs (and have as few targets), 256 otherwise: what a short row costs beside its bytes
+// then overlaps with more rows' (5372 bf16 rows of 1726, 7 targets, gradient: 13 us against 24).
+constexpr int kLossThreads = 256, kLossShort = 64;
 // 16-byte vectors a thread has on their way.  bf16 rows are half compute: they want warps (six CTAs per SM) more than loads in flight.  1500 of
 // 50 257 over the intersection: 54 us with eight and three CTAs, 46 with four and four, 42 with four and six; 8192 of 128 256: 361 with four and
 // six, 377 with two and six.  fp32 rows the other way: 4096 of 256 000 in 613 us with eight, 648 with four.  (The next batch asked for before
@@ -150,9 +152,9 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
 // Bound by DRAM on large batches: 4096 fp32 rows of 256 000 (4.2 GB) in 0.61 ms, 6.8 TB/s; 8192 bf16 rows of 128 256 (2.1 GB) in 0.36 ms, 5.8 TB/s, the
 // special-function unit close behind.  On smaller ones by what a row costs beside its bytes (lookups, joins) and by how its CTAs fill the SMs: 1500
 // bf16 rows of 50 257 over the intersection, 20 targets each, 41 us for 151 MB, 34 without mask and with even rows.
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_kernel(const __grid_constant__ LossParams P) {
-    constexpr int WARPS = kLossThreads / 32, kBatch = kLossBatch<DT>;
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS, (DT == TLI_F32 ? 3 : 6) * (kLossThreads / THREADS)) tli_loss_kernel(const __grid_constant__ LossParams P) {
+    constexpr int WARPS = THREADS / 32, kBatch = kLossBatch<DT>;
     __shared__ float sh[WARPS], sh_m[WARPS], sh_s[WARPS];
     __shared__ float part[kLossMaxCluster][2];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_
     auto load = [&](int at) {
         int v[kBatch];
 #pragma unroll
-        for (int q = 0; q < kBatch; ++q) v[q] = at + q * kLossThreads;
+        for (int q = 0; q < kBatch; ++q) v[q] = at + q * THREADS;
         row_vectors<DT, kBatch>(rv.vec0, rv.row, rv.head, P.V, v1, P.T.mask, v, raw);
     };
     load(v0 + tid);                                                // (on their way while the targets are looked up)
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(kLossThreads, DT == TLI_F32 ? 3 : 6) tli_loss_
     }
     if (rank == 0 && target >= 0) z_t = load_elt<DT>(rv.row, target);
 #pragma unroll 1
-    for (int at = v0 + tid + kLossThreads * kBatch; at < v1; at += kLossThreads * kBatch) {
+    for (int at = v0 + tid + THREADS * kBatch; at < v1; at += THREADS * kBatch) {
         load(at);
         loss_batch<DT, kBatch>(raw, s, m, sum);
     }
@@ -277,11 +279,11 @@ template <int THREADS> __device__ __forceinline__ float target_mass(const Target
 
 // Bound by DRAM: 8192 bf16 rows of 128 256 (2.1 GB read, 2.1 written) in 0.65 ms, 6.4 TB/s; 2048 of 49 152 with 32 targets and a mask in 76 us, 5.3 TB/s
 // (92 us with 32 KB of a row per CTA: the targets are then looked up three times a row).
-template <int DT>
-__global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __grid_constant__ LossParams P) {
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS) tli_loss_grad_kernel(const __grid_constant__ LossParams P) {
     constexpr int EPV = Elt<DT>::kPerVec, kBatch = kLossBatch<DT>;
-    __shared__ float sh[kLossThreads / 32], sh_w[TLI_MAX_TARGETS];
-    __shared__ int sh_id[TLI_MAX_TARGETS];
+    __shared__ float sh[THREADS / 32], sh_w[THREADS];
+    __shared__ int sh_id[THREADS];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, seg = static_cast<int>(blockIdx.x % P.nseg);
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
     auto load = [&](int at) {
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
-            const int v = at + q * kLossThreads, e0 = v * EPV - rv.head;
+            const int v = at + q * THREADS, e0 = v * EPV - rv.head;
             raw[q] = make_uint4(Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord, Elt<DT>::kNegInfWord);
             if (v < v1) raw[q] = e0 >= 0 && e0 + EPV <= P.V ? __ldcg(rv.vec0 + v) : ragged_vector<DT>(rv.row, e0, P.V);
         }
@@ -309,12 +311,12 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
     if (here) z_t = load_elt<DT>(rv.row, target);
     const int any = __syncthreads_or(here);
     float mass = 1.f;
-    if (any && P.T.teacher) mass = target_mass<kLossThreads>(P.T, target, teacher, slope.s, sh, sh_id, sh_w);
+    if (any && P.T.teacher) mass = target_mass<THREADS>(P.T, target, teacher, slope.s, sh, sh_id, sh_w);
 #pragma unroll 1
     for (int at = v0 + tid; at < v1; ) {
 #pragma unroll
         for (int q = 0; q < kBatch; ++q) {
-            const int v = at + q * kLossThreads, e0 = v * EPV - rv.head;
+            const int v = at + q * THREADS, e0 = v * EPV - rv.head;
             if (v >= v1) break;
             if (P.T.mask) raw[q] = mask_vector<DT>(raw[q], P.T.mask, e0);
             float x[EPV];
@@ -329,7 +331,7 @@ __global__ void __launch_bounds__(kLossThreads) tli_loss_grad_kernel(const __gri
                     if (e0 + i >= 0 && e0 + i < P.V) set_element<DT>(out, e0 + i, x[i]);
             }
         }
-        at += kLossThreads * kBatch;
+        at += THREADS * kBatch;
         if (at < v1 && !slope.zero) load(at);
     }
     if (any) {
@@ -358,6 +360,11 @@ int check_targets(const tli_ctx *ctx, int32_t N, int32_t k, int32_t side, int32_
     T.mask = support == TLI_SUPPORT_SHARED ? ctx->d_mask : nullptr;
     T.teacher = teacher; T.teacher_bf16 = teacher && teacher_dtype == TLI_BF16;
     return TLI_OK;
+}
+// Rows of nvec vectors in `parts` CTAs each: whether the short CTA is the better one, up to `batches` of its batches.  5372 bf16 rows: 36 us against 41 at
+// eight (16 000 ids), 69 against 66 at sixteen; 4000 fp32 rows, loss: 23 against 28 at four, the same at eight; gradient: 44 against 42 at four.
+bool few_threads(long long nvec, int dtype, int k, int parts, int batches) {
+    return parts == 1 && k <= kLossShort && nvec <= static_cast<long long>(batches) * kLossShort * (dtype == TLI_F32 ? kLossBatch<TLI_F32> : kLossBatch<TLI_BF16>);
 }
 bool aligned8(const void *p) { return reinterpret_cast<uintptr_t>(p) % 8 == 0; }
 
@@ -399,7 +406,13 @@ int tli_loss(tli_ctx *ctx, const tli_loss_args *a, void *cuda_stream) {
         cfg.numAttrs = 2;
     }
     cfg.gridDim = dim3(static_cast<unsigned>(a->N) * P.cluster); cfg.blockDim = dim3(kLossThreads);
-    const cudaError_t e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_F32>, P) : cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_BF16>, P);
+    cudaError_t e;
+    if (few_threads(nvec, a->dtype, a->k, P.cluster, a->dtype == TLI_F32 ? 4 : 8)) {
+        cfg.blockDim = dim3(kLossShort);
+        e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_F32, kLossShort>, P) : cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_BF16, kLossShort>, P);
+    } else {
+        e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_F32, kLossThreads>, P) : cudaLaunchKernelEx(&cfg, tli_loss_kernel<TLI_BF16, kLossThreads>, P);
+    }
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_loss_kernel");
     return TLI_OK;
 }
@@ -430,7 +443,13 @@ int tli_loss_grad(tli_ctx *ctx, const tli_loss_grad_args *a, void *cuda_stream) 
     cudaLaunchAttribute attr[1];
     pdl_config(cfg, attr, reinterpret_cast<cudaStream_t>(cuda_stream));
     cfg.gridDim = dim3(static_cast<unsigned>(a->N) * P.nseg); cfg.blockDim = dim3(kLossThreads);
-    const cudaError_t e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_F32>, P) : cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_BF16>, P);
+    cudaError_t e;
+    if (few_threads(nvec, a->dtype, a->k, P.nseg, a->dtype == TLI_F32 ? 2 : 8)) {
+        cfg.blockDim = dim3(kLossShort);
+        e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_F32, kLossShort>, P) : cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_BF16, kLossShort>, P);
+    } else {
+        e = a->dtype == TLI_F32 ? cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_F32, kLossThreads>, P) : cudaLaunchKernelEx(&cfg, tli_loss_grad_kernel<TLI_BF16, kLossThreads>, P);
+    }
     if (e != cudaSuccess) return cuda_fail(e, "launch tli_loss_grad_kernel");
     return TLI_OK;
 }
