@@ -655,7 +655,8 @@ int tli_loss_grad(tli_ctx *ctx, const tli_loss_grad_args *args, void *cuda_strea
 /*
  * The same loss with z = hidden * weight^T, bf16 operands with fp32 sums, the logits
  * formed tile by tile and never written.  Rows that are left out cost nothing and
- * may hold anything.
+ * may hold anything.  So may the weight rows of ids that do not take part; where they hold
+ * NaN or infinities, tli_head_loss_grad() takes many times as long.
  */
 typedef struct {
     int32_t N;                  /* rows, 0 .. TLI_MAX_HEAD_TOKENS */

@@ -65,6 +65,8 @@ struct HeadGemm {
     const float4 *rowp;                    // {s, m, f, -} of a row
     const int *tid; const float *tval; int k;     // SLOPE: the rows' targets, ids (-1) and elements of G
     float2 *part; long long part_pitch;    // STATS: [tile of the vocabulary][row]
+    // GRADS, with a mask: the operands of d hidden once more, for weight rows outside it that are not finite
+    const __nv_bfloat16 *G, *weight; long long pitch, weight_stride;
 };
 
 // ---- tensor memory, matrix instructions, tensor copies ----
@@ -383,6 +385,33 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                 if (P.mask && left > 0) bits &= __ldg(P.mask + ((P.c0 + w.n + c) >> 5));
                 return bits;
             };
+            // 32 columns of d hidden, this thread's row, over the ids inside the mask alone, without the matrix unit: for tiles that a weight
+            // row outside the mask made NaN (a row that is NaN itself is none of them, and costs nothing).  Rows of the vocabulary one after
+            // the other, the weight's read once by the warp: WAS_MEASURED.
+            auto inside_only = [&](float (&x)[32], int column) {
+                const __nv_bfloat16 *g = P.G + max(0, min(pos, rows - 1)) * P.pitch, *wt = P.weight + P.c0 * P.weight_stride + column;
+                const int end = min(w.k0 + w.ks * kHeadK, P.cols);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = 0.f;
+#pragma unroll 1
+                for (int v = w.k0; v < end; v += 8) {              // (eight ids have their bits in one word: runs and splits begin at multiples of 64)
+                    uint32_t in = __ldg(P.mask + ((P.c0 + v) >> 5)) >> ((P.c0 + v) & 31) & 0xffu;
+                    if (end - v < 8) in &= (1u << (end - v)) - 1u;
+                    if (!in) continue;
+                    float gv[8];
+                    unpack<TLI_BF16>(*reinterpret_cast<const uint4 *>(g + v), gv);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            float y[8];
+                            unpack<TLI_BF16>((in >> u & 1u) && column + i < P.H ? __ldg(reinterpret_cast<const uint4 *>(wt + (v + u) * P.weight_stride + i)) : make_uint4(0, 0, 0, 0), y);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[i + j] = fmaf(gv[u], y[j], x[i + j]);
+                        }
+                }
+                __syncwarp();
+            };
             if constexpr (MODE == HEAD_STATS) {
                 const bool any = m_warp < rows && c0 < P.bn;       // the same for the warp
                 float x[4][32];
@@ -519,6 +548,12 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     if (w.ks == 0) {                               // (a split of a short run may have no step)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) x[i] = 0.f;
+                    } else if (P.mask) {                           // G is 0 outside the mask, but 0 times a weight that is no number is none
+                        float none = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) none = fmaf(x[i], 0.f, none);
+                        if (__any_sync(0xffffffffu, none != none && pos < rows && isfinite(__ldg(P.rowp + max(0, min(pos, rows - 1))).z)))
+                            inside_only(x, w.n + c0 + h);
                     }
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
@@ -1316,6 +1351,7 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     S.a_rows = std::min(128, (N + 7) / 8 * 8);
     bool maps = tensor_map(&S.a, false, R.rows, R.H, N, R.H, S.a_rows) && tensor_map(&S.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadN / L.cg) &&
                 tensor_map(&S.out, false, R.G, L.run, N, L.run, 32) && tensor_map(&G.a, false, R.G, L.run, N, L.run, 128);
+    G.G = R.G; G.pitch = R.pitch; G.weight = R.weight; G.weight_stride = R.weight_stride;
     G.splits = L.splits; G.want_dh = a->grad_hidden != nullptr; G.want_dw = a->grad_weight != nullptr;
     maps = maps && tensor_map(&G.a2, false, R.G, L.run, N, L.run, kHeadK) && tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadK) &&
            tensor_map(&G.b2, false, R.rows, R.H, N, R.H, kHeadK) && tensor_map(&G.out2, true, R.sums, R.H, N, R.H, 32, L.splits);
