@@ -386,8 +386,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                 return bits;
             };
             // 32 columns of d hidden, this thread's row, over the ids inside the mask alone, without the matrix unit: for tiles that a weight
-            // row outside the mask made NaN (a row that is NaN itself is none of them, and costs nothing).  Rows of the vocabulary one after
-            // the other, the weight's read once by the warp: WAS_MEASURED.
+            // row outside the mask made NaN (a row that is NaN itself is none of them, and costs nothing).  2000 x 1024 x 49 152, half of the
+            // ids inside: 25 ms a call, 0.46 without such a row; 1000 x 4096 x 128 256: 137 ms, no tile near the waits' limit of 17 s.
             auto inside_only = [&](float (&x)[32], int column) {
                 const __nv_bfloat16 *g = P.G + max(0, min(pos, rows - 1)) * P.pitch, *wt = P.weight + P.c0 * P.weight_stride + column;
                 const int end = min(w.k0 + w.ks * kHeadK, P.cols);
