@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
         for (int i = 0; tiles.get(P, i, w); ++i) {
             const int m = w.m + static_cast<int>(rank) * 128, pos = m + row, m_warp = m + quarter * 32;
             // What depends on the row is a value here and no branch: a compiler that makes two paths of one (rows that count and rows that
-            // do not) parts the warp in front of the instructions below that a whole warp has to take.
+            // do not) parts the warp in front of the instructions below that a whole warp has to take.  Where one lane alone has done
+            // something (an arrival, a store), the warp meets again before it goes on to them.
             float s = 0.f, top = 0.f, f = 0.f;
             // (G is contracted over its rows in steps of kHeadK: the zeros of the last one are stored too)
             const int rows_stored = MODE == HEAD_SLOPE ? (rows + kHeadK - 1) / kHeadK * kHeadK : rows;
@@ -376,6 +377,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     if constexpr (CG == 1) mbar_arrive(&sm.tempty[acc & 1]);
                     else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr(smem_addr(&sm.tempty[acc & 1]), 0u)) : "memory");
                 }
+                __syncwarp();
                 ++acc;
             };
             // which of 32 columns from column c of the tile on take part
@@ -535,6 +537,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     slab_full();
                     if (store) tensor_store(&P.out, w.n + c0 + c, m_warp, mine);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    __syncwarp();
                 }
                 sum_free();
             } else if (w.split >= 0) {                             // d hidden: fp32 sums, 32 columns a slab
@@ -562,6 +565,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     slab_full();
                     if (store) tensor_store3(&P.out2, w.n + c0 + h, m_warp, w.split, mine, !P.first);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    __syncwarp();
                 }
                 sum_free();
             } else {                                               // d weight: bf16, 64 columns a slab
@@ -589,6 +593,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) tli_head_gemm_kernel(const __
                     slab_full();
                     if (store) tensor_store(&P.out, w.n + c0 + c, P.c0 + m_warp, mine);
                     if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    __syncwarp();
                 }
                 sum_free();
             }
