@@ -809,6 +809,9 @@ _PACK_HEAD_LOSS = struct.Struct("@iiiiiiiPqPqPPPPPPPPN").pack
 _PACK_HEAD_LOSS_GRAD = struct.Struct("@iiiiiiiPqPqPPPPPPPqPqPPN").pack
 
 
+_KEPT_BYTES = 64 << 20                                             # of scratch, per thread and stream of a Verifier
+
+
 def _packed_entries():
     """The entry points of the calls below as functions of (ctx, packed struct, stream)."""
     load()
@@ -882,11 +885,12 @@ class Verifier:
         return out
 
     # The calls below may overlap others on this context.  Scratch is kept per thread and stream (on one stream calls use it one
-    # after the other; two threads could interleave the kernels of theirs), a captured call has its own.  What depends on
-    # shapes alone is worked out once per shape.
+    # after the other; two threads could interleave the kernels of theirs), a captured call has its own, and what is more than
+    # _KEPT_BYTES (a training batch's head gradients, hundreds of MB) goes back to torch's allocator behind the call, which takes
+    # so long that asking for it again is nothing.  What depends on shapes alone is worked out once per shape.
 
     def _scratch(self, need: int) -> torch.Tensor:
-        if torch._C._cuda_isCurrentStreamCapturing() or _current_device() != self._index:
+        if need > _KEPT_BYTES or torch._C._cuda_isCurrentStreamCapturing() or _current_device() != self._index:
             return torch.empty(need, dtype=torch.uint8, device=self.device)
         kept = self._kept.__dict__
         stream = _raw_stream(self._index)
