@@ -610,8 +610,10 @@ int tli_embed_grad(tli_ctx *ctx, const tli_embed_grad_args *args, void *cuda_str
  *
  * Sums are fp32, in an order that does not depend on timing.  The calls are
  * asynchronous on the stream, allocate nothing, only launch kernels (they can be
- * captured) and use of the context only its maps: calls on one context may
- * overlap if their outputs (and workspaces) are distinct.  Errors as for tli_sample().
+ * captured) and use of the context its maps and, the head calls, its sticky time-out
+ * word: calls on one context may overlap if their outputs (and workspaces) are distinct,
+ * but a wait that runs out in one of them flags the rows of the head calls beside it
+ * too (TLI_ROW_TIMEOUT, until tli_reset()).  Errors as for tli_sample().
  */
 enum { TLI_SUPPORT_ALL = 0, TLI_SUPPORT_SHARED = 1 };
 

@@ -24,8 +24,9 @@
 // epilogue and the first and last tiles weigh more); L2 at half its rate, DRAM at a quarter and less.  Long calls run at the power limit (1.5 GHz and below).
 // With one row block the weight is read once for STATS and SLOPE each (DRAM: 131 MB in 17 us of a call of 32).
 // Operands come as they lie in memory: rows along the contracted axis (K-major) or across it (MN-major), 128-byte swizzle either way.
-// All waits are bounded: when one runs out the context's error word is set, every role stops, copies in flight are waited for, tensor
-// memory is given back, and the rows' status says TLI_ROW_TIMEOUT.
+// Waits on the barriers in shared memory are bounded: when one runs out the context's error word is set, every role stops, copies in flight
+// are waited for, tensor memory is given back, and the rows' status says TLI_ROW_TIMEOUT.  (Not bounded are the barriers of the CTA and the
+// pair, which every thread comes to, after a time-out too, and the allocation of tensor memory, which waits for kernels that hold it.)
 
 #include <cuda.h>
 
