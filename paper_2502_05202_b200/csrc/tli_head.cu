@@ -634,7 +634,6 @@ struct HeadRows {
     int *near_id; float *near_off;         // ... the kHeadNear largest of a row, and what bf16 leaves off them
     __nv_bfloat16 *rows;                   // [N, H]
     const float2 *part; long long part_pitch; int tiles;
-    __nv_bfloat16 *G; long long pitch; int c0, cols;
     const float *sums; int splits, groups; // d hidden: [splits][N, H]; threads that share them
     __nv_bfloat16 *grad_hidden; long long grad_hidden_stride; int out_vec;
 };
@@ -1338,7 +1337,7 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     R.tid = reinterpret_cast<int *>(ws + L.tid); R.tval = reinterpret_cast<float *>(ws + L.tval);
     R.tid_of = reinterpret_cast<int *>(ws + L.tid_of); R.tval_of = reinterpret_cast<float *>(ws + L.tval_of);
     R.near_id = reinterpret_cast<int *>(ws + L.near_id); R.near_off = reinterpret_cast<float *>(ws + L.near_off);
-    R.G = reinterpret_cast<__nv_bfloat16 *>(ws + L.G); R.pitch = L.run;
+    __nv_bfloat16 *slopes = reinterpret_cast<__nv_bfloat16 *>(ws + L.G);
     R.sums = reinterpret_cast<const float *>(ws + L.sums); R.splits = L.splits;
     R.grad_hidden = reinterpret_cast<__nv_bfloat16 *>(a->grad_hidden); R.grad_hidden_stride = a->grad_hidden_stride;
     R.out_vec = on_vectors(a->grad_hidden, a->grad_hidden_stride, 2);
@@ -1356,10 +1355,10 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     S.bn = kHeadN; S.early = G.early = N <= 128 * L.cg;
     S.a_rows = std::min(128, (N + 7) / 8 * 8);
     bool maps = tensor_map(&S.a, false, R.rows, R.H, N, R.H, S.a_rows) && tensor_map(&S.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadN / L.cg) &&
-                tensor_map(&S.out, false, R.G, L.run, N, L.run, 32) && tensor_map(&G.a, false, R.G, L.run, N, L.run, 128);
-    G.G = R.G; G.pitch = R.pitch; G.weight = R.weight; G.weight_stride = R.weight_stride;
+                tensor_map(&S.out, false, slopes, L.run, N, L.run, 32) && tensor_map(&G.a, false, slopes, L.run, N, L.run, 128);
+    G.G = slopes; G.pitch = L.run; G.weight = R.weight; G.weight_stride = R.weight_stride;
     G.splits = L.splits; G.want_dh = a->grad_hidden != nullptr; G.want_dw = a->grad_weight != nullptr;
-    maps = maps && tensor_map(&G.a2, false, R.G, L.run, N, L.run, kHeadK) && tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadK) &&
+    maps = maps && tensor_map(&G.a2, false, slopes, L.run, N, L.run, kHeadK) && tensor_map(&G.b, false, R.weight, R.H, R.V, R.weight_stride, kHeadK) &&
            tensor_map(&G.b2, false, R.rows, R.H, N, R.H, kHeadK) && tensor_map(&G.out2, true, R.sums, R.H, N, R.H, 32, L.splits);
     if (maps && a->grad_weight) maps = tensor_map(&G.out, false, a->grad_weight, R.H, R.V, a->grad_weight_stride, 32);
     if (!maps) return cuda_fail(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
@@ -1367,8 +1366,8 @@ int tli_head_loss_grad(tli_ctx *ctx, const tli_head_loss_grad_args *a, void *cud
     rc = launch_head_rows<true>(R, stream);
     for (int i = 0; i < L.runs && rc == TLI_OK; ++i) {
         const int c0 = i * L.run, cols = std::min(L.run, R.V - c0);
-        S.c0 = G.c0 = R.c0 = c0;
-        S.cols = G.cols = R.cols = cols;
+        S.c0 = G.c0 = c0;
+        S.cols = G.cols = cols;
         G.first = i == 0;
         rc = launch_head_gemm<HEAD_SLOPE>(S, L.cg, ctx, mb * ((cols + kHeadN - 1) / kHeadN), stream);
         if (rc == TLI_OK) rc = launch_head_gemm<HEAD_GRADS>(G, L.cg, ctx, mb * hb * L.splits + (cols + 128 * L.cg - 1) / (128 * L.cg) * hb, stream);
