@@ -10,8 +10,12 @@
 //                             <SLOPE>  backward, for a run of the vocabulary: G = g dz in bf16, [rows, run], to the workspace;
 //                             <GRADS>  d hidden += G * weight and d weight = G^T * hidden of that run, one list of tiles.
 //   tli_head_rows_kernel      d hidden from its fp32 sums to bf16, at the rows' places.
-// A run's G has 256 MB at most, whatever the vocabulary: 8192 tokens x 128 256 x 2048 in 9.9 ms; with 128 MB, about what L2 holds, 11.2 (more launches and
-// shorter sums of d hidden), with 64 MB 10.9, with 32 MB 14.1, with 512 MB 10.2.
+// A run's G has 256 MB at most, whatever the vocabulary.  Side by side in one session, 8192 tokens x 128 256 x 2048: 9.9 ms; with 128 MB, about what L2
+// holds, 11.2 (more launches and shorter sums of d hidden), with 64 MB 10.9, with 32 MB 14.1, with 512 MB 10.2.  (A card that has worked for seconds at its
+// power limit, 1.38 GHz, takes 10.6 to 11.0; the first calls after a pause 9.5.)
+// G is held in bf16, the type of the operands of both its products (as two bf16 parts it would double them).  Its rounding is off by half a step, 2^-8
+// at most, and is most of what d hidden and d weight are off beside the rounding of their own: 0.0019 to 0.0023 of fp64 in the norm, 0.0017 without it.
+// d hidden gets back what is left off a row's kHeadNear largest elements; d weight gets nothing back (its rows would need a list of their targets each).
 //
 // tli_head_gemm_kernel: persistent, one CTA per SM or one pair (CG = 2) per two SMs.  A tile of D is 128 CG rows x 256 columns of fp32 in
 // tensor memory, two of them, so that the epilogue of one runs under the products of the next.  Warp 0 fills a ring of stages of
@@ -20,8 +24,9 @@
 // TMA from a slab of each warp's own, so that no warp waits for another.  (Four threads per row and slabs for them take the room of a
 // stage: 17 % slower where the products count.)  With CG = 2 each CTA loads half of both operands and the pair's leader issues the products of both.
 // What bounds it: the matrix unit and the shared memory that feeds it (32 KB in and 32 KB out per stage and CTA of 512 cycles).  Tensor pipe active
-// 86 % of the cycles for STATS at H = 2048 (4096 rows, 64 000 ids), 62 % for SLOPE and 77 % for GRADS at H = 1024 (2000 rows, 49 152 ids, where the
-// epilogue and the first and last tiles weigh more); L2 at half its rate, DRAM at a quarter and less.  Long calls run at the power limit (1.5 GHz and below).
+// 86 % of the cycles for STATS at H = 2048 (4096 rows, 64 000 ids), 64 % for SLOPE (179 us) and 79 % for GRADS (284 us) at H = 1024 (2000 rows, 49 152
+// ids, one run, 1.6 GHz; there the epilogue and the first and last tiles weigh more); L2 at half its rate, DRAM at a quarter and less.  Long calls run at
+// the power limit (1.4 GHz and below).
 // With one row block the weight is read once for STATS and SLOPE each (DRAM: 131 MB in 17 us of a call of 32).
 // Operands come as they lie in memory: rows along the contracted axis (K-major) or across it (MN-major), 128-byte swizzle either way.
 // Waits on the barriers in shared memory are bounded: when one runs out the context's error word is set, every role stops, copies in flight
@@ -37,7 +42,8 @@ constexpr int kHeadThreads = 64 + 32 * kHeadEpilogue;
 // The matrix unit cuts what a sum cannot hold (it does not round): a sum of 2048 products of a logit was 1e-5 off where one rounded at every step
 // is 4e-6 off.  The logits that the statistics are made of are therefore summed in parts, which the epilogue adds up: 128 elements where the
 // weight's way through the SM is what counts (one token: 32.3 us, 31.6 with 256, 33.5 with 64), else half of H but 512 to 1024 (8192 x
-// 128 256 x 2048: one part 3.07 ms and 1e-5 off, two 3.16 and 5e-6, four 3.35 and 2e-6).
+// 128 256 x 2048: one part 3.07 ms and 1e-5 off, two 3.16 and 5e-6, four 3.35 and 2e-6).  SLOPE forms its logits in one part whatever H is: what that
+// leaves off grows with H, by the same count to 3e-4 at 65 536, a tenth of what rounding G to bf16 does.
 constexpr int kHeadK = 64;                 // elements of the contracted axis in a stage: 128 bytes, one swizzle span
 constexpr int kHeadN = 256;                // columns of a tile
 constexpr int kHeadABytes = 128 * kHeadK * 2;
@@ -914,7 +920,8 @@ __global__ void __launch_bounds__(256, 4) tli_head_loss_kernel(const __grid_cons
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, k = P.T.k;
     const long long row0 = static_cast<long long>(blockIdx.x) * ROWS, row = row0 + (ROWS == 1 ? 0 : warp), at = row * k;
-    // The targets' logits are made of the call's inputs: a CTA that finds room beside the products begins with them.
+    // The targets' logits are made of the call's inputs: a CTA on an SM without products (one token: 143 tiles on 148 SMs) begins with them.  Beside a CTA of
+    // the products there is no room, their ring leaves 1792 bytes of shared memory.
     int id[Q];
     float t[Q], z[Q], tau = 1.f, s = 1.f;
     bool takes = false;

@@ -19,7 +19,7 @@ namespace {
 constexpr int kLossThreads = 256, kLossShort = 64;
 // 16-byte vectors a thread has on their way.  bf16 rows are half compute: they want warps (six CTAs per SM) more than loads in flight.  1500 of
 // 50 257 over the intersection: 54 us with eight and three CTAs, 46 with four and four, 42 with four and six; 8192 of 128 256: 361 with four and
-// six, 377 with two and six.  fp32 rows the other way: 4096 of 256 000 in 613 us with eight, 648 with four.  (The next batch asked for before
+// six, 377 with two and six (for six, 40 registers, the compiler keeps 52 bytes a thread in local memory, which those times have in them).  fp32 rows the other way: 4096 of 256 000 in 613 us with eight, 648 with four.  (The next batch asked for before
 // this one is worked on costs registers, hence warps: 48 us.)
 template <int DT> constexpr int kLossBatch = DT == TLI_F32 ? 8 : 4;
 constexpr int kLossMaxCluster = 8;
@@ -149,8 +149,8 @@ __device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
-// Bound by DRAM on large batches: 4096 fp32 rows of 256 000 (4.2 GB) in 0.61 ms, 6.8 TB/s; 8192 bf16 rows of 128 256 (2.1 GB) in 0.36 ms, 5.8 TB/s, the
-// special-function unit close behind.  On smaller ones by what a row costs beside its bytes (lookups, joins) and by how its CTAs fill the SMs: 1500
+// Bound by DRAM on large batches: 4096 fp32 rows of 256 000 (4.2 GB) in 0.61 ms, 6.8 TB/s; 8192 bf16 rows of 128 256 (2.1 GB) in 0.34 to 0.38 ms, 5.6 to
+// 6.2 TB/s, with the special-function unit active 79 % of the cycles and DRAM at 77 % of its nominal rate.  On smaller ones by what a row costs beside its bytes (lookups, joins) and by how its CTAs fill the SMs: 1500
 // bf16 rows of 50 257 over the intersection, 20 targets each, 41 us for 151 MB, 34 without mask and with even rows.
 template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS, (DT == TLI_F32 ? 3 : 6) * (kLossThreads / THREADS)) tli_loss_kernel(const __grid_constant__ LossParams P) {
@@ -277,7 +277,7 @@ template <int THREADS> __device__ __forceinline__ float target_mass(const Target
     return mass / W;
 }
 
-// Bound by DRAM: 8192 bf16 rows of 128 256 (2.1 GB read, 2.1 written) in 0.65 ms, 6.4 TB/s; 2048 of 49 152 with 32 targets and a mask in 76 us, 5.3 TB/s
+// Bound by DRAM: 8192 bf16 rows of 128 256 (2.1 GB read, 2.1 written) in 0.65 ms, 6.4 TB/s; 4096 fp32 rows of as many in 0.67 ms, 6.3 TB/s; 2048 of 49 152 with 32 targets and a mask in 76 us, 5.3 TB/s
 // (92 us with 32 KB of a row per CTA: the targets are then looked up three times a row).
 template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS) tli_loss_grad_kernel(const __grid_constant__ LossParams P) {
