@@ -913,7 +913,8 @@ __device__ __forceinline__ float dot_bf16(const uint4 &a, const uint4 &b, float 
     for (int i = 0; i < 8; ++i) acc = fmaf(x[i], y[i], acc);
     return acc;
 }
-// ROWS rows per CTA: eight, a warp each, for few targets; one, its targets dealt out to the warps four at a time, for more.
+// ROWS rows per CTA: eight, a warp each, for few targets; one, its targets dealt out to the warps four at a time, for more.  (Beyond 128 targets the 64
+// registers of four CTAs per SM leave 124 bytes a thread in local memory.)
 template <int Q, int ROWS>
 __global__ void __launch_bounds__(256, 4) tli_head_loss_kernel(const __grid_constant__ HeadRows P) {
     __shared__ float sh_m[256 / ROWS][ROWS], sh_s[256 / ROWS][ROWS], sh_z[ROWS == 1 ? Q * 32 : 1];

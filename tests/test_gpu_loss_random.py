@@ -6,6 +6,7 @@ Bounds, as derived in test_gpu_loss.py and test_gpu_head.py: with dz = (H / 16 +
     eps (of the sum) = mean of (2^-22 a + 2 dz / tau) under q + high / tau + (V / 8192 + 60) 2^-22 + (V / 1024 + 64) 2^-24,      high = max dz
     loss: eps + 2^-22 |ln sum| + (terms + 1) 2^-20 + 2 high / tau + the targets' share, far (1 + (a + far) / 2) 2^-21, far = max |t - max t| / tau
     G:    |g / tau| (q (2^-22 a + (2 dz + high) / tau + eps + 2^-21) + p (2^-20 + 2 far 2^-22)), then half a step of its type
+          and (1 + |g / tau|) 2^-126: a weight below 2^-126 is flushed to 0 before g / (tau sum), sum >= 1, multiplies it, and the product is flushed again
     a product's sums over n terms: (n / 16 + 8) 2^-23 of sum |G w|, then half a step of bf16."""
 import math
 import random
@@ -91,10 +92,10 @@ def one(rng, gen):
     scale = ((torch.ones(N, device="cuda") if g is None else g).double() * live)[:, None] / tau64
     spread = torch.zeros_like(q).scatter_add_(1, at, p)
     G = scale * (q - spread)
-    err = scale.abs() * (q * (a * 2.0 ** -22 + 2 * dz / tau64 + (high + eps)[:, None] + 2.0 ** -21) + spread * (2.0 ** -20 + far[:, None] * 2.0 ** -21))
+    err = scale.abs() * (q * (a * 2.0 ** -22 + 2 * dz / tau64 + (high + eps)[:, None] + 2.0 ** -21) + spread * (2.0 ** -20 + far[:, None] * 2.0 ** -21)) + TINY * (1 + scale.abs())
     if head:
         b = v.head_loss_grad(h, w, ids, f["stats"], f["target_logits"], grad_loss=g, **how)
-        err = err + 2.0 ** -8 * (G.abs() + err) + TINY
+        err = err + 2.0 ** -8 * (G.abs() + err)
         for got, x, e, s, n in ((b["grad_hidden"], G @ w64, err @ w64.abs(), G.abs() @ w64.abs(), V), (b["grad_weight"], G.T @ h64, err.T @ h64.abs(), G.abs().T @ h64.abs(), N)):
             e = e + (n / 16 + 8) * 2.0 ** -23 * (s + e)
             e = e + 2.0 ** -8 * (x.abs() + e) + TINY
@@ -102,7 +103,7 @@ def one(rng, gen):
         assert (b["grad_hidden"][~live] == 0).all()
     else:
         got = v.loss_grad(rows, ids, f["stats"], grad_loss=g, **how)["grad"]
-        e = err + HALF[rows.dtype] * (G.abs() + err) + TINY
+        e = err + HALF[rows.dtype] * (G.abs() + err)
         assert ((got.double() - G).abs() <= e).all(), (what, ((got.double() - G).abs() - e).max().item())
     v.close()
 
